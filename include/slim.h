@@ -104,6 +104,9 @@ typedef enum {
 /* Element types. Activations (X, dY) are SLIM_F16 or SLIM_BF16; Y and dX are always SLIM_F32. */
 typedef enum { SLIM_F16 = 0, SLIM_BF16 = 1, SLIM_F32 = 2 } slim_dtype;
 
+/* Values kept in 8 bits (see "The 8-bit path" below), where an entry point names it among its types. */
+typedef enum { SLIM_Q8_E4M3 = 3 } slim_dtype_q8;
+
 /* Human-readable name of a status code (static string, never NULL). */
 const char* slim_status_string(int status);
 
@@ -484,6 +487,104 @@ int slim_linear_hybrid_workspace(int64_t M, int64_t N, int64_t K, size_t* bytes)
 int slim_linear_hybrid(const void* X, int64_t M, int64_t N, int64_t K, const uint64_t* tile_info,
                        const uint8_t* payload, size_t payload_bytes, float* Y, void* ws, size_t ws_bytes,
                        void* stream);
+
+/*
+ * ---- The 8-bit path: the norm before a linear layer, activations kept in 8 bits (as the next
+ * layer's input and as the backward's checkpoint), the product of two 8-bit operands with a scale
+ * for each block of 128, and the weight gradient from an 8-bit checkpoint. The thesis also gives a
+ * layer's input 8 bits (SLiM appendix, FP8 input quantization, one scale for a tensor); here every
+ * group of 128 has its own, as the thesis's weights have.
+ *
+ * Format. A value is c 2^e: c an e4m3 code (OCP: sign, 4 exponent bits, 3 mantissa bits, largest
+ * 448, NaN 0x7F and 0xFF, no infinities), e one integer for each group of 128 consecutive values of
+ * a row (of weights: for each 128 x 128 block), the smallest e >= -126 with (largest finite
+ * magnitude of the group) / 2^e <= 448. Codes are value / 2^e rounded to nearest, ties to even. A
+ * NaN or an infinity becomes the code NaN and does not count towards its group's e. Exponents are
+ * stored as bytes e + 127.
+ *   rows      codes uint8 [M][K rounded up to 128], the columns past K zero; exponents uint8
+ *             [M][K/128 rounded up to 4], the bytes past the last group zero.
+ *   weights   tiles of 16 rows and 128 columns, 2 KiB each: codes uint8
+ *             [N/16 up][K/128 up][2][4][16][16], where byte i of [half][block][row] is the code of
+ *             row `row`, column 32 block + 16 half + i of the tile, zeros past N and K; exponents
+ *             uint8 [N/128 up][K/128 rounded up to 4], the bytes past the last block zero.
+ * 16-bit and fp32 operands may have rows of any stride >= their width (in elements) and start at
+ * any element; codes and exponents are 16-byte aligned. M = 0 is allowed: nothing is read, and
+ * sums over rows are zero. Rows are at most 2^22 columns. Every call is asynchronous, allocates
+ * nothing, may be captured into a graph, and gives the same bits for the same inputs.
+ * ----
+ *
+ * slim_quant8 - X [M, K] (`dtype` SLIM_F16, SLIM_BF16 or SLIM_F32, row stride ldx) in 8 bits.
+ * slim_dequant8 - the values back in `dtype`, row stride ldy: exact in fp32 and bf16; in fp16
+ *   rounded to nearest (exact for values that came from fp16 below 63488; past 65519 infinite).
+ */
+int slim_quant8(const void* X, int dtype, int64_t M, int64_t K, int64_t ldx, uint8_t* codes, uint8_t* exps, void* stream);
+int slim_dequant8(const uint8_t* codes, const uint8_t* exps, int64_t M, int64_t K, void* Y, int dtype, int64_t ldy,
+                  void* stream);
+
+/*
+ * slim_pack8 - W [N, K] (`dtype` SLIM_F16, SLIM_BF16 or SLIM_F32, row stride ldw) as an 8-bit weight:
+ *   codes, exps     rows N, columns K: the forward's operand. Both NULL: not wanted.
+ *   codesT, expsT   W^T (rows K, columns N), the same values: the input gradient's. Both NULL: not wanted.
+ * A weight's NaN or infinity becomes NaN; no status word is read back.
+ */
+int slim_pack8(const void* W, int dtype, int64_t N, int64_t K, int64_t ldw, uint8_t* codes, uint8_t* exps,
+               uint8_t* codesT, uint8_t* expsT, void* stream);
+
+/*
+ * slim_linear8 - Y [M, N] = X W^T with an 8-bit weight (rows N, columns K). The input gradient
+ * dX = dY W is the same call on the transposed pack: X = dY, N and K exchanged, codesT, expsT.
+ *   X, xdtype   [M, K]: SLIM_Q8_E4M3 codes with exponents xexps (ldx is not looked at); or SLIM_F16,
+ *               SLIM_BF16 or SLIM_F32 with row stride ldx (xexps is not looked at), which the call
+ *               turns into 8 bits first, to the bit as slim_quant8 does.
+ *   Y, ydtype   out, SLIM_F16 or SLIM_BF16, row stride ldy.
+ *   ws          slim_linear8_workspace(xdtype, M, N, K) bytes (0 when the call needs none); its
+ *               contents need not be kept or cleared.
+ * Products are exact and accumulate in fp32 inside the scaled matrix instructions, whose own sums of
+ * 128 products are a little coarser than fp32 (1.5e-5 of the result's norm), before Y is rounded to
+ * 16 bits; for that reason fp32 is not offered for Y.
+ */
+int slim_linear8_workspace(int xdtype, int64_t M, int64_t N, int64_t K, size_t* bytes);
+int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t N, int64_t K, int64_t ldx,
+                 const uint8_t* codes, const uint8_t* exps, void* Y, int ydtype, int64_t ldy, void* ws, size_t ws_bytes,
+                 void* stream);
+
+/*
+ * slim_grad_w8 - the weight gradient dY^T X with X [M, K] an 8-bit checkpoint (xcodes, xexps).
+ *   dY, dtype   [M, N], SLIM_F16 or SLIM_BF16, row stride lddy. X is widened to the same type (exact
+ *               in bf16; in fp16 as slim_dequant8); products are exact, sums fp32 along M.
+ *   meta        NULL: gW fp32 [N, K], all of it. Else the index words of a value pack (slim_pack16,
+ *               [N, K/8], K % 16 == 0): gW fp32 [N, K/2] at the positions they keep, as slim_grad_w.
+ */
+int slim_grad_w8(const void* dY, int dtype, int64_t lddy, const uint8_t* xcodes, const uint8_t* xexps, int64_t M,
+                 int64_t N, int64_t K, const uint8_t* meta, float* gW, void* stream);
+
+/*
+ * slim_norm - y = (x - mu) rstd gamma + beta for each row x of X [M, K], rstd = (v + eps)^(-1/2), mu
+ * and v the row's mean and variance (divided by K); with rms nonzero mu = 0 and v the mean square.
+ *   X, dtype    SLIM_F16, SLIM_BF16 or SLIM_F32, row stride ldx.
+ *   gamma, beta [K] of `pdtype` (any of the three); NULL for ones and zeros. No beta with rms.
+ *   Y, ydtype   out: `dtype`, row stride ldy; or SLIM_Q8_E4M3: codes with exponents yexps (ldy is not
+ *               looked at), rounded to 8 bits from fp32 without a rounding to 16 bits between.
+ *   mean, rstd  out, fp32 [M], for the backward; mean may be NULL.
+ * eps >= 0. All arithmetic is fp32, the variance taken about the mean.
+ *
+ * slim_norm_bwd - the gradients, with xh = (x - mean) rstd and t = dy gamma:
+ *   dx = rstd (t - mean_k(t) - xh mean_k(t xh)), dgamma = sum over rows of dy xh, dbeta = that of dy.
+ *   dY, dtype   [M, K], row stride lddy; dX out, the same type, row stride lddx (may be dY).
+ *   X, xdtype   the forward's input: `dtype` with row stride ldx, or SLIM_Q8_E4M3 with xexps: a
+ *               checkpoint of it (slim_quant8), whose rounded values stand in for x.
+ *   gamma       as in the forward.
+ *   mean, rstd  the forward's; mean NULL for the RMS norm (whose dx has no mean_k(t)).
+ *   dgamma, dbeta  out, fp32 [K]; NULL if not wanted.
+ *   ws          slim_norm_bwd_workspace(M, K) bytes; its contents need not be kept or cleared.
+ */
+int slim_norm(const void* X, int dtype, int64_t M, int64_t K, int64_t ldx, const void* gamma, const void* beta,
+              int pdtype, int rms, float eps, void* Y, int ydtype, int64_t ldy, uint8_t* yexps, float* mean, float* rstd,
+              void* stream);
+int slim_norm_bwd_workspace(int64_t M, int64_t K, size_t* bytes);
+int slim_norm_bwd(const void* dY, int dtype, int64_t lddy, const void* X, int xdtype, const uint8_t* xexps, int64_t ldx,
+                  int64_t M, int64_t K, const void* gamma, int pdtype, const float* mean, const float* rstd, void* dX,
+                  int64_t lddx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Per-kernel timing for benchmarks (host-side bookkeeping; not part of the layer's math).

@@ -26,6 +26,8 @@ the thesis' definitions:
 * SLiM-LoRA's saliency-based adapters (``slim_lora``; SLiM, eq. lora_svd and Alg. lora).
 * PATCH's hybrid dense / 2:4 tile weight and its product (``patch_hybrid``; PATCH, "Efficient
   deployment of PATCH").
+* The 8-bit path (``act8``): e4m3 codes with a power of two for each group of 128, their product, and
+  the norms with their backward pass.
 
 Parity status per function is stated in ``slim_oracle``'s module docstring.
 """
@@ -34,3 +36,4 @@ from . import slope_train  # noqa: F401
 from . import slim_quant  # noqa: F401
 from . import slim_lora  # noqa: F401
 from . import patch_hybrid  # noqa: F401
+from . import act8  # noqa: F401

@@ -73,3 +73,4 @@ int slim_check_linear(bool bwd, const void* X, int xdtype, int64_t M, int64_t N,
                       const void* ws, size_t ws_bytes, SlimPlan* plan);
 
 inline bool slim_aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline bool slim_aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }

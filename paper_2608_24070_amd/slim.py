@@ -22,6 +22,7 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "slim.h")
 (SLIM_OK, SLIM_EINVAL, SLIM_ESHAPE, SLIM_EDTYPE, SLIM_EALIGN, SLIM_ENONFINITE, SLIM_EWORKSPACE, SLIM_EDEVICE,
  SLIM_EUNSUPPORTED, SLIM_ERANGE) = range(10)
 SLIM_F16, SLIM_BF16, SLIM_F32 = 0, 1, 2
+SLIM_Q8_E4M3 = 3
 
 _c_i64 = ctypes.c_int64
 _c_p = ctypes.c_void_p
@@ -60,6 +61,19 @@ _SIGS = {
     "slim_lora_workspace": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
     "slim_lora": (ctypes.c_int, [_c_p, _c_i64, _c_i64, _c_p, _c_p, _c_p, _c_p, ctypes.c_int, _c_i64, _c_i64, _c_p,
                                  _c_p, _c_p, ctypes.POINTER(ctypes.c_int), _c_p, ctypes.c_size_t, _c_p]),
+    "slim_quant8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p]),
+    "slim_dequant8": (ctypes.c_int, [_c_p, _c_p, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_i64, _c_p]),
+    "slim_pack8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p, _c_p, _c_p]),
+    "slim_linear8_workspace": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_linear8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
+                                    ctypes.c_int, _c_i64, _c_p, ctypes.c_size_t, _c_p]),
+    "slim_grad_w8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p]),
+    "slim_norm": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, ctypes.c_int, ctypes.c_int,
+                                 ctypes.c_float, _c_p, ctypes.c_int, _c_i64, _c_p, _c_p, _c_p, _c_p]),
+    "slim_norm_bwd_workspace": (ctypes.c_int, [_c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_norm_bwd": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64,
+                                     _c_p, ctypes.c_int, _c_p, _c_p, _c_p, _c_i64, _c_p, _c_p, _c_p, ctypes.c_size_t,
+                                     _c_p]),
     "slim_timing_enable": (ctypes.c_int, [ctypes.c_int]),
     "slim_timing_reset": (ctypes.c_int, []),
     "slim_timing_read": (ctypes.c_int, [ctypes.c_char_p, ctypes.c_size_t]),
@@ -229,6 +243,48 @@ def slim_sparse_add(A, B, beta, gamma, out, count, stream) -> int:
 
 def slim_update_pack16(Wnew, count, vals, stream) -> int:
     return lib().slim_update_pack16(Wnew, count, vals, stream)
+
+
+def slim_quant8(X, dtype, M, K, ldx, codes, exps, stream) -> int:
+    return lib().slim_quant8(X, dtype, M, K, ldx, codes, exps, stream)
+
+
+def slim_dequant8(codes, exps, M, K, Y, dtype, ldy, stream) -> int:
+    return lib().slim_dequant8(codes, exps, M, K, Y, dtype, ldy, stream)
+
+
+def slim_pack8(W, dtype, N, K, ldw, codes, exps, codesT, expsT, stream) -> int:
+    return lib().slim_pack8(W, dtype, N, K, ldw, codes, exps, codesT, expsT, stream)
+
+
+def slim_linear8_workspace(xdtype, M, N, K) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().slim_linear8_workspace(xdtype, M, N, K, ctypes.byref(out)), "slim_linear8_workspace")
+    return out.value
+
+
+def slim_linear8(X, xdtype, xexps, M, N, K, ldx, codes, exps, Y, ydtype, ldy, ws, ws_bytes, stream) -> int:
+    return lib().slim_linear8(X, xdtype, xexps, M, N, K, ldx, codes, exps, Y, ydtype, ldy, ws, ws_bytes, stream)
+
+
+def slim_grad_w8(dY, dtype, lddy, xcodes, xexps, M, N, K, meta, gW, stream) -> int:
+    return lib().slim_grad_w8(dY, dtype, lddy, xcodes, xexps, M, N, K, meta, gW, stream)
+
+
+def slim_norm(X, dtype, M, K, ldx, gamma, beta, pdtype, rms, eps, Y, ydtype, ldy, yexps, mean, rstd, stream) -> int:
+    return lib().slim_norm(X, dtype, M, K, ldx, gamma, beta, pdtype, rms, eps, Y, ydtype, ldy, yexps, mean, rstd, stream)
+
+
+def slim_norm_bwd_workspace(M, K) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().slim_norm_bwd_workspace(M, K, ctypes.byref(out)), "slim_norm_bwd_workspace")
+    return out.value
+
+
+def slim_norm_bwd(dY, dtype, lddy, X, xdtype, xexps, ldx, M, K, gamma, pdtype, mean, rstd, dX, lddx, dgamma, dbeta, ws,
+                  ws_bytes, stream) -> int:
+    return lib().slim_norm_bwd(dY, dtype, lddy, X, xdtype, xexps, ldx, M, K, gamma, pdtype, mean, rstd, dX, lddx, dgamma,
+                               dbeta, ws, ws_bytes, stream)
 
 
 def slim_timing_enable(on: bool) -> int:
@@ -661,3 +717,260 @@ def update_pack16(Wnew, p: dict, stream=None) -> dict:
     _on_gpu(Wnew)
     _check(slim_update_pack16(_ptr(Wnew), Wnew.numel(), _ptr(p["vals"]), _stream(stream)), "slim_update_pack16")
     return p
+
+
+# ------------------------------------------------- the 8-bit path
+
+_FLOAT_CODES: dict = {}
+
+
+def _float_code(dt) -> int:
+    """slim_dtype of a torch floating type (fp16, bf16, fp32)."""
+    if not _FLOAT_CODES:
+        torch = _torch()
+        _FLOAT_CODES.update({torch.float16: SLIM_F16, torch.bfloat16: SLIM_BF16, torch.float32: SLIM_F32})
+    code = _FLOAT_CODES.get(dt)
+    if code is None:
+        raise TypeError(f"expected fp16, bf16 or fp32, got {dt}")
+    return code
+
+
+def _ld(t, what: str) -> int:
+    """Row stride of a 2-D tensor on the GPU whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what} must be a 2-D tensor on the GPU")
+    ld, step = t.stride()
+    cols = t.shape[1]
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    if ld < cols:            # one row, or rows that overlap (expanded)
+        if t.shape[0] > 1:
+            raise ValueError(f"{what} must not have overlapping rows")
+        ld = cols
+    return ld
+
+
+def _out(out, shape, dtype, like, what: str = "out"):
+    """`out` checked, or a new tensor."""
+    if out is None:
+        return _torch().empty(shape, dtype=dtype, device=like.device)
+    if out.shape != shape or out.dtype != dtype:
+        raise ValueError(f"{what} must be {tuple(shape)} of {dtype}, got {tuple(out.shape)} of {out.dtype}")
+    return out
+
+
+def _rows8(q: dict):
+    """Checked parts of 8-bit rows: codes, exps, M, K."""
+    codes, exps, M, K = q["codes"], q["exps"], q["M"], q["K"]
+    if codes.shape != (M, -(-K // 128) * 128) or exps.shape != (M, -(-K // 512) * 4):
+        raise ValueError("codes and exponents do not have the shape of the 8-bit rows")
+    _on_gpu(codes, exps)
+    return codes, exps, M, K
+
+
+def _empty_rows8(M: int, K: int, device) -> dict:
+    torch = _torch()
+    return {"codes": torch.empty((M, -(-K // 128) * 128), dtype=torch.uint8, device=device),
+            "exps": torch.empty((M, -(-K // 512) * 4), dtype=torch.uint8, device=device), "M": M, "K": K}
+
+
+def _one_device(a, *ts):
+    for t in ts:
+        if t is not None and t.device != a.device:
+            raise ValueError(f"tensors must be on one device, got {a.device} and {t.device}")
+
+
+def quant8(X, out: dict | None = None, stream=None) -> dict:
+    """slim_quant8 of X [M, K] (fp16, bf16 or fp32; rows of any stride): {"codes" uint8 [M, K up to 128],
+    "exps" uint8, "M", "K"}."""
+    ldx = _ld(X, "X")
+    M, K = X.shape
+    if out is None:
+        out = _empty_rows8(M, K, X.device)
+    elif (out["M"], out["K"]) != (M, K):
+        raise ValueError("out is of another shape")
+    codes, exps, _, _ = _rows8(out)
+    _one_device(X, codes, exps)
+    _check(slim_quant8(X.data_ptr(), _float_code(X.dtype), M, K, ldx, codes.data_ptr(), exps.data_ptr(), _stream(stream)),
+           "slim_quant8")
+    return out
+
+
+def dequant8(q: dict, dtype=None, out=None, stream=None):
+    """slim_dequant8: the values of 8-bit rows as [M, K] of `dtype` (bf16 if neither it nor `out` is given)."""
+    codes, exps, M, K = _rows8(q)
+    if dtype is None:
+        dtype = out.dtype if out is not None else _torch().bfloat16
+    out = _out(out, (M, K), dtype, codes)
+    _one_device(codes, out)
+    _check(slim_dequant8(codes.data_ptr(), exps.data_ptr(), M, K, out.data_ptr(), _float_code(dtype), _ld(out, "out"),
+                         _stream(stream)), "slim_dequant8")
+    return out
+
+
+def pack8(W, bwd: bool = False, stream=None) -> dict:
+    """slim_pack8 of W [N, K] (fp16, bf16 or fp32): {"codes", "exps", "N", "K"}, with `bwd` also the input gradient's
+    {"codesT", "expsT"}."""
+    torch = _torch()
+    ldw = _ld(W, "W")
+    N, K = W.shape
+    up = lambda a, b: -(-a // b)
+
+    def empty(n, k):
+        return (torch.empty((up(n, 16), up(k, 128), 2, 4, 16, 16), dtype=torch.uint8, device=W.device),
+                torch.empty((up(n, 128), up(k, 512) * 4), dtype=torch.uint8, device=W.device))
+
+    out = {"N": N, "K": K}
+    out["codes"], out["exps"] = empty(N, K)
+    if bwd:
+        out["codesT"], out["expsT"] = empty(K, N)
+    _check(slim_pack8(W.data_ptr(), _float_code(W.dtype), N, K, ldw, _ptr(out["codes"]), _ptr(out["exps"]),
+                      _ptr(out.get("codesT")), _ptr(out.get("expsT")), _stream(stream)), "slim_pack8")
+    return out
+
+
+_ws8: dict = {}
+
+
+def _workspace8(nbytes: int, device, stream):
+    """The 8-bit calls' workspace, kept per (device, stream). Its contents are of no interest between calls, so it is not
+    slim_linear's, whose counters have to stay zero."""
+    if not nbytes:
+        return None
+    key = (device, _stream(stream))
+    ws = _ws8.get(key)
+    if ws is None or ws.numel() < nbytes:
+        ws = _ws8[key] = _torch().empty(max(nbytes, 1 << 16), dtype=_torch().uint8, device=device)
+    return ws
+
+
+def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, stream, where: str):
+    if codes.shape != (-(-N // 16), -(-K // 128), 2, 4, 16, 16) or exps.shape != (-(-N // 128), -(-K // 512) * 4):
+        raise ValueError("codes and exponents do not have the shape of the 8-bit weight")
+    if isinstance(X, dict):
+        x, xe, M, k = _rows8(X)
+        xdt, ldx = SLIM_Q8_E4M3, 0
+    else:
+        x, xe, ldx, xdt = X, None, _ld(X, "X"), _float_code(X.dtype)
+        M, k = X.shape
+    if k != K:
+        raise ValueError("the rows' width does not match the pack")
+    if dtype is None:
+        torch = _torch()
+        dtype = out.dtype if out is not None else torch.float16 if xdt == SLIM_F16 else torch.bfloat16
+    out = _out(out, (M, N), dtype, x)
+    _one_device(x, codes, exps, out)
+    _on_gpu(codes, exps)
+    need = slim_linear8_workspace(xdt, M, N, K)
+    if ws is None:
+        ws = _workspace8(need, x.device, stream)
+    _check(slim_linear8(x.data_ptr(), xdt, _ptr(xe), M, N, K, ldx, codes.data_ptr(), exps.data_ptr(), out.data_ptr(),
+                        _float_code(dtype), _ld(out, "out"), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)),
+           where)
+    return out
+
+
+def linear8(X, p: dict, dtype=None, out=None, ws=None, stream=None):
+    """slim_linear8: Y [M, N] = X W^T with an 8-bit weight (pack8). X [M, K]: 8-bit rows (quant8, norm) or an fp16, bf16
+    or fp32 tensor, which the call turns into 8 bits. Y in `dtype`, fp16 or bf16 (default: fp16 for fp16 X, else bf16)."""
+    return _product8(X, p["codes"], p["exps"], p["N"], p["K"], dtype, out, ws, stream, "slim_linear8")
+
+
+def bwd_dx8(dY, p: dict, dtype=None, out=None, ws=None, stream=None):
+    """slim_linear8 on the transposed pack: dX [M, K] = dY W for dY [M, N] (pack8 with bwd=True); types as linear8."""
+    return _product8(dY, p["codesT"], p["expsT"], p["K"], p["N"], dtype, out, ws, stream, "slim_linear8")
+
+
+def grad_w8(dY, q: dict, p: dict | None = None, out=None, stream=None):
+    """slim_grad_w8: dY^T X for dY [M, N] (fp16, bf16) and X [M, K] in 8 bits: fp32 [N, K], or with a value pack `p`
+    (pack16) fp32 [N, K/2] at the positions it keeps."""
+    torch = _torch()
+    xc, xe, M, K = _rows8(q)
+    ldy = _ld(dY, "dY")
+    if dY.shape[0] != M:
+        raise ValueError("dY and the checkpoint must have one number of rows")
+    N = dY.shape[1]
+    meta = None
+    if p is not None:
+        meta = p["meta"]
+        if meta.shape != (N, K // 8):
+            raise ValueError("the value pack does not match dY and the checkpoint")
+        _on_gpu(meta)
+    out = _out(out, (N, K if p is None else K // 2), torch.float32, dY)
+    _on_gpu(out)
+    _one_device(dY, xc, xe, meta, out)
+    _check(slim_grad_w8(dY.data_ptr(), _dtype_code(dY), ldy, xc.data_ptr(), xe.data_ptr(), M, N, K, _ptr(meta),
+                        out.data_ptr(), _stream(stream)), "slim_grad_w8")
+    return out
+
+
+def _params(K: int, *ps) -> int:
+    """The one slim_dtype of a norm's parameters, each contiguous [K] or None."""
+    code = None
+    for t in ps:
+        if t is None:
+            continue
+        if t.shape != (K,) or not t.is_contiguous():
+            raise ValueError("gamma and beta must be contiguous vectors of the rows' width")
+        c = _float_code(t.dtype)
+        if code is not None and c != code:
+            raise TypeError("gamma and beta must have one dtype")
+        code = c
+    return SLIM_F32 if code is None else code
+
+
+def norm(X, gamma=None, beta=None, eps: float = 1e-5, rms: bool = False, q8: bool = False, out=None, stream=None):
+    """slim_norm over the rows of X [M, K] (fp16, bf16 or fp32): layer norm, or with `rms` the RMS norm. Returns (Y, mean,
+    rstd): Y of X's type, or with `q8` 8-bit rows (as quant8); mean and rstd fp32 [M] for norm_bwd, mean None with `rms`."""
+    torch = _torch()
+    ldx = _ld(X, "X")
+    M, K = X.shape
+    dt, pdt = _float_code(X.dtype), _params(K, gamma, beta)
+    stats = torch.empty((2, M), dtype=torch.float32, device=X.device)
+    mean, rstd = None if rms else stats[0], stats[1]
+    if q8:
+        if out is None:
+            out = _empty_rows8(M, K, X.device)
+        y, ye, m, k = _rows8(out)
+        if (m, k) != (M, K):
+            raise ValueError("out is of another shape")
+        ydt, ldy = SLIM_Q8_E4M3, 0
+    else:
+        out = y = _out(out, (M, K), X.dtype, X)
+        ye, ydt, ldy = None, dt, _ld(y, "out")
+    _one_device(X, gamma, beta, y, ye)
+    _check(slim_norm(X.data_ptr(), dt, M, K, ldx, _ptr(gamma), _ptr(beta), pdt, 1 if rms else 0, eps, y.data_ptr(), ydt,
+                     ldy, _ptr(ye), _ptr(mean), rstd.data_ptr(), _stream(stream)), "slim_norm")
+    return out, mean, rstd
+
+
+def norm_bwd(dY, X, gamma, mean, rstd, out=None, ws=None, stream=None):
+    """slim_norm_bwd: (dX, dgamma, dbeta) from dY [M, K], the forward's input X (dY's type, or its 8-bit checkpoint from
+    quant8), gamma (or None) and the forward's mean and rstd; mean None: RMS norm, dbeta None. dX of dY's type, dgamma
+    and dbeta fp32."""
+    torch = _torch()
+    lddy = _ld(dY, "dY")
+    M, K = dY.shape
+    dt, pdt = _float_code(dY.dtype), _params(K, gamma)
+    if isinstance(X, dict):
+        x, xe, m, k = _rows8(X)
+        xdt, ldx = SLIM_Q8_E4M3, 0
+    else:
+        x, xe, xdt, ldx = X, None, _float_code(X.dtype), _ld(X, "X")
+        m, k = X.shape
+    if (m, k) != (M, K):
+        raise ValueError("dY and X must have one shape")
+    for t in (mean, rstd):
+        if t is not None and (t.shape != (M,) or t.dtype != torch.float32 or not t.is_contiguous()):
+            raise ValueError("mean and rstd must be contiguous fp32 vectors of the number of rows")
+    out = _out(out, (M, K), dY.dtype, dY)
+    grads = torch.empty((1 if mean is None else 2, K), dtype=torch.float32, device=dY.device)
+    dgamma, dbeta = grads[0], None if mean is None else grads[1]
+    _one_device(dY, x, xe, gamma, mean, rstd, out)
+    need = slim_norm_bwd_workspace(M, K)
+    if ws is None:
+        ws = _workspace8(need, dY.device, stream)
+    _check(slim_norm_bwd(dY.data_ptr(), dt, lddy, x.data_ptr(), xdt, _ptr(xe), ldx, M, K, _ptr(gamma), pdt, _ptr(mean),
+                         rstd.data_ptr(), out.data_ptr(), _ld(out, "out"), dgamma.data_ptr(), _ptr(dbeta), _ptr(ws),
+                         0 if ws is None else ws.numel(), _stream(stream)), "slim_norm_bwd")
+    return out, dgamma, dbeta

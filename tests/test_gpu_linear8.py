@@ -1,0 +1,147 @@
+"""slim_linear8 against the oracle's 64-bit product of the same 8-bit values, forward and input gradient.
+
+Bound, per element: the rounding of Y to 16 bits, u |y| with u = 2^-8 (bf16) or 2^-11 (fp16), and for the matrix unit's own
+sums 2^-14 of the sum of the products' magnitudes (they are kept to at least 14 bits below the largest of each 128)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import act8
+from paper_2608_24070_amd import slim, synth
+from tests.gpu_common import dev, host
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+U = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+
+
+def check(Y, x, w, out):
+    ref, mag = x @ w.T, np.abs(x) @ np.abs(w).T
+    got = Y.double().cpu().numpy()
+    lim = U[out] * np.abs(ref) + 2.0 ** -14 * mag + (2.0 ** -24 if out == "fp16" else 0.0)
+    bad = ~(np.abs(got - ref) <= lim)
+    assert not bad.any(), f"{bad.sum()} of {bad.size} elements out of bound, first {np.argwhere(bad)[:3].tolist()}"
+
+
+def inputs(m, n, k, dtype, seed=0):
+    rng = synth.stream(seed, f"linear8/{m}x{n}x{k}/{dtype}")
+    x = rng.standard_normal((m, k)) * 4.0 ** rng.integers(-2, 3, (m, 1)) * np.where(rng.random(k) < 0.01, 20.0, 1.0)
+    w = rng.standard_normal((n, k)) * 0.02 * 2.0 ** rng.integers(-2, 3, (n, 1))
+    t = torch.from_numpy(x.astype(np.float32)).to(DT[dtype])
+    return t, w.astype(np.float32)
+
+
+def values(w):
+    codes, e = act8.quant_weight(w.astype(np.float64))
+    return act8.values_weight(codes, e)
+
+
+SIZES = [(1, 1, 1), (1, 16, 128), (1, 4096, 512), (3, 100, 300), (16, 257, 1000), (17, 64, 129), (33, 130, 640), (45, 48, 2100),
+         (64, 513, 384), (65, 300, 256), (127, 17, 5000), (128, 256, 128), (200, 700, 900), (257, 260, 1152), (300, 1030, 520),
+         (513, 515, 700)]
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp16", "fp16"), ("fp32", "bf16"), ("bf16", "fp16")])
+def test_forward(m, n, k, dtype, out):
+    print(f"linear8 m={m} n={n} k={k} {dtype} -> {out}", flush=True)
+    t, w = inputs(m, n, k, dtype)
+    p = slim.pack8(dev(w))
+    x = act8.values_rows(*act8.quant_rows(t.double().numpy()), k)
+    Y = slim.linear8(t.cuda(), p, dtype=DT[out])
+    assert Y.shape == (m, n) and Y.dtype == DT[out]
+    check(Y, x, values(w), out)
+    # rows that are in 8 bits already give the same bits
+    assert torch.equal(slim.linear8(slim.quant8(t.cuda()), p, dtype=DT[out]), Y)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 512, 256), (20, 130, 300), (70, 1000, 129), (300, 640, 520)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_input_gradient(m, n, k, dtype):
+    print(f"linear8 dx m={m} n={n} k={k} {dtype}", flush=True)
+    t, _ = inputs(m, 1, n, dtype, seed=1)
+    _, w = inputs(1, n, k, dtype, seed=2)
+    p = slim.pack8(dev(w), bwd=True)
+    dy = act8.values_rows(*act8.quant_rows(t.double().numpy()), n)
+    check(slim.bwd_dx8(t.cuda(), p), dy, values(w).T, dtype)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 40, 256), (50, 300, 384), (150, 290, 1300), (400, 600, 900)])
+def test_small_integers_are_exact(m, n, k):
+    # values -2 .. 2 in a few places a row: every sum is a small integer, exact in fp16 whatever the order
+    rng = synth.stream(7, f"linear8/int/{m}x{n}x{k}")
+    x = rng.integers(-2, 3, (m, k)) * (rng.random((m, k)) < 0.2)
+    w = rng.integers(-2, 3, (n, k)) * (rng.random((n, k)) < 0.2)
+    p = slim.pack8(dev(w.astype(np.float32)), bwd=True)
+    Y = slim.linear8(dev(x.astype(np.float32)).to(torch.float16), p)
+    assert np.array_equal(host(Y).astype(int), x @ w.T)
+    # <X W^T, dY> = <X, dY W>: the input gradient is the forward's transpose
+    dy = rng.integers(-1, 2, (m, n)) * (rng.random((m, n)) < 0.2)
+    dX = host(slim.bwd_dx8(dev(dy.astype(np.float32)).to(torch.float16), p)).astype(int)
+    assert np.array_equal(dX, dy @ w) and (dX * x).sum() == (host(Y).astype(int) * dy).sum()
+
+
+@pytest.mark.parametrize("m", [5, 90, 300])
+def test_strides_and_the_bytes_around_the_result(m):
+    t, w = inputs(m + 3, 333, 600, "bf16", seed=3)
+    view = t.cuda()[2:2 + m, 11:11 + 517]
+    p = slim.pack8(dev(w)[:, 11:11 + 517])
+    buf = torch.full((m + 2, 400), -7.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[1:1 + m, 9:9 + 333]
+    slim.linear8(view, p, out=out)
+    assert torch.equal(out, slim.linear8(view.contiguous(), p))
+    buf[1:1 + m, 9:342] = -7.0
+    assert bool((buf == -7).all())
+
+
+@pytest.mark.parametrize("m", [4, 40, 200])
+def test_nan_rows_stay_apart(m):
+    t, w = inputs(m, 70, 300, "bf16", seed=4)
+    p = slim.pack8(dev(w))
+    clean = slim.linear8(t.cuda(), p)
+    t[1, 40], t[3, 299] = float("nan"), float("inf")
+    Y = slim.linear8(t.cuda(), p)
+    rows = torch.ones(m, dtype=torch.bool)
+    rows[[1, 3]] = False
+    assert bool(Y[[1, 3]].isnan().all()) and torch.equal(Y[rows.cuda()], clean[rows.cuda()])
+
+
+def test_no_rows_and_results_repeat():
+    _, w = inputs(1, 70, 300, "bf16")
+    p = slim.pack8(dev(w))
+    assert slim.linear8(torch.empty((0, 300), dtype=torch.bfloat16, device="cuda"), p).shape == (0, 70)
+    t, w = inputs(333, 515, 1300, "fp16", seed=5)
+    p = slim.pack8(dev(w))
+    first = slim.linear8(t.cuda(), p)
+    assert all(torch.equal(slim.linear8(t.cuda(), p), first) for _ in range(3))
+
+
+def test_another_stream():
+    t, w = inputs(130, 300, 512, "bf16", seed=6)
+    p, x = slim.pack8(dev(w)), t.cuda()
+    want = slim.linear8(x, p)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = slim.linear8(x, p, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("m", [1, 40, 300])
+def test_graph_replays(m):
+    t, w = inputs(m, 515, 640, "bf16", seed=8)
+    x, p = t.cuda(), slim.pack8(dev(w))
+    ws = torch.empty(max(slim.slim_linear8_workspace(slim.SLIM_BF16, m, 515, 640), 256), dtype=torch.uint8, device="cuda")
+    out = torch.empty((m, 515), dtype=torch.bfloat16, device="cuda")
+    slim.linear8(x, p, out=out, ws=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        slim.linear8(x, p, out=out, ws=ws)
+    for rep in range(3):
+        x.copy_(inputs(m, 1, 640, "bf16", seed=20 + rep)[0])
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, slim.linear8(x, p)), rep
