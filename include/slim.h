@@ -539,9 +539,9 @@ int slim_pack8(const void* W, int dtype, int64_t N, int64_t K, int64_t ldw, uint
  *   Y, ydtype   out, SLIM_F16 or SLIM_BF16, row stride ldy.
  *   ws          slim_linear8_workspace(xdtype, M, N, K) bytes (0 when the call needs none); its
  *               contents need not be kept or cleared.
- * Products are exact and accumulate in fp32 inside the scaled matrix instructions, whose own sums of
- * 128 products are a little coarser than fp32 (1.5e-5 of the result's norm), before Y is rounded to
- * 16 bits; for that reason fp32 is not offered for Y.
+ * Sums are fp32, but for those of each eight consecutive products, which the scaled matrix instructions
+ * cut at 2^-13 of the largest of them: together 1.5e-5 of the result's norm, before Y is rounded to
+ * 16 bits. For that reason fp32 is not offered for Y.
  */
 int slim_linear8_workspace(int xdtype, int64_t M, int64_t N, int64_t K, size_t* bytes);
 int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t N, int64_t K, int64_t ldx,
@@ -554,9 +554,13 @@ int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int
  *               in bf16; in fp16 as slim_dequant8); products are exact, sums fp32 along M.
  *   meta        NULL: gW fp32 [N, K], all of it. Else the index words of a value pack (slim_pack16,
  *               [N, K/8], K % 16 == 0): gW fp32 [N, K/2] at the positions they keep, as slim_grad_w.
+ *   ws          slim_grad_w8_workspace(M, N, K, meta != NULL, aligned) bytes, where `aligned` says that
+ *               dY is 16-byte aligned and lddy a multiple of 8 below 2^22 (0 always suffices); its
+ *               contents need not be kept or cleared.
  */
+int slim_grad_w8_workspace(int64_t M, int64_t N, int64_t K, int masked, int aligned, size_t* bytes);
 int slim_grad_w8(const void* dY, int dtype, int64_t lddy, const uint8_t* xcodes, const uint8_t* xexps, int64_t M,
-                 int64_t N, int64_t K, const uint8_t* meta, float* gW, void* stream);
+                 int64_t N, int64_t K, const uint8_t* meta, float* gW, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * slim_norm - y = (x - mu) rstd gamma + beta for each row x of X [M, K], rstd = (v + eps)^(-1/2), mu

@@ -5,6 +5,8 @@
 // on the way into LDS (exact in bf16, and in fp16 for checkpoints of fp16 values below 63488), and the products run on
 // v_mfma_f32_32x32x16 with fp32 accumulators. X moves at half the bytes of a 16-bit activation.
 #include <hip/hip_runtime.h>
+#include <algorithm>
+#include <type_traits>
 
 #include "slim_launch.h"
 #include "slim_q8.h"
@@ -54,121 +56,533 @@ SLIM_DEV void store_grad4(float* gW, const uint8_t* meta, int64_t n, int64_t k, 
   }
 }
 
-// 128 (k) x 128 (n) tiles, four waves of 64 x 64; chunks of 32 rows through registers into two LDS slots.
+// ------------------------------------------------------------------------------------- small layers
+// 128 (k) x 128 (n) tiles over a slice of the rows, eight waves in two groups: of each chunk of 64 rows group g takes the 32
+// from 32 g on, as 2 x 2 waves of 64 x 64, and group 1's sums go through LDS to group 0 at the end. Both operands go through
+// registers, where X is widened (and dY's rows may start anywhere), into two LDS slots; registers are loaded four chunks
+// ahead, since a lone chunk takes less than a load's time to come. One barrier a chunk. A split launch writes its sums as one
+// array a slice, which k_wgrad8_sum adds in slice order.
 template <int DT>
-__global__ void __launch_bounds__(256)
-k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xe, int64_t M,
-         int64_t N, int64_t K, const uint8_t* __restrict__ meta, float* __restrict__ gW) {
-  __shared__ __attribute__((aligned(16))) uint8_t lx[2][kWM * 256], ly[2][kWM * 256];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t Kp = q8_row(K), Ge = q8_exp_row(K), tk = Kp / 128;
-  const int64_t n0 = (int64_t)(blockIdx.x / tk) * 128, k0 = (int64_t)(blockIdx.x % tk) * 128;
+SLIM_DEV u32x2_t widen4(uint32_t c, float s);
+
+template <int DT>
+__global__ void __launch_bounds__(512, 2)
+k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xe,
+         int64_t M, int64_t N, int64_t K, const uint8_t* __restrict__ meta, float* __restrict__ gW, int64_t slice, int64_t slice_out) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int kRows = 2 * kWM, kAhead = 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kRows * 256];      // X slots, dY slots; at the end group 1's sums
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t Kp = q8_row(K), Ge = q8_exp_row(K);
+  const uint32_t tk = (uint32_t)(Kp / 128), nt = blockIdx.x / tk;
+  const int64_t n0 = (int64_t)__builtin_amdgcn_readfirstlane((int)nt) * 128;
+  const int64_t k0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x - nt * tk)) * 128;
+  const int64_t mb = blockIdx.y * slice, me = mb + slice < M ? mb + slice : M;
+  gW += blockIdx.y * slice_out;
   // staging: row tid / 8 of the chunk, columns 16 (tid % 8) .. + 15
   const int row = tid >> 3, col = 16 * (tid & 7);
-  const int64_t nleft = N - n0 - col;
-  u32x4_t y0, y1, c;
-  float sc;
-  auto load = [&](int64_t m) {
+  const int nleft = (int)(cols - n0 - col < 16 ? cols - n0 - col : 16);     // cols: readable columns of dY, at least 16
+  struct Stage {
+    u32x4_t y0, y1, c;
+    uint32_t e;
+  };
+  auto load = [&](Stage& S, int64_t m) {
     m += row;
-    y0 = y1 = c = u32x4_t{0, 0, 0, 0};
-    sc = 0.f;
-    if (m >= M) return;
-    const uint16_t* p = dY + m * lddy + n0 + col;
-    if (nleft >= 16) {
-      __builtin_memcpy(&y0, p, 16);
-      __builtin_memcpy(&y1, p + 8, 16);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        y0[e] = (2 * e < nleft ? (uint32_t)p[2 * e] : 0u) | (2 * e + 1 < nleft ? (uint32_t)p[2 * e + 1] << 16 : 0u);
-        y1[e] = (2 * e + 8 < nleft ? (uint32_t)p[2 * e + 8] : 0u) | (2 * e + 9 < nleft ? (uint32_t)p[2 * e + 9] << 16 : 0u);
+    S.y0 = S.y1 = S.c = u32x4_t{0, 0, 0, 0};
+    S.e = 0;
+    if (m >= me) return;
+    if (nleft > 0) {
+      // past N the next row's values do no harm (results there are not stored); the last row's last piece is taken 16 values
+      // from its end (N >= 16) and moved into place
+      const int past = m == M - 1 ? 16 - nleft : 0;
+      const uint16_t* p = dY + m * lddy + n0 + col - past;
+      __builtin_memcpy(&S.y0, p, 16);
+      __builtin_memcpy(&S.y1, p + 8, 16);
+      if (past) {
+        if (past & 8) S.y0 = S.y1;
+        if (past & 4) S.y0 = u32x4_t{S.y0[2], S.y0[3], S.y1[0], S.y1[1]}, S.y1 = u32x4_t{S.y1[2], S.y1[3], 0, 0};
+        if (past & 2) S.y0 = u32x4_t{S.y0[1], S.y0[2], S.y0[3], S.y1[0]}, S.y1 = u32x4_t{S.y1[1], S.y1[2], S.y1[3], 0};
+        if (past & 1) {
+          S.y0 = u32x4_t{S.y0[0] >> 16 | S.y0[1] << 16, S.y0[1] >> 16 | S.y0[2] << 16, S.y0[2] >> 16 | S.y0[3] << 16,
+                         S.y0[3] >> 16 | S.y1[0] << 16};
+          S.y1 = u32x4_t{S.y1[0] >> 16 | S.y1[1] << 16, S.y1[1] >> 16 | S.y1[2] << 16, S.y1[2] >> 16 | S.y1[3] << 16, S.y1[3] >> 16};
+        }
       }
     }
-    c = *reinterpret_cast<const u32x4_t*>(xc + m * Kp + k0 + col);
-    sc = q8_pow2(xe[m * Ge + k0 / 128]);
+    S.c = *reinterpret_cast<const u32x4_t*>(xc + m * Kp + k0 + col);
+    S.e = xe[m * Ge + k0 / 128];
   };
-  auto put = [&](int z) {
-    uint8_t* y = &ly[z][lds_at(row, col)];
-    *reinterpret_cast<u32x4_t*>(y) = y0;
-    *reinterpret_cast<u32x4_t*>(y + 16) = y1;
-    u32x4_t v[2];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float f[4];
-      q8_values4(c[e], sc, f);
-      v[e >> 1][2 * (e & 1)] = to_16<DT>(f[0]) | to_16<DT>(f[1]) << 16;
-      v[e >> 1][2 * (e & 1) + 1] = to_16<DT>(f[2]) | to_16<DT>(f[3]) << 16;
-    }
-    uint8_t* x = &lx[z][lds_at(row, col)];
-    *reinterpret_cast<u32x4_t*>(x) = v[0];
-    *reinterpret_cast<u32x4_t*>(x + 16) = v[1];
+  uint8_t* const lx = lds + lds_at(row, col);
+  auto put = [&](const Stage& S, int z) {
+    uint8_t* x = lx + z * (kRows * 256);
+    uint8_t* y = x + 2 * (kRows * 256);
+    *reinterpret_cast<u32x4_t*>(y) = S.y0;
+    *reinterpret_cast<u32x4_t*>(y + 16) = S.y1;
+    const float s = q8_pow2(S.e);
+    const u32x2_t a = widen4<DT>(S.c[0], s), b = widen4<DT>(S.c[1], s), c = widen4<DT>(S.c[2], s), d = widen4<DT>(S.c[3], s);
+    *reinterpret_cast<u32x4_t*>(x) = u32x4_t{a[0], a[1], b[0], b[1]};
+    *reinterpret_cast<u32x4_t*>(x + 16) = u32x4_t{c[0], c[1], d[0], d[1]};
   };
   f16_t acc[2][2];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[i >> 1][i & 1][e] = 0.f;
-  const int G = lane >> 4, q = lane & 15, wk = 64 * (wave & 1), wn = 64 * (wave >> 1);
-  const int rr = 8 * (G >> 1) + (q >> 2), cr = 16 * (G & 1) + 4 * (q & 3);
-  load(0);
-  put(0);
-  __syncthreads();
-  int z = 0;
-  for (int64_t m = 0; m < M; m += kWM, z ^= 1) {
-    const bool more = m + kWM < M;
-    if (more) load(m + kWM);
+  const int G = lane >> 4, q = lane & 15, grp = wave >> 2, wk = 64 * (wave & 1), wn = 64 * ((wave >> 1) & 1);
+  const int rr = 32 * grp + 8 * (G >> 1) + (q >> 2), cr = 16 * (G & 1) + 4 * (q & 3);
+  Stage S[kAhead];
+  auto sync = [] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+  };
+  // chunk at row m, in slot j % 2; after its barrier no wave reads the other slot, which the next chunk takes
+  auto chunk = [&](int64_t m, auto jc) {
+    constexpr int j = decltype(jc)::value, z = j & 1;
+    sync();
+    put(S[(j + 1) % kAhead], z ^ 1);
+    load(S[(j + 1) % kAhead], m + (kAhead + 1) * kRows);
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
       u32x2_t a[2][2], b[2][2];
 #pragma unroll
       for (int f = 0; f < 2; ++f)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          a[f][j] = read_tr(&lx[z][lds_at(16 * st + rr + 4 * j, wk + 32 * f + cr)]);
-          b[f][j] = read_tr(&ly[z][lds_at(16 * st + rr + 4 * j, wn + 32 * f + cr)]);
+        for (int i = 0; i < 2; ++i) {
+          a[f][i] = read_tr(lds + z * (kRows * 256) + lds_at(16 * st + rr + 4 * i, wk + 32 * f + cr));
+          b[f][i] = read_tr(lds + (2 + z) * (kRows * 256) + lds_at(16 * st + rr + 4 * i, wn + 32 * f + cr));
         }
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int y = 0; y < 2; ++y) acc[x][y] = mfma_acc<DT>(a[x][0], a[x][1], b[y][0], b[y][1], acc[x][y]);
     }
-    if (more) put(z ^ 1);
-    __syncthreads();
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load(S[i], mb + i * kRows);
+  put(S[0], 0);
+  load(S[0], mb + kAhead * kRows);
+  // chunks past the last are zeros
+  for (int64_t m = mb; m < me; m += kAhead * kRows) {
+    chunk(m, std::integral_constant<int, 0>{});
+    chunk(m + kRows, std::integral_constant<int, 1>{});
+    chunk(m + 2 * kRows, std::integral_constant<int, 2>{});
+    chunk(m + 3 * kRows, std::integral_constant<int, 3>{});
   }
+  __syncthreads();
+  f4_t* const hand = reinterpret_cast<f4_t*>(lds) + (wave & 3) * 1024;
+  if (grp == 1) {
 #pragma unroll
-  for (int y = 0; y < 2; ++y) {
-    const int64_t n = n0 + wn + 32 * y + (lane & 31);
-    if (n >= N) continue;
+    for (int i = 0; i < 16; ++i) {
+      const f16_t& c = acc[i >> 3][(i >> 2) & 1];
+      hand[i * 64 + lane] = f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+    }
+  }
+  __syncthreads();
+  if (grp == 1) return;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+  for (int i = 0; i < 16; ++i) {
+    const f16_t& c = acc[i >> 3][(i >> 2) & 1];
+    hand[i * 64 + lane] += f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+  }
+  // (in a loop: written out, the stores of partial groups are more instructions than the rest)
+#pragma unroll 1
+  for (int i = 0; i < 16; ++i) {
+    const int64_t n = n0 + wn + 32 * ((i >> 2) & 1) + (lane & 31), k = k0 + wk + 32 * (i >> 3) + 8 * (i & 3) + 4 * (lane >> 5);
+    if (n < N && k < K) store_grad4(gW, meta, n, k, K, hand[i * 64 + lane]);
+  }
+#endif
+}
+
+// The slices' sums, in slice order; four values a thread.
+__global__ void __launch_bounds__(256)
+k_wgrad8_sum(const float* __restrict__ part, int64_t slices, int64_t slice_out, int64_t count, float* __restrict__ gW) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= count) return;
+  f4_t v = *reinterpret_cast<const f4_t*>(part + i);       // arrays of whole 16 bytes
+  for (int64_t s = 1; s < slices; ++s) v += *reinterpret_cast<const f4_t*>(part + s * slice_out + i);
+  if (i + 4 <= count) {
+    *reinterpret_cast<f4_t*>(gW + i) = v;
+  } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t k = k0 + wk + 32 * x + 8 * i + 4 * (lane >> 5);
-        if (k < K)
-          store_grad4(gW, meta, n, k, K, f4_t{acc[x][y][4 * i], acc[x][y][4 * i + 1], acc[x][y][4 * i + 2], acc[x][y][4 * i + 3]});
-      }
+    for (int e = 0; e < 3; ++e)
+      if (i + e < count) gW[i + e] = v[e];
   }
 }
 
+// Rows of dY moved to 16-byte aligned ones (16 columns a thread), for the direct loads of the wide kernel.
+__global__ void __launch_bounds__(256)
+k_align_rows(const uint16_t* __restrict__ dY, int64_t lddy, uint32_t N, uint32_t pieces, uint32_t total, uint16_t* __restrict__ out) {
+  const uint32_t u = blockIdx.x * 256 + threadIdx.x;
+  if (u >= total) return;
+  const uint32_t row = u / pieces, col = (u - row * pieces) * 16;
+  const uint16_t* p = dY + (int64_t)row * lddy + col;
+  uint16_t* o = out + ((int64_t)row * pieces * 16 + col);
+  if (col + 16 <= N) {
+    u32x4_t a, b;
+    __builtin_memcpy(&a, p, 16);
+    __builtin_memcpy(&b, p + 8, 16);
+    *reinterpret_cast<u32x4_t*>(o) = a;
+    *reinterpret_cast<u32x4_t*>(o + 8) = b;
+  } else {
+    for (uint32_t e = 0; e < 16; ++e) o[e] = col + e < N ? p[e] : (uint16_t)0;
+  }
+}
+
+// ------------------------------------------------------------------------------------- large layers
+// c += a b, written out so that the sum stays in its accumulation registers (the compiler moves 256 of them around a loop
+// that has no others free). The operands were waited for; the sum was last written 15 products ago.
+template <int DT>
+SLIM_DEV void mfma_in_place(f16_t& c, u32x4_t a, u32x4_t b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (DT == 1) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  else asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+#endif
+}
+
+// Four codes times s as 16-bit values (two packed pairs); s is a power of two, of which the instruction takes the exponent.
+template <int DT>
+SLIM_DEV u32x2_t widen4(uint32_t c, float s) {
+  u32x2_t o;
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (DT == 1) {
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, true));
+  } else {
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, s, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, s, true));
+  }
+#endif
+  return o;
+}
+
+template <int N, int I = 0, class F>
+SLIM_DEV void each(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    each<N, I + 1>(f);
+  }
+}
+
+// byte offset of 16-bit column c of row r in 512-byte LDS rows, swizzled as lds_at
+SLIM_DEV uint32_t lds_at_wide(int r, int c) {
+  return (uint32_t)r * 512u + ((uint32_t)((c >> 4) ^ (2 * (r & 3))) << 5) + (uint32_t)((c & 15) * 2);
+}
+
+// 256 (k) x 256 (n) tiles, four waves of 128 x 128 (4 x 4 fragments, all accumulation registers of a SIMD's one wave): per
+// 16 rows of the reduction a CU reads 32 KiB of operands from LDS for 512 cycles of products, half of what LDS delivers.
+// A ring of four slots of 32 rows (16 KiB of dY, 16 KiB of widened X). dY, whose rows are 16-byte aligned, goes to LDS by
+// direct loads three chunks ahead; X's codes are loaded four chunks ahead, widened and written to LDS two chunks ahead. One barrier a chunk, between its two 16-row steps, whose operands are read while the
+// step before is multiplied. Columns past N and K read what lies there or zero; their results are not stored.
+template <int DT>
+__global__ void __launch_bounds__(256, 1)
+k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xe,
+              int64_t M, int64_t N, int64_t K, const uint8_t* __restrict__ meta, float* __restrict__ gW) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr uint32_t kSlot = kWM * 512, kY = 4 * kSlot;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[8 * kSlot];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wk = 128 * (wave & 1), wn = 128 * (wave >> 1);
+  const uint32_t Kp = (uint32_t)q8_row(K), Ge = (uint32_t)q8_exp_row(K);
+  // XCD-aware order (block b on XCD b % 8): bands of four n tiles, k tile by k tile
+  const uint32_t tn = (uint32_t)((N + 255) / 256), tk = (uint32_t)((K + 255) / 256), T = tn * tk, Q = (T + 7) / 8;
+  const uint32_t pos = (blockIdx.x % 8) * Q + blockIdx.x / 8;
+  if (pos >= T) return;
+  const uint32_t band = pos / (4 * tk), q0 = pos - band * 4 * tk, width = tn - band * 4 < 4 ? tn - band * 4 : 4, kt = q0 / width;
+  const int64_t n0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(band * 4 + q0 - kt * width)) * 256;
+  const int64_t k0 = (int64_t)__builtin_amdgcn_readfirstlane((int)kt) * 256;
+  const int nch = (int)((M + kWM - 1) / kWM);
+
+  // direct loads of dY: four pieces of 1 KiB (two rows) a wave; lane L writes LDS bytes 16 L of its piece, row L / 32,
+  // physical slot L % 32, which holds logical slot (L % 32) ^ 4 (row % 4)
+  uint32_t yo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 8 * wave + 2 * i + (lane >> 5), ls = (lane & 31) ^ (4 * (row & 3));
+    yo[i] = ((uint32_t)row * (uint32_t)lddy + (uint32_t)(n0 + 8 * ls)) * 2u;
+  }
+  // Loads of chunk c: resources start at the group of four chunks being worked on, so that 32-bit offsets do for operands of
+  // any size, and end with the operand, so that rows past M read as zero. A chunk past the last gets an offset past every
+  // resource (the last group's are below 2 GiB) and reads as zero too, without a memory access; its uniform offset is 0,
+  // since the bounds check takes the uniform offset off the resource's size. M >= 1.
+  const uint32_t ystep = (uint32_t)(kWM * 2) * (uint32_t)lddy, xstep = kWM * Kp, estep = kWM * Ge;
+  rsrc_t ry, rx, re;
+  int c0 = 0;
+  auto rebase = [&](int c) {
+    const int64_t m = (int64_t)c * kWM, left = M - m;
+    c0 = c;
+    // whole 32-bit words, by which the bounds are checked: an odd N ends inside one (lddy is even)
+    ry = make_rsrc(dY + m * lddy, ((left - 1) * lddy + N + (N & 1)) * 2);
+    rx = make_rsrc(xc + m * Kp, left * Kp);
+    re = make_rsrc(xe + m * Ge, left * Ge);
+  };
+  auto in_group = [&](int c) { return c < nch ? (uint32_t)(c - c0) : 0u; };
+  auto or_past = [&](int c, uint32_t o) { return c < nch ? o : 0x80000000u; };
+  auto issue_y = [&](int c, auto zc, auto ic) {
+    constexpr int i = decltype(ic)::value;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, (lds_ptr_t)&lds[kY + decltype(zc)::value * kSlot + (uint32_t)(4 * wave + i) * 1024u], 16,
+                                             or_past(c, yo[i]), in_group(c) * ystep, 0, 0);
+  };
+  // X through registers: rows tid / 16 and 16 more, 16 columns from 16 (tid % 16) on
+  const int sr = tid >> 4, scol = 16 * (tid & 15);
+  const uint32_t kc = (uint32_t)(k0 + scol < Kp ? k0 + scol : Kp - 16);
+  uint32_t xo[2], eo[2], xw[2][2];
+  const uint32_t lb = (uint32_t)(uintptr_t)(lds_ptr_t)&lds[0];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    xo[j] = (uint32_t)(sr + 16 * j) * Kp + kc;
+    eo[j] = (uint32_t)(sr + 16 * j) * Ge + kc / 128;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) xw[j][h] = lb + lds_at_wide(sr + 16 * j, scol) + 16u * h;
+  }
+  struct Stage {
+    u32x4_t x[2];
+    uint32_t e[2];
+  };
+  auto load_x = [&](Stage& S, int c, auto jc) {
+    constexpr int j = decltype(jc)::value;
+    const uint32_t g = in_group(c);
+    S.x[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, or_past(c, xo[j]), g * xstep, 0);
+    S.e[j] = __builtin_amdgcn_raw_buffer_load_b8(re, or_past(c, eo[j]), g * estep, 0);
+  };
+  // piece i (0 .. 3): eight codes widened and written
+  auto put_x = [&](const Stage& S, auto zc, auto ic) {
+    constexpr uint32_t off = decltype(zc)::value * kSlot;
+    constexpr int j = decltype(ic)::value >> 1, h = decltype(ic)::value & 1;
+    const float s = q8_pow2(S.e[j]);
+    const u32x2_t a = widen4<DT>(S.x[j][2 * h], s), b = widen4<DT>(S.x[j][2 * h + 1], s);
+    const u32x4_t v = {a[0], a[1], b[0], b[1]};
+    const uint32_t at = xw[j][h];
+    asm volatile("ds_write_b128 %0, %1 offset:%2" :: "v"(at), "v"(v), "i"(off) : "memory");
+  };
+
+  f16_t acc[4][4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.f;
+  // per-lane addresses of the transposed reads in slot 0, step 0 (lane mapping as in k_wgrad8)
+  const int Gl = lane >> 4, ql = lane & 15, rr = 8 * (Gl >> 1) + (ql >> 2), cr = 16 * (Gl & 1) + 4 * (ql & 3);
+  uint32_t ax[4][2], by[4][2];
+#pragma unroll
+  for (int f = 0; f < 4; ++f)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      ax[f][j] = lb + lds_at_wide(rr + 4 * j, wk + 32 * f + cr);
+      by[f][j] = lb + kY + lds_at_wide(rr + 4 * j, wn + 32 * f + cr);
+    }
+  struct Frags {
+    u32x2_t a[4][2], b[4][2];
+  };
+  auto rd = [](u32x2_t& v, uint32_t at, auto oc) {
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(at), "i"(decltype(oc)::value));
+  };
+  // read i (0 .. 15) of a step: fragments of dY and X in the order the products need them
+  auto read_i = [&](Frags& F, auto ic, auto oc) {
+    constexpr int i = decltype(ic)::value, f = i >> 2, j = i & 1;
+    if constexpr (i & 2) rd(F.a[f][j], ax[f][j], oc);
+    else rd(F.b[f][j], by[f][j], oc);
+  };
+  auto landed = [](Frags& F) {
+    asm volatile("s_waitcnt lgkmcnt(0)"
+                 : "+v"(F.a[0][0]), "+v"(F.a[0][1]), "+v"(F.a[1][0]), "+v"(F.a[1][1]), "+v"(F.a[2][0]), "+v"(F.a[2][1]),
+                   "+v"(F.a[3][0]), "+v"(F.a[3][1]), "+v"(F.b[0][0]), "+v"(F.b[0][1]), "+v"(F.b[1][0]), "+v"(F.b[1][1]),
+                   "+v"(F.b[2][0]), "+v"(F.b[2][1]), "+v"(F.b[3][0]), "+v"(F.b[3][1]));
+  };
+  // The 16 products of the step in F; before each of the first eight two reads of the next step (at offset oc) into Nx, and
+  // before product i the work of extra(i): a product takes 32 cycles, in which a wave issues about seven more instructions,
+  // so the loads, widenings and writes of the chunks to come are spread over the products.
+  auto step = [&](const Frags& F, Frags& Nx, auto oc, auto&& extra) {
+    each<16>([&](auto ic) {
+      constexpr int i = decltype(ic)::value, x = i >> 2, y = i & 3;
+      if constexpr (i < 8) {
+        read_i(Nx, std::integral_constant<int, 2 * i>{}, oc);
+        read_i(Nx, std::integral_constant<int, 2 * i + 1>{}, oc);
+      }
+      extra(ic);
+      __builtin_amdgcn_sched_barrier(0);
+      const u32x4_t av = {F.a[x][0][0], F.a[x][0][1], F.a[x][1][0], F.a[x][1][1]};
+      const u32x4_t bv = {F.b[y][0][0], F.b[y][0][1], F.b[y][1][0], F.b[y][1][1]};
+      mfma_in_place<DT>(acc[x][y], av, bv);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  using I3 = std::integral_constant<int, 3>;
+  Frags A, B;
+  Stage S[2];
+  // Chunk c in slot z = c % 4. At its barrier dY of chunk c + 1 has landed for this wave once only the loads issued after it
+  // are outstanding (X of chunk c + 2, dY of c + 2, X of c + 3: 12), and this wave's part of X, written a chunk ago, is in
+  // LDS; after it no wave reads chunk c - 1, whose slot chunk c + 3 takes.
+  auto chunk = [&](int c, auto zc) {
+    constexpr int z = decltype(zc)::value;
+    step(A, B, std::integral_constant<uint32_t, z * kSlot + 16 * 512>{}, [&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      if constexpr (i >= 8 && i % 2 == 0) put_x(S[z & 1], std::integral_constant<int, (z + 2) % 4>{}, std::integral_constant<int, (i - 8) / 2>{});
+    });
+    landed(B);
+    __builtin_amdgcn_s_waitcnt(vmcnt_wait(12));
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    step(B, A, std::integral_constant<uint32_t, ((z + 1) % 4) * kSlot>{}, [&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      if constexpr (i >= 8 && i < 12) issue_y(c + 3, std::integral_constant<int, (z + 3) % 4>{}, std::integral_constant<int, i - 8>{});
+      if constexpr (i == 13) load_x(S[z & 1], c + 4, I0{});
+      if constexpr (i == 15) load_x(S[z & 1], c + 4, I1{});
+    });
+    landed(A);
+  };
+  rebase(0);
+  each<4>([&](auto ic) { issue_y(0, I0{}, ic); });
+  each<4>([&](auto ic) { issue_y(1, I1{}, ic); });
+  each<4>([&](auto ic) { issue_y(2, I2{}, ic); });
+  each<2>([&](auto jc) { load_x(S[0], 0, jc); });
+  each<2>([&](auto jc) { load_x(S[1], 1, jc); });
+  each<4>([&](auto ic) { put_x(S[0], I0{}, ic); });
+  each<4>([&](auto ic) { put_x(S[1], I1{}, ic); });
+  each<2>([&](auto jc) { load_x(S[0], 2, jc); });
+  each<2>([&](auto jc) { load_x(S[1], 3, jc); });
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(vmcnt_wait(0));
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  each<16>([&](auto ic) { read_i(A, ic, std::integral_constant<uint32_t, 0>{}); });
+  landed(A);
+  int c = 0;
+  do {                  // at least once: no way around the loop, on which the sums would be moved
+    if (c) rebase(c);
+    // chunks past the last are zeros: with branches here the sums would be moved about
+    chunk(c, I0{});
+    chunk(c + 1, I1{});
+    chunk(c + 2, I2{});
+    chunk(c + 3, I3{});
+    c += 4;
+  } while (c < nch);
+  // no direct load may still be writing LDS; the last products are written before their sums are read
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int x = 0; x < 4; ++x) asm volatile("" : "+a"(acc[x][0]), "+a"(acc[x][1]), "+a"(acc[x][2]), "+a"(acc[x][3]));   // not before
+  __builtin_amdgcn_sched_barrier(0);
+  // the sums leave through LDS, half of them at a time, in a loop (see k_wgrad8)
+  f4_t* const mine = reinterpret_cast<f4_t*>(lds) + wave * 2048;
+#pragma unroll
+  for (int y2 = 0; y2 < 2; ++y2) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const f16_t& c = acc[i >> 3][2 * y2 + ((i >> 2) & 1)];
+      mine[i * 64 + lane] = f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+    }
+#pragma unroll 2
+    for (int i = 0; i < 32; ++i) {
+      const int64_t n = n0 + wn + 32 * (2 * y2 + ((i >> 2) & 1)) + (lane & 31), k = k0 + wk + 32 * (i >> 3) + 8 * (i & 3) + 4 * (lane >> 5);
+      if (n < N && k < K) store_grad4(gW, meta, n, k, K, mine[i * 64 + lane]);
+    }
+  }
+#endif
+}
+
+// How a gradient is computed: 256 x 256 tiles (dY's rows aligned, if need be in a copy of them), or 128 x 128 tiles over
+// `slices` slices of the rows.
+struct GradPlan {
+  bool wide, copy;
+  int64_t slices, slice, slice_out;
+  size_t off_part, bytes;   // workspace: the copied rows, the slices' sums from off_part on
+};
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
+
+GradPlan grad_plan(int64_t M, int64_t N, int64_t K, bool masked, bool aligned) {
+  GradPlan p{};
+  p.wide = M > 0 && cdiv(N, 256) * cdiv(K, 256) >= 128 && N < (int64_t(1) << 22) - 16;
+  p.copy = M > 0 && (p.wide ? !aligned : N < 16);        // (the other kernel takes pieces of 16)
+  p.slices = 1;
+  p.slice = M;
+  if (p.copy) p.bytes = round256((size_t)M * (size_t)(cdiv(N, 16) * 16) * 2);
+  if (p.wide) return p;
+  const int64_t tiles = cdiv(N, 128) * cdiv(K, 128);
+  // slices of at least 512 rows, so that their sums cost less than they save (999 x 2051 x 768: one slice 18.5 us, three
+  // 19.9; 8192 x 128 x 128: sixteen 16.6, 32 19.2), up to a block a CU
+  p.slices = std::max<int64_t>(1, std::min(256 / tiles, M / 512));
+  p.slice = cdiv(cdiv(M, p.slices), 2 * kWM) * 2 * kWM;
+  p.slices = std::max<int64_t>(1, cdiv(M, std::max<int64_t>(p.slice, 1)));
+  p.slice_out = cdiv(N * (masked ? K / 2 : K), 64) * 64;
+  p.off_part = p.bytes;
+  if (p.slices > 1) p.bytes += (size_t)p.slices * (size_t)p.slice_out * 4;
+  return p;
+}
+
+int check_grad(int64_t M, int64_t N, int64_t K, bool masked) {
+  if (M < 0 || N < 1 || K < 1 || N > kMaxRow8 || K > kMaxRow8 || (masked && K % 16)) return SLIM_ESHAPE;
+  if (cdiv(N, 128) * cdiv(K, 128) > 0x7FFFFFFF || M >= (int64_t(1) << 31) || M > (int64_t(1) << 36) / cdiv(N, 16))
+    return SLIM_EUNSUPPORTED;
+  return SLIM_OK;
+}
+
+template <int DT>
+int grad(const GradPlan& p, const uint16_t* dY, int64_t lddy, const uint8_t* xc, const uint8_t* xe, int64_t M, int64_t N, int64_t K,
+         const uint8_t* meta, float* gW, void* ws, hipStream_t s) {
+  int64_t cols = N;         // columns of dY's rows that may be read
+  if (p.copy) {
+    const int64_t pieces = cdiv(N, 16);
+    uint16_t* rows = reinterpret_cast<uint16_t*>(ws);
+    SlimKernelTimer timer("align_rows", s);
+    SLIM_LAUNCH(timer, k_align_rows, dim3((unsigned)cdiv(M * pieces, 256)), dim3(256), s, dY, lddy, (uint32_t)N, (uint32_t)pieces,
+                (uint32_t)(M * pieces), rows);
+    dY = rows;
+    cols = lddy = pieces * 16;
+  }
+  if (p.wide) {
+    SlimKernelTimer timer("grad_w8_wide", s);
+    SLIM_LAUNCH(timer, (k_wgrad8_wide<DT>), dim3((unsigned)(8 * cdiv(cdiv(N, 256) * cdiv(K, 256), 8))), dim3(256), s, dY, lddy, xc, xe,
+                M, N, K, meta, gW);
+    return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
+  }
+  const dim3 grid((unsigned)(cdiv(N, 128) * cdiv(K, 128)), (unsigned)p.slices);
+  float* out = p.slices > 1 ? reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + p.off_part) : gW;
+  {
+    SlimKernelTimer timer("grad_w8", s);
+    SLIM_LAUNCH(timer, (k_wgrad8<DT>), grid, dim3(512), s, dY, lddy, cols, xc, xe, M, N, K, meta, out, p.slice, p.slice_out);
+  }
+  if (p.slices > 1) {
+    const int64_t count = N * (meta ? K / 2 : K);
+    SlimKernelTimer timer("grad_w8_sum", s);
+    SLIM_LAUNCH(timer, k_wgrad8_sum, dim3((unsigned)cdiv(count, 1024)), dim3(256), s, out, p.slices, p.slice_out, count, gW);
+  }
+  return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
+}
+
+// Rows that the wide kernel's direct loads take as they are.
+bool aligned_rows(const void* dY, int64_t lddy) { return slim_aligned16(dY) && lddy % 8 == 0 && lddy < (int64_t(1) << 22); }
+
 }  // namespace
 
+extern "C" int slim_grad_w8_workspace(int64_t M, int64_t N, int64_t K, int masked, int aligned, size_t* bytes) {
+  if (!bytes) return SLIM_EINVAL;
+  const int rc = check_grad(M, N, K, masked != 0);
+  if (rc != SLIM_OK) return rc;
+  *bytes = grad_plan(M, N, K, masked != 0, aligned != 0).bytes;
+  return SLIM_OK;
+}
+
 extern "C" int slim_grad_w8(const void* dY, int dtype, int64_t lddy, const uint8_t* xcodes, const uint8_t* xexps, int64_t M,
-                            int64_t N, int64_t K, const uint8_t* meta, float* gW, void* stream) {
+                            int64_t N, int64_t K, const uint8_t* meta, float* gW, void* ws, size_t ws_bytes, void* stream) {
   if (dtype != SLIM_F16 && dtype != SLIM_BF16) return SLIM_EDTYPE;
-  if (M < 0 || N < 1 || K < 1 || N > kMaxRow8 || K > kMaxRow8 || lddy < N || (meta && K % 16)) return SLIM_ESHAPE;
+  const int rc = check_grad(M, N, K, meta != nullptr);
+  if (rc != SLIM_OK) return rc;
+  if (lddy < N) return SLIM_ESHAPE;
   if (!gW || (M > 0 && (!dY || !xcodes || !xexps))) return SLIM_EINVAL;
   if (!slim_aligned_to(dY, 2) || !slim_aligned16(xcodes) || !slim_aligned16(xexps) || !slim_aligned16(meta) ||
       !slim_aligned16(gW))
     return SLIM_EALIGN;
-  const int64_t tiles = ((N + 127) / 128) * ((K + 127) / 128);
-  if (tiles > 0x7FFFFFFF) return SLIM_EUNSUPPORTED;
-  hipStream_t s = (hipStream_t)stream;
-  SlimKernelTimer timer("grad_w8", s);
-  if (dtype == SLIM_F16)
-    SLIM_LAUNCH(timer, k_wgrad8<0>, dim3((unsigned)tiles), dim3(256), s, reinterpret_cast<const uint16_t*>(dY), lddy, xcodes,
-                xexps, M, N, K, meta, gW);
-  else
-    SLIM_LAUNCH(timer, k_wgrad8<1>, dim3((unsigned)tiles), dim3(256), s, reinterpret_cast<const uint16_t*>(dY), lddy, xcodes,
-                xexps, M, N, K, meta, gW);
-  return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
+  const GradPlan p = grad_plan(M, N, K, meta != nullptr, aligned_rows(dY, lddy));
+  if (p.bytes && (!ws || ws_bytes < p.bytes)) return SLIM_EWORKSPACE;
+  if (p.bytes && !slim_aligned16(ws)) return SLIM_EALIGN;
+  const uint16_t* y = reinterpret_cast<const uint16_t*>(dY);
+  return dtype == SLIM_F16 ? grad<0>(p, y, lddy, xcodes, xexps, M, N, K, meta, gW, ws, (hipStream_t)stream)
+                           : grad<1>(p, y, lddy, xcodes, xexps, M, N, K, meta, gW, ws, (hipStream_t)stream);
 }

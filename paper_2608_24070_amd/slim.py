@@ -67,7 +67,10 @@ _SIGS = {
     "slim_linear8_workspace": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
     "slim_linear8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
                                     ctypes.c_int, _c_i64, _c_p, ctypes.c_size_t, _c_p]),
-    "slim_grad_w8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p]),
+    "slim_grad_w8_workspace": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, ctypes.c_int, ctypes.c_int,
+                                              ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_grad_w8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
+                                    ctypes.c_size_t, _c_p]),
     "slim_norm": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_p, _c_p, ctypes.c_int, ctypes.c_int,
                                  ctypes.c_float, _c_p, ctypes.c_int, _c_i64, _c_p, _c_p, _c_p, _c_p]),
     "slim_norm_bwd_workspace": (ctypes.c_int, [_c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
@@ -267,8 +270,14 @@ def slim_linear8(X, xdtype, xexps, M, N, K, ldx, codes, exps, Y, ydtype, ldy, ws
     return lib().slim_linear8(X, xdtype, xexps, M, N, K, ldx, codes, exps, Y, ydtype, ldy, ws, ws_bytes, stream)
 
 
-def slim_grad_w8(dY, dtype, lddy, xcodes, xexps, M, N, K, meta, gW, stream) -> int:
-    return lib().slim_grad_w8(dY, dtype, lddy, xcodes, xexps, M, N, K, meta, gW, stream)
+def slim_grad_w8_workspace(M, N, K, masked, aligned) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().slim_grad_w8_workspace(M, N, K, masked, aligned, ctypes.byref(out)), "slim_grad_w8_workspace")
+    return out.value
+
+
+def slim_grad_w8(dY, dtype, lddy, xcodes, xexps, M, N, K, meta, gW, ws, ws_bytes, stream) -> int:
+    return lib().slim_grad_w8(dY, dtype, lddy, xcodes, xexps, M, N, K, meta, gW, ws, ws_bytes, stream)
 
 
 def slim_norm(X, dtype, M, K, ldx, gamma, beta, pdtype, rms, eps, Y, ydtype, ldy, yexps, mean, rstd, stream) -> int:
@@ -881,7 +890,7 @@ def bwd_dx8(dY, p: dict, dtype=None, out=None, ws=None, stream=None):
     return _product8(dY, p["codesT"], p["expsT"], p["K"], p["N"], dtype, out, ws, stream, "slim_linear8")
 
 
-def grad_w8(dY, q: dict, p: dict | None = None, out=None, stream=None):
+def grad_w8(dY, q: dict, p: dict | None = None, out=None, ws=None, stream=None):
     """slim_grad_w8: dY^T X for dY [M, N] (fp16, bf16) and X [M, K] in 8 bits: fp32 [N, K], or with a value pack `p`
     (pack16) fp32 [N, K/2] at the positions it keeps."""
     torch = _torch()
@@ -899,8 +908,13 @@ def grad_w8(dY, q: dict, p: dict | None = None, out=None, stream=None):
     out = _out(out, (N, K if p is None else K // 2), torch.float32, dY)
     _on_gpu(out)
     _one_device(dY, xc, xe, meta, out)
-    _check(slim_grad_w8(dY.data_ptr(), _dtype_code(dY), ldy, xc.data_ptr(), xe.data_ptr(), M, N, K, _ptr(meta),
-                        out.data_ptr(), _stream(stream)), "slim_grad_w8")
+    y = dY.data_ptr()
+    aligned = 1 if y % 16 == 0 and ldy % 8 == 0 and ldy < 1 << 22 else 0
+    need = slim_grad_w8_workspace(M, N, K, 0 if p is None else 1, aligned)
+    if ws is None:
+        ws = _workspace8(need, dY.device, stream)
+    _check(slim_grad_w8(y, _dtype_code(dY), ldy, xc.data_ptr(), xe.data_ptr(), M, N, K, _ptr(meta), out.data_ptr(), _ptr(ws),
+                        0 if ws is None else ws.numel(), _stream(stream)), "slim_grad_w8")
     return out
 
 

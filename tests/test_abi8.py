@@ -64,10 +64,22 @@ def test_linear8(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(dY=None), INV), (dict(xc=None), INV), (dict(xe=None), INV), (dict(gW=None), INV), (dict(dt=F32), DTYPE), (dict(dt=Q8), DTYPE),
     (dict(M=-1), SHAPE), (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(lddy=9), SHAPE), (dict(meta=A, K=40), SHAPE), (dict(N=WIDE, lddy=WIDE), SHAPE),
-    (dict(dY=ODD), ALIGN), (dict(xc=MIS), ALIGN), (dict(xe=MIS), ALIGN), (dict(gW=MIS), ALIGN), (dict(meta=MIS, K=32), ALIGN)])
+    (dict(dY=ODD), ALIGN), (dict(xc=MIS), ALIGN), (dict(xe=MIS), ALIGN), (dict(gW=MIS), ALIGN), (dict(meta=MIS, K=32), ALIGN), (dict(ws=None), WS), (dict(short=1), WS), (dict(ws=MIS), ALIGN), (dict(M=1 << 31), UNSUP)])
 def test_grad_w8(kw, status):
-    a = dict(dict(dY=A, dt=BF16, lddy=10, xc=A, xe=A, M=5, N=10, K=36, meta=None, gW=A), **kw)
-    assert slim.slim_grad_w8(a["dY"], a["dt"], a["lddy"], a["xc"], a["xe"], a["M"], a["N"], a["K"], a["meta"], a["gW"], None) == status
+    a = dict(dict(dY=A, dt=BF16, lddy=10, xc=A, xe=A, M=5000, N=10, K=36, meta=None, gW=A, ws=A, short=0), **kw)
+    try:
+        need = slim.slim_grad_w8_workspace(a["M"], a["N"], a["K"], int(a["meta"] is not None), 0)
+    except slim.SlimError as e:
+        assert e.status == status
+        need = 1 << 40
+    assert slim.slim_grad_w8(a["dY"], a["dt"], a["lddy"], a["xc"], a["xe"], a["M"], a["N"], a["K"], a["meta"], a["gW"], a["ws"],
+                             need - a["short"], None) == status
+
+
+def test_grad_w8_workspace_is_for_odd_rows_and_short_layers():
+    assert slim.slim_grad_w8_workspace(8192, 28672, 8192, 1, 1) == 0
+    assert slim.slim_grad_w8_workspace(100, 8193, 8192, 0, 0) == -(-100 * 8208 * 2 // 256) * 256
+    assert slim.slim_grad_w8_workspace(8192, 128, 128, 0, 1) > 0 and slim.slim_grad_w8_workspace(0, 128, 128, 0, 0) == 0
 
 
 @pytest.mark.parametrize("kw,status", [

@@ -58,6 +58,55 @@ def test_kept_positions(m, n, k, dtype):
     check(slim.grad_w8(dy.cuda(), q, p), dy.double().numpy(), xv, pick)
 
 
+# layers of 128 and more tiles of 256 x 256; odd widths end inside a word, a tile and a group
+WIDE = [(1, 8200, 1024), (70, 8191, 1021), (33, 8250, 1000), (129, 2100, 4000)]
+
+
+@pytest.mark.parametrize("m,n,k", WIDE)
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_large_layers(m, n, k, dtype):
+    print(f"grad_w8 wide m={m} n={n} k={k} {dtype}", flush=True)
+    dy, x = inputs(m, n, k, dtype, seed=8)
+    q = slim.quant8(x.cuda())
+    xv = act8.values_rows(*act8.quant_rows(x.double().numpy()), k)
+    got = slim.grad_w8(dy.cuda(), q)
+    check(got, dy.double().numpy(), xv)
+    # rows that are aligned, as part of wider ones that NaN fills, and rows that start anywhere: the same bits
+    for start, width in ((8, n + 24 - n % 8), (3, n + 7)):
+        buf = torch.full((m, width), float("nan"), dtype=DT[dtype], device="cuda")
+        buf[:, start:start + n] = dy.cuda()
+        assert torch.equal(slim.grad_w8(buf[:, start:start + n], q), got), start
+
+
+@pytest.mark.parametrize("m,n,k", [(45, 16387, 512), (100, 4096, 2064)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_large_layers_kept_positions(m, n, k, dtype):
+    print(f"grad_w8 wide kept m={m} n={n} k={k} {dtype}", flush=True)
+    dy, x = inputs(m, n, k, dtype, seed=9)
+    p, pick = kept(n, k)
+    xv = act8.values_rows(*act8.quant_rows(x.double().numpy()), k)
+    check(slim.grad_w8(dy.cuda(), slim.quant8(x.cuda()), p), dy.double().numpy(), xv, pick)
+
+
+def test_large_layer_of_no_rows():
+    q = slim.quant8(torch.empty((0, 1024), dtype=torch.bfloat16, device="cuda"))
+    g = slim.grad_w8(torch.empty((0, 8200), dtype=torch.bfloat16, device="cuda"), q)
+    assert g.shape == (8200, 1024) and bool((g == 0).all())
+
+
+@pytest.mark.parametrize("n", [1, 7, 15, 16, 17, 130])
+def test_narrow_layers_over_many_rows(n):
+    # slices of the rows, joined; rows shorter than a load
+    dy, x = inputs(2600, n, 140, "bf16", seed=10)
+    q = slim.quant8(x.cuda())
+    xv = act8.values_rows(*act8.quant_rows(x.double().numpy()), 140)
+    buf = torch.full((2600, n + 5), float("nan"), dtype=torch.bfloat16, device="cuda")
+    buf[:, 3:3 + n] = dy.cuda()
+    got = slim.grad_w8(dy.cuda(), q)
+    check(got, dy.double().numpy(), xv)
+    assert torch.equal(slim.grad_w8(buf[:, 3:3 + n], q), got)
+
+
 @pytest.mark.parametrize("m,n,k", [(50, 130, 300), (700, 300, 260), (2000, 520, 640)])
 def test_small_integers_are_exact(m, n, k):
     rng = synth.stream(2, f"grad_w8/int/{m}x{n}x{k}")
