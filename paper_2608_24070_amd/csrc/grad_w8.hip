@@ -40,11 +40,11 @@ SLIM_DEV uint32_t lds_at(int r, int c) {
   return (uint32_t)r * 256u + ((uint32_t)((c >> 4) ^ (2 * (r & 3))) << 5) + (uint32_t)((c & 15) * 2);
 }
 
-// Four consecutive positions k .. k + 3 of row n of the gradient: all of them, or the two that the pattern keeps.
-SLIM_DEV void store_grad4(float* gW, const uint8_t* meta, int64_t n, int64_t k, int64_t K, f4_t v) {
-  if (meta) {
-    const uint32_t nib = (uint32_t)(meta[n * (K / 8) + k / 8] >> (k & 4)) & 0xFu;
-    const uint32_t i0 = nib & 3u, i1 = nib >> 2;
+// Four consecutive positions k .. k + 3 of row n of the gradient: all of them, or the two that the pattern's byte for
+// positions 8 (k / 8) .. keeps.
+SLIM_DEV void store_grad4(float* gW, bool masked, uint32_t byte, int64_t n, int64_t k, int64_t K, f4_t v) {
+  if (masked) {
+    const uint32_t nib = (byte >> (k & 4)) & 0xFu, i0 = nib & 3u, i1 = nib >> 2;
     const f2_t o = {i0 == 0 ? v[0] : i0 == 1 ? v[1] : i0 == 2 ? v[2] : v[3], i1 == 0 ? v[0] : i1 == 1 ? v[1] : i1 == 2 ? v[2] : v[3]};
     *reinterpret_cast<f2_t*>(gW + n * (K / 2) + k / 2) = o;
   } else if (k + 4 <= K) {
@@ -56,21 +56,41 @@ SLIM_DEV void store_grad4(float* gW, const uint8_t* meta, int64_t n, int64_t k, 
   }
 }
 
+// COUNT rows n, n + step, ... of a tile kept in LDS as [n][k] (32 16-byte slots a row, XOR-swizzled by the row), positions
+// k .. k + 3 of each by this lane: the pattern's bytes first, so that their loads are in flight together.
+template <int COUNT>
+SLIM_DEV void store_rows(float* gW, const uint8_t* meta, const f4_t* tile, int row, int step, int64_t n0, int64_t N, int slot, int64_t k,
+                         int64_t K) {
+  if (k >= K) return;
+  uint32_t byte[COUNT];
+  if (meta)
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j) {
+      const int64_t n = n0 + row + j * step;
+      byte[j] = meta[(n < N ? n : N - 1) * (K / 8) + k / 8];
+    }
+#pragma unroll
+  for (int j = 0; j < COUNT; ++j) {
+    const int i = row + j * step;
+    if (n0 + i < N) store_grad4(gW, meta != nullptr, byte[j], n0 + i, k, K, tile[i * 32 + (slot ^ (i & 31))]);
+  }
+}
+
 // ------------------------------------------------------------------------------------- small layers
 // 128 (k) x 128 (n) tiles over a slice of the rows, eight waves in two groups: of each chunk of 64 rows group g takes the 32
 // from 32 g on, as 2 x 2 waves of 64 x 64, and group 1's sums go through LDS to group 0 at the end. Both operands go through
-// registers, where X is widened (and dY's rows may start anywhere), into two LDS slots; registers are loaded four chunks
-// ahead, since a lone chunk takes less than a load's time to come. One barrier a chunk. A split launch writes its sums as one
+// registers, where X is widened (and dY's rows may start anywhere), into two LDS slots; registers are loaded three chunks
+// ahead, since a lone chunk takes less than a load's time to come (more would cost the second block on a CU). One barrier a chunk. A split launch writes its sums as one
 // array a slice, which k_wgrad8_sum adds in slice order.
 template <int DT>
 SLIM_DEV u32x2_t widen4(uint32_t c, float s);
 
 template <int DT>
-__global__ void __launch_bounds__(512, 2)
+__global__ void __launch_bounds__(512, 4)
 k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xe,
          int64_t M, int64_t N, int64_t K, const uint8_t* __restrict__ meta, float* __restrict__ gW, int64_t slice, int64_t slice_out) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int kRows = 2 * kWM, kAhead = 4;
+  constexpr int kRows = 2 * kWM, kAhead = 2;
   __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kRows * 256];      // X slots, dY slots; at the end group 1's sums
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t Kp = q8_row(K), Ge = q8_exp_row(K);
@@ -86,16 +106,22 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     u32x4_t y0, y1, c;
     uint32_t e;
   };
-  auto load = [&](Stage& S, int64_t m) {
-    m += row;
-    S.y0 = S.y1 = S.c = u32x4_t{0, 0, 0, 0};
-    S.e = 0;
-    if (m >= me) return;
-    if (nleft > 0) {
+  // the next chunk's row of this thread: rows are loaded in order
+  int left = (int)(me - mb) - row, to_last = (int)(M - 1 - mb) - row;
+  const uint16_t* py = dY + (mb + row) * lddy + n0 + col;
+  // X by resources that move on with the chunk and end with the slice: rows past it read as zero
+  const uint32_t xo = (uint32_t)row * (uint32_t)Kp + (uint32_t)(k0 + col), eo = (uint32_t)row * (uint32_t)Ge + (uint32_t)(k0 / 128);
+  int64_t xm = mb;
+  auto load = [&](Stage& S) {
+    S.y0 = S.y1 = u32x4_t{0, 0, 0, 0};
+    S.c = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(xc + xm * Kp, (me - xm) * Kp), xo, 0, 0);
+    S.e = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(xe + xm * Ge, (me - xm) * Ge), eo, 0, 0);
+    xm += kRows;
+    if (left > 0 && nleft > 0) {
       // past N the next row's values do no harm (results there are not stored); the last row's last piece is taken 16 values
       // from its end (N >= 16) and moved into place
-      const int past = m == M - 1 ? 16 - nleft : 0;
-      const uint16_t* p = dY + m * lddy + n0 + col - past;
+      const int past = to_last == 0 ? 16 - nleft : 0;
+      const uint16_t* p = py - past;
       __builtin_memcpy(&S.y0, p, 16);
       __builtin_memcpy(&S.y1, p + 8, 16);
       if (past) {
@@ -109,8 +135,10 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
         }
       }
     }
-    S.c = *reinterpret_cast<const u32x4_t*>(xc + m * Kp + k0 + col);
-    S.e = xe[m * Ge + k0 / 128];
+    left -= kRows;
+    to_last -= kRows;
+    py += kRows * lddy;
+    asm volatile("" : "+v"(py));       // one pointer, not one for each chunk of a round
   };
   uint8_t* const lx = lds + lds_at(row, col);
   auto put = [&](const Stage& S, int z) {
@@ -130,27 +158,30 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     for (int e = 0; e < 16; ++e) acc[i >> 1][i & 1][e] = 0.f;
   const int G = lane >> 4, q = lane & 15, grp = wave >> 2, wk = 64 * (wave & 1), wn = 64 * ((wave >> 1) & 1);
   const int rr = 32 * grp + 8 * (G >> 1) + (q >> 2), cr = 16 * (G & 1) + 4 * (q & 3);
+  const uint8_t* ax[2] = {lds + lds_at(rr, wk + cr), lds + lds_at(rr, wk + 32 + cr)};
+  const uint8_t* by[2] = {lds + 2 * (kRows * 256) + lds_at(rr, wn + cr), lds + 2 * (kRows * 256) + lds_at(rr, wn + 32 + cr)};
   Stage S[kAhead];
   auto sync = [] {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
   };
-  // chunk at row m, in slot j % 2; after its barrier no wave reads the other slot, which the next chunk takes
-  auto chunk = [&](int64_t m, auto jc) {
+  // a chunk in slot j % 2; after its barrier no wave reads the other slot, which the next chunk takes
+  auto chunk = [&](auto jc) {
     constexpr int j = decltype(jc)::value, z = j & 1;
     sync();
     put(S[(j + 1) % kAhead], z ^ 1);
-    load(S[(j + 1) % kAhead], m + (kAhead + 1) * kRows);
+    load(S[(j + 1) % kAhead]);
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
+      __builtin_amdgcn_sched_barrier(0);        // one step's operands at a time: 128 registers for two blocks a CU
       u32x2_t a[2][2], b[2][2];
 #pragma unroll
       for (int f = 0; f < 2; ++f)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          a[f][i] = read_tr(lds + z * (kRows * 256) + lds_at(16 * st + rr + 4 * i, wk + 32 * f + cr));
-          b[f][i] = read_tr(lds + (2 + z) * (kRows * 256) + lds_at(16 * st + rr + 4 * i, wn + 32 * f + cr));
+          a[f][i] = read_tr(ax[f] + z * (kRows * 256) + st * 4096 + i * 1024);      // 16 st + 4 i rows on: the same swizzle
+          b[f][i] = read_tr(by[f] + z * (kRows * 256) + st * 4096 + i * 1024);
         }
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -159,38 +190,36 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     }
   };
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) load(S[i], mb + i * kRows);
+  for (int i = 0; i < kAhead; ++i) load(S[i]);
   put(S[0], 0);
-  load(S[0], mb + kAhead * kRows);
+  load(S[0]);
   // chunks past the last are zeros
   for (int64_t m = mb; m < me; m += kAhead * kRows) {
-    chunk(m, std::integral_constant<int, 0>{});
-    chunk(m + kRows, std::integral_constant<int, 1>{});
-    chunk(m + 2 * kRows, std::integral_constant<int, 2>{});
-    chunk(m + 3 * kRows, std::integral_constant<int, 3>{});
+    chunk(std::integral_constant<int, 0>{});
+    chunk(std::integral_constant<int, 1>{});
   }
+  // The tile as [n][k] in LDS (512 bytes a row, 16-byte slots XOR-swizzled by n): group 1's sums, then both groups', which
+  // leave in whole rows.
   __syncthreads();
-  f4_t* const hand = reinterpret_cast<f4_t*>(lds) + (wave & 3) * 1024;
-  if (grp == 1) {
+  f4_t* const tile = reinterpret_cast<f4_t*>(lds);
+  const int nl = wn + (lane & 31), sl = wk / 4 + (lane >> 5);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const f16_t& c = acc[i >> 3][(i >> 2) & 1];
-      hand[i * 64 + lane] = f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+  for (int g = 1; g >= 0; --g) {
+    if (grp == g) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const f16_t& c = acc[i >> 3][(i >> 2) & 1];
+        f4_t& t = tile[(nl + 32 * ((i >> 2) & 1)) * 32 + ((sl + 8 * (i >> 3) + 2 * (i & 3)) ^ (nl & 31))];
+        const f4_t v = {c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+        if (g == 1) t = v;
+        else t += v;
+      }
     }
+    __syncthreads();
   }
-  __syncthreads();
-  if (grp == 1) return;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const f16_t& c = acc[i >> 3][(i >> 2) & 1];
-    hand[i * 64 + lane] += f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
-  }
-  // (in a loop: written out, the stores of partial groups are more instructions than the rest)
-#pragma unroll 1
-  for (int i = 0; i < 16; ++i) {
-    const int64_t n = n0 + wn + 32 * ((i >> 2) & 1) + (lane & 31), k = k0 + wk + 32 * (i >> 3) + 8 * (i & 3) + 4 * (lane >> 5);
-    if (n < N && k < K) store_grad4(gW, meta, n, k, K, hand[i * 64 + lane]);
-  }
+  const int slot = tid & 31;
+  const int64_t k = k0 + 4 * slot;
+  store_rows<8>(gW, meta, tile, tid >> 5, 16, n0, N, slot, k, K);
 #endif
 }
 
@@ -467,21 +496,22 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
 #pragma unroll
   for (int x = 0; x < 4; ++x) asm volatile("" : "+a"(acc[x][0]), "+a"(acc[x][1]), "+a"(acc[x][2]), "+a"(acc[x][3]));   // not before
   __builtin_amdgcn_sched_barrier(0);
-  // the sums leave through LDS, half of them at a time, in a loop (see k_wgrad8)
+  // the sums leave through LDS in whole rows, half of the wave's columns n at a time (see k_wgrad8)
   f4_t* const mine = reinterpret_cast<f4_t*>(lds) + wave * 2048;
+  const int slot = lane & 31;
+  const int64_t k = k0 + wk + 4 * slot;
 #pragma unroll
   for (int y2 = 0; y2 < 2; ++y2) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const f16_t& c = acc[i >> 3][2 * y2 + ((i >> 2) & 1)];
-      mine[i * 64 + lane] = f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+      mine[((lane & 31) + 32 * ((i >> 2) & 1)) * 32 + ((8 * (i >> 3) + 2 * (i & 3) + (lane >> 5)) ^ (lane & 31))] =
+          f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
     }
-#pragma unroll 2
-    for (int i = 0; i < 32; ++i) {
-      const int64_t n = n0 + wn + 32 * (2 * y2 + ((i >> 2) & 1)) + (lane & 31), k = k0 + wk + 32 * (i >> 3) + 8 * (i & 3) + 4 * (lane >> 5);
-      if (n < N && k < K) store_grad4(gW, meta, n, k, K, mine[i * 64 + lane]);
-    }
+    // (in a loop: written out, the stores of partial groups are more instructions than the products)
+#pragma unroll 1
+    for (int i = lane >> 5; i < 64; i += 16) store_rows<8>(gW, meta, mine, i, 2, n0 + wn + 64 * y2, N, slot, k, K);
   }
 #endif
 }
@@ -498,7 +528,12 @@ size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
 
 GradPlan grad_plan(int64_t M, int64_t N, int64_t K, bool masked, bool aligned) {
   GradPlan p{};
-  p.wide = M > 0 && cdiv(N, 256) * cdiv(K, 256) >= 128 && N < (int64_t(1) << 22) - 16;
+  // A wide tile's block stands alone on its CU, so its first loads and last stores show: over few rows two small blocks to a CU
+  // are as fast or faster (9776 x 5786, M 64: 56 us against 58, M 128: 62 against 66, M 256: 95 against 77), and over more
+  // where the wide tiles leave CUs idle (2048 x 4096, 128 of them: M 512 20 against 23, M 1024 32 against 33, M 2048 55
+  // against 53; 22736 x 128, 89: 82 against 95 still at M 4096).
+  const int64_t wide = cdiv(N, 256) * cdiv(K, 256);
+  p.wide = (wide >= 256 ? M >= 192 : wide >= 128 && M >= 1536) && N < (int64_t(1) << 22) - 16;
   p.copy = M > 0 && (p.wide ? !aligned : N < 16);        // (the other kernel takes pieces of 16)
   p.slices = 1;
   p.slice = M;
