@@ -82,8 +82,8 @@ SLIM_DEV void store_rows(float* gW, const uint8_t* meta, const f4_t* tile, int r
 // registers, where X is widened (and dY's rows may start anywhere), into two LDS slots; registers are loaded three chunks
 // ahead, since a lone chunk takes less than a load's time to come (more would cost the second block on a CU). One barrier a chunk. A split launch writes its sums as one
 // array a slice, which k_wgrad8_sum adds in slice order.
-template <int DT>
-SLIM_DEV u32x2_t widen4(uint32_t c, float s);
+template <int DT, int HI>
+SLIM_DEV uint32_t widen2(uint32_t c, float s);
 
 template <int DT>
 __global__ void __launch_bounds__(512, 4)
@@ -147,9 +147,10 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     *reinterpret_cast<u32x4_t*>(y) = S.y0;
     *reinterpret_cast<u32x4_t*>(y + 16) = S.y1;
     const float s = q8_pow2(S.e);
-    const u32x2_t a = widen4<DT>(S.c[0], s), b = widen4<DT>(S.c[1], s), c = widen4<DT>(S.c[2], s), d = widen4<DT>(S.c[3], s);
-    *reinterpret_cast<u32x4_t*>(x) = u32x4_t{a[0], a[1], b[0], b[1]};
-    *reinterpret_cast<u32x4_t*>(x + 16) = u32x4_t{c[0], c[1], d[0], d[1]};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      *reinterpret_cast<u32x4_t*>(x + 16 * h) = u32x4_t{widen2<DT, 0>(S.c[2 * h], s), widen2<DT, 1>(S.c[2 * h], s),
+                                                        widen2<DT, 0>(S.c[2 * h + 1], s), widen2<DT, 1>(S.c[2 * h + 1], s)};
   };
   f16_t acc[2][2];
 #pragma unroll
@@ -269,20 +270,15 @@ SLIM_DEV void mfma_in_place(f16_t& c, u32x4_t a, u32x4_t b) {
 #endif
 }
 
-// Four codes times s as 16-bit values (two packed pairs); s is a power of two, of which the instruction takes the exponent.
-template <int DT>
-SLIM_DEV u32x2_t widen4(uint32_t c, float s) {
-  u32x2_t o;
+// Two of four codes times s as a pair of 16-bit values; s is a power of two, of which the instruction takes the exponent.
+template <int DT, int HI>
+SLIM_DEV uint32_t widen2(uint32_t c, float s) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  if constexpr (DT == 1) {
-    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, false));
-    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, true));
-  } else {
-    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, s, false));
-    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, s, true));
-  }
+  if constexpr (DT == 1) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, HI));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, s, HI));
+#else
+  return 0;
 #endif
-  return o;
 }
 
 template <int N, int I = 0, class F>
@@ -374,15 +370,17 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
     S.x[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, or_past(c, xo[j]), g * xstep, 0);
     S.e[j] = __builtin_amdgcn_raw_buffer_load_b8(re, or_past(c, eo[j]), g * estep, 0);
   };
-  // piece i (0 .. 3): eight codes widened and written
+  // step i (0 .. 15) of a chunk's widening: two codes, and after each eighth the 16 bytes to LDS
+  u32x4_t wide;
   auto put_x = [&](const Stage& S, auto zc, auto ic) {
     constexpr uint32_t off = decltype(zc)::value * kSlot;
-    constexpr int j = decltype(ic)::value >> 1, h = decltype(ic)::value & 1;
-    const float s = q8_pow2(S.e[j]);
-    const u32x2_t a = widen4<DT>(S.x[j][2 * h], s), b = widen4<DT>(S.x[j][2 * h + 1], s);
-    const u32x4_t v = {a[0], a[1], b[0], b[1]};
-    const uint32_t at = xw[j][h];
-    asm volatile("ds_write_b128 %0, %1 offset:%2" :: "v"(at), "v"(v), "i"(off) : "memory");
+    constexpr int i = decltype(ic)::value, j = i >> 3, h = (i >> 2) & 1, e = i & 3;
+    wide[e] = widen2<DT, e & 1>(S.x[j][2 * h + (e >> 1)], q8_pow2(S.e[j]));
+    if constexpr (e == 3) {
+      const uint32_t at = xw[j][h];
+      const u32x4_t v = wide;
+      asm volatile("ds_write_b128 %0, %1 offset:%2" :: "v"(at), "v"(v), "i"(off) : "memory");
+    }
   };
 
   f16_t acc[4][4];
@@ -451,7 +449,7 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
     constexpr int z = decltype(zc)::value;
     step(A, B, std::integral_constant<uint32_t, z * kSlot + 16 * 512>{}, [&](auto ic) {
       constexpr int i = decltype(ic)::value;
-      if constexpr (i >= 8 && i % 2 == 0) put_x(S[z & 1], std::integral_constant<int, (z + 2) % 4>{}, std::integral_constant<int, (i - 8) / 2>{});
+      put_x(S[z & 1], std::integral_constant<int, (z + 2) % 4>{}, ic);
     });
     landed(B);
     __builtin_amdgcn_s_waitcnt(vmcnt_wait(12));
@@ -471,8 +469,8 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
   each<4>([&](auto ic) { issue_y(2, I2{}, ic); });
   each<2>([&](auto jc) { load_x(S[0], 0, jc); });
   each<2>([&](auto jc) { load_x(S[1], 1, jc); });
-  each<4>([&](auto ic) { put_x(S[0], I0{}, ic); });
-  each<4>([&](auto ic) { put_x(S[1], I1{}, ic); });
+  each<16>([&](auto ic) { put_x(S[0], I0{}, ic); });
+  each<16>([&](auto ic) { put_x(S[1], I1{}, ic); });
   each<2>([&](auto jc) { load_x(S[0], 2, jc); });
   each<2>([&](auto jc) { load_x(S[1], 3, jc); });
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
