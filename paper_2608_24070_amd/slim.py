@@ -730,90 +730,117 @@ def update_pack16(Wnew, p: dict, stream=None) -> dict:
 
 # ------------------------------------------------- the 8-bit path
 
+# These helpers run before kernels of a few microseconds too: a check is made once, by the cheapest of torch's properties
+# (a tensor's get_device() for its device), and what a helper has just made is not checked again.
+
 _FLOAT_CODES: dict = {}
+_raw_stream = None
 
 
 def _float_code(dt) -> int:
     """slim_dtype of a torch floating type (fp16, bf16, fp32)."""
-    if not _FLOAT_CODES:
-        torch = _torch()
-        _FLOAT_CODES.update({torch.float16: SLIM_F16, torch.bfloat16: SLIM_BF16, torch.float32: SLIM_F32})
     code = _FLOAT_CODES.get(dt)
     if code is None:
+        if not _FLOAT_CODES:
+            torch = _torch()
+            _FLOAT_CODES.update({torch.float16: SLIM_F16, torch.bfloat16: SLIM_BF16, torch.float32: SLIM_F32})
+            return _float_code(dt)
         raise TypeError(f"expected fp16, bf16 or fp32, got {dt}")
     return code
 
 
-def _ld(t, what: str) -> int:
-    """Row stride of a 2-D tensor on the GPU whose rows are contiguous."""
+def _stream_on(dev: int, stream):
+    """The hipStream_t of `stream`, or of device `dev`'s current stream."""
+    global _raw_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        torch = _torch()
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(dev)
+
+
+def _matrix(t, what: str):
+    """(rows, columns, row stride, device) of a 2-D tensor on the GPU whose rows are contiguous."""
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{what} must be a 2-D tensor on the GPU")
+    m, n = t.shape
     ld, step = t.stride()
-    cols = t.shape[1]
-    if step != 1 and cols > 1:
+    if step != 1 and n > 1:
         raise ValueError(f"{what} must have contiguous rows")
-    if ld < cols:            # one row, or rows that overlap (expanded)
-        if t.shape[0] > 1:
+    if ld < n:               # one row, or rows that overlap (expanded)
+        if m > 1:
             raise ValueError(f"{what} must not have overlapping rows")
-        ld = cols
+        ld = n
+    return m, n, ld, t.get_device()
+
+
+def _matrix_out(out, m: int, n: int, dtype, dev: int, what: str = "out") -> int:
+    """Row stride of a given output, checked."""
+    rows, cols, ld, d = _matrix(out, what)
+    if (rows, cols) != (m, n) or out.dtype != dtype:
+        raise ValueError(f"{what} must be ({m}, {n}) of {dtype}, got {tuple(out.shape)} of {out.dtype}")
+    if d != dev:
+        raise ValueError(f"{what} must be on device {dev}, got {d}")
     return ld
 
 
-def _out(out, shape, dtype, like, what: str = "out"):
-    """`out` checked, or a new tensor."""
-    if out is None:
-        return _torch().empty(shape, dtype=dtype, device=like.device)
-    if out.shape != shape or out.dtype != dtype:
-        raise ValueError(f"{what} must be {tuple(shape)} of {dtype}, got {tuple(out.shape)} of {out.dtype}")
-    return out
+def _vector(t, n: int, dev: int, what: str):
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous vector of {n}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} must be on device {dev}")
 
 
-def _rows8(q: dict):
-    """Checked parts of 8-bit rows: codes, exps, M, K."""
+def _rows8(q: dict, dev: int | None = None):
+    """Checked parts of 8-bit rows: codes, exps, M, K, device (`dev` if given)."""
     codes, exps, M, K = q["codes"], q["exps"], q["M"], q["K"]
-    if codes.shape != (M, -(-K // 128) * 128) or exps.shape != (M, -(-K // 512) * 4):
+    if codes.shape != (M, (K + 127) // 128 * 128) or exps.shape != (M, (K + 511) // 512 * 4):
         raise ValueError("codes and exponents do not have the shape of the 8-bit rows")
     _on_gpu(codes, exps)
-    return codes, exps, M, K
+    d = codes.get_device()
+    if d != exps.get_device() or (dev is not None and d != dev):
+        raise ValueError("8-bit rows must be on one device with the other tensors")
+    return codes, exps, M, K, d
 
 
-def _empty_rows8(M: int, K: int, device) -> dict:
-    torch = _torch()
-    return {"codes": torch.empty((M, -(-K // 128) * 128), dtype=torch.uint8, device=device),
-            "exps": torch.empty((M, -(-K // 512) * 4), dtype=torch.uint8, device=device), "M": M, "K": K}
-
-
-def _one_device(a, *ts):
-    for t in ts:
-        if t is not None and t.device != a.device:
-            raise ValueError(f"tensors must be on one device, got {a.device} and {t.device}")
+def _empty_rows8(M: int, K: int, like) -> dict:
+    u8 = _torch().uint8
+    return {"codes": like.new_empty((M, (K + 127) // 128 * 128), dtype=u8),
+            "exps": like.new_empty((M, (K + 511) // 512 * 4), dtype=u8), "M": M, "K": K}
 
 
 def quant8(X, out: dict | None = None, stream=None) -> dict:
     """slim_quant8 of X [M, K] (fp16, bf16 or fp32; rows of any stride): {"codes" uint8 [M, K up to 128],
     "exps" uint8, "M", "K"}."""
-    ldx = _ld(X, "X")
-    M, K = X.shape
+    M, K, ldx, dev = _matrix(X, "X")
     if out is None:
-        out = _empty_rows8(M, K, X.device)
-    elif (out["M"], out["K"]) != (M, K):
-        raise ValueError("out is of another shape")
-    codes, exps, _, _ = _rows8(out)
-    _one_device(X, codes, exps)
-    _check(slim_quant8(X.data_ptr(), _float_code(X.dtype), M, K, ldx, codes.data_ptr(), exps.data_ptr(), _stream(stream)),
-           "slim_quant8")
+        out = _empty_rows8(M, K, X)
+    else:
+        _rows8(out, dev)
+        if (out["M"], out["K"]) != (M, K):
+            raise ValueError("out is of another shape")
+    st = lib().slim_quant8(X.data_ptr(), _float_code(X.dtype), M, K, ldx, out["codes"].data_ptr(), out["exps"].data_ptr(),
+                           _stream_on(dev, stream))
+    if st:
+        raise SlimError(st, "slim_quant8")
     return out
 
 
 def dequant8(q: dict, dtype=None, out=None, stream=None):
     """slim_dequant8: the values of 8-bit rows as [M, K] of `dtype` (bf16 if neither it nor `out` is given)."""
-    codes, exps, M, K = _rows8(q)
+    codes, exps, M, K, dev = _rows8(q)
     if dtype is None:
         dtype = out.dtype if out is not None else _torch().bfloat16
-    out = _out(out, (M, K), dtype, codes)
-    _one_device(codes, out)
-    _check(slim_dequant8(codes.data_ptr(), exps.data_ptr(), M, K, out.data_ptr(), _float_code(dtype), _ld(out, "out"),
-                         _stream(stream)), "slim_dequant8")
+    code = _float_code(dtype)
+    if out is None:
+        out, ldy = codes.new_empty((M, K), dtype=dtype), K
+    else:
+        ldy = _matrix_out(out, M, K, dtype, dev)
+    st = lib().slim_dequant8(codes.data_ptr(), exps.data_ptr(), M, K, out.data_ptr(), code, ldy, _stream_on(dev, stream))
+    if st:
+        raise SlimError(st, "slim_dequant8")
     return out
 
 
@@ -821,8 +848,7 @@ def pack8(W, bwd: bool = False, stream=None) -> dict:
     """slim_pack8 of W [N, K] (fp16, bf16 or fp32): {"codes", "exps", "N", "K"}, with `bwd` also the input gradient's
     {"codesT", "expsT"}."""
     torch = _torch()
-    ldw = _ld(W, "W")
-    N, K = W.shape
+    N, K, ldw, dev = _matrix(W, "W")
     up = lambda a, b: -(-a // b)
 
     def empty(n, k):
@@ -834,48 +860,63 @@ def pack8(W, bwd: bool = False, stream=None) -> dict:
     if bwd:
         out["codesT"], out["expsT"] = empty(K, N)
     _check(slim_pack8(W.data_ptr(), _float_code(W.dtype), N, K, ldw, _ptr(out["codes"]), _ptr(out["exps"]),
-                      _ptr(out.get("codesT")), _ptr(out.get("expsT")), _stream(stream)), "slim_pack8")
+                      _ptr(out.get("codesT")), _ptr(out.get("expsT")), _stream_on(dev, stream)), "slim_pack8")
     return out
 
 
 _ws8: dict = {}
 
 
-def _workspace8(nbytes: int, device, stream):
+def _workspace8(nbytes: int, like, stream: int):
     """The 8-bit calls' workspace, kept per (device, stream). Its contents are of no interest between calls, so it is not
     slim_linear's, whose counters have to stay zero."""
-    if not nbytes:
-        return None
-    key = (device, _stream(stream))
+    key = (like.get_device(), stream)
     ws = _ws8.get(key)
     if ws is None or ws.numel() < nbytes:
-        ws = _ws8[key] = _torch().empty(max(nbytes, 1 << 16), dtype=_torch().uint8, device=device)
+        ws = _ws8[key] = like.new_empty(max(nbytes, 1 << 16), dtype=_torch().uint8)
     return ws
 
 
+def _given8(nbytes: int, ws, like, stream: int):
+    """(pointer, size) of the workspace of a call that needs nbytes."""
+    if ws is None:
+        if not nbytes:
+            return None, 0
+        ws = _workspace8(nbytes, like, stream)
+    return ws.data_ptr(), ws.numel()
+
+
 def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, stream, where: str):
-    if codes.shape != (-(-N // 16), -(-K // 128), 2, 4, 16, 16) or exps.shape != (-(-N // 128), -(-K // 512) * 4):
+    if codes.shape != ((N + 15) // 16, (K + 127) // 128, 2, 4, 16, 16) or exps.shape != ((N + 127) // 128, (K + 511) // 512 * 4):
         raise ValueError("codes and exponents do not have the shape of the 8-bit weight")
-    if isinstance(X, dict):
-        x, xe, M, k = _rows8(X)
-        xdt, ldx = SLIM_Q8_E4M3, 0
+    _on_gpu(codes, exps)
+    if type(X) is dict:
+        x, xe, M, k, dev = _rows8(X)
+        xe, xdt, ldx = xe.data_ptr(), SLIM_Q8_E4M3, 0
     else:
-        x, xe, ldx, xdt = X, None, _ld(X, "X"), _float_code(X.dtype)
-        M, k = X.shape
+        x, xe, xdt = X, None, _float_code(X.dtype)
+        M, k, ldx, dev = _matrix(X, "X")
     if k != K:
         raise ValueError("the rows' width does not match the pack")
+    if codes.get_device() != dev or exps.get_device() != dev:
+        raise ValueError("X and the pack must be on one device")
     if dtype is None:
         torch = _torch()
         dtype = out.dtype if out is not None else torch.float16 if xdt == SLIM_F16 else torch.bfloat16
-    out = _out(out, (M, N), dtype, x)
-    _one_device(x, codes, exps, out)
-    _on_gpu(codes, exps)
-    need = slim_linear8_workspace(xdt, M, N, K)
-    if ws is None:
-        ws = _workspace8(need, x.device, stream)
-    _check(slim_linear8(x.data_ptr(), xdt, _ptr(xe), M, N, K, ldx, codes.data_ptr(), exps.data_ptr(), out.data_ptr(),
-                        _float_code(dtype), _ld(out, "out"), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)),
-           where)
+    ydt = _float_code(dtype)
+    if out is None:
+        out, ldy = x.new_empty((M, N), dtype=dtype), N
+    else:
+        ldy = _matrix_out(out, M, N, dtype, dev)
+    L, st = lib(), _stream_on(dev, stream)
+    need = ctypes.c_size_t()
+    rc = L.slim_linear8_workspace(xdt, M, N, K, need)
+    if not rc:
+        wp, wn = _given8(need.value, ws, x, st)
+        rc = L.slim_linear8(x.data_ptr(), xdt, xe, M, N, K, ldx, codes.data_ptr(), exps.data_ptr(), out.data_ptr(), ydt, ldy, wp,
+                            wn, st)
+    if rc:
+        raise SlimError(rc, where)
     return out
 
 
@@ -893,68 +934,71 @@ def bwd_dx8(dY, p: dict, dtype=None, out=None, ws=None, stream=None):
 def grad_w8(dY, q: dict, p: dict | None = None, out=None, ws=None, stream=None):
     """slim_grad_w8: dY^T X for dY [M, N] (fp16, bf16) and X [M, K] in 8 bits: fp32 [N, K], or with a value pack `p`
     (pack16) fp32 [N, K/2] at the positions it keeps."""
-    torch = _torch()
-    xc, xe, M, K = _rows8(q)
-    ldy = _ld(dY, "dY")
-    if dY.shape[0] != M:
+    m, N, ldy, dev = _matrix(dY, "dY")
+    xc, xe, M, K, _ = _rows8(q, dev)
+    if m != M:
         raise ValueError("dY and the checkpoint must have one number of rows")
-    N = dY.shape[1]
-    meta = None
+    dt, meta, cols = _dtype_code(dY), None, K
     if p is not None:
-        meta = p["meta"]
+        meta, cols = p["meta"], K // 2
         if meta.shape != (N, K // 8):
             raise ValueError("the value pack does not match dY and the checkpoint")
         _on_gpu(meta)
-    out = _out(out, (N, K if p is None else K // 2), torch.float32, dY)
-    _on_gpu(out)
-    _one_device(dY, xc, xe, meta, out)
-    y = dY.data_ptr()
+        if meta.get_device() != dev:
+            raise ValueError("dY and the value pack must be on one device")
+        meta = meta.data_ptr()
+    if out is None:
+        out = dY.new_empty((N, cols), dtype=_torch().float32)
+    else:
+        _on_gpu(out)
+        _matrix_out(out, N, cols, _torch().float32, dev)
+    y, L, st = dY.data_ptr(), lib(), _stream_on(dev, stream)
     aligned = 1 if y % 16 == 0 and ldy % 8 == 0 and ldy < 1 << 22 else 0
-    need = slim_grad_w8_workspace(M, N, K, 0 if p is None else 1, aligned)
-    if ws is None:
-        ws = _workspace8(need, dY.device, stream)
-    _check(slim_grad_w8(y, _dtype_code(dY), ldy, xc.data_ptr(), xe.data_ptr(), M, N, K, _ptr(meta), out.data_ptr(), _ptr(ws),
-                        0 if ws is None else ws.numel(), _stream(stream)), "slim_grad_w8")
+    need = ctypes.c_size_t()
+    rc = L.slim_grad_w8_workspace(M, N, K, 0 if p is None else 1, aligned, need)
+    if not rc:
+        wp, wn = _given8(need.value, ws, dY, st)
+        rc = L.slim_grad_w8(y, dt, ldy, xc.data_ptr(), xe.data_ptr(), M, N, K, meta, out.data_ptr(), wp, wn, st)
+    if rc:
+        raise SlimError(rc, "slim_grad_w8")
     return out
-
-
-def _params(K: int, *ps) -> int:
-    """The one slim_dtype of a norm's parameters, each contiguous [K] or None."""
-    code = None
-    for t in ps:
-        if t is None:
-            continue
-        if t.shape != (K,) or not t.is_contiguous():
-            raise ValueError("gamma and beta must be contiguous vectors of the rows' width")
-        c = _float_code(t.dtype)
-        if code is not None and c != code:
-            raise TypeError("gamma and beta must have one dtype")
-        code = c
-    return SLIM_F32 if code is None else code
 
 
 def norm(X, gamma=None, beta=None, eps: float = 1e-5, rms: bool = False, q8: bool = False, out=None, stream=None):
     """slim_norm over the rows of X [M, K] (fp16, bf16 or fp32): layer norm, or with `rms` the RMS norm. Returns (Y, mean,
     rstd): Y of X's type, or with `q8` 8-bit rows (as quant8); mean and rstd fp32 [M] for norm_bwd, mean None with `rms`."""
-    torch = _torch()
-    ldx = _ld(X, "X")
-    M, K = X.shape
-    dt, pdt = _float_code(X.dtype), _params(K, gamma, beta)
-    stats = torch.empty((2, M), dtype=torch.float32, device=X.device)
-    mean, rstd = None if rms else stats[0], stats[1]
+    M, K, ldx, dev = _matrix(X, "X")
+    dt = _float_code(X.dtype)
+    pdt, gp, bp = SLIM_F32, None, None
+    if gamma is not None:
+        _vector(gamma, K, dev, "gamma")
+        pdt, gp = _float_code(gamma.dtype), gamma.data_ptr()
+    if beta is not None:
+        _vector(beta, K, dev, "beta")
+        if gamma is not None and beta.dtype != gamma.dtype:
+            raise TypeError("gamma and beta must have one dtype")
+        pdt, bp = _float_code(beta.dtype), beta.data_ptr()
+    f32 = _torch().float32
+    rstd = X.new_empty((M,), dtype=f32)
+    mean = None if rms else X.new_empty((M,), dtype=f32)
     if q8:
         if out is None:
-            out = _empty_rows8(M, K, X.device)
-        y, ye, m, k = _rows8(out)
-        if (m, k) != (M, K):
-            raise ValueError("out is of another shape")
-        ydt, ldy = SLIM_Q8_E4M3, 0
+            out = _empty_rows8(M, K, X)
+        else:
+            _rows8(out, dev)
+            if (out["M"], out["K"]) != (M, K):
+                raise ValueError("out is of another shape")
+        yp, ye, ydt, ldy = out["codes"].data_ptr(), out["exps"].data_ptr(), SLIM_Q8_E4M3, 0
     else:
-        out = y = _out(out, (M, K), X.dtype, X)
-        ye, ydt, ldy = None, dt, _ld(y, "out")
-    _one_device(X, gamma, beta, y, ye)
-    _check(slim_norm(X.data_ptr(), dt, M, K, ldx, _ptr(gamma), _ptr(beta), pdt, 1 if rms else 0, eps, y.data_ptr(), ydt,
-                     ldy, _ptr(ye), _ptr(mean), rstd.data_ptr(), _stream(stream)), "slim_norm")
+        if out is None:
+            out, ldy = X.new_empty((M, K)), K
+        else:
+            ldy = _matrix_out(out, M, K, X.dtype, dev)
+        yp, ye, ydt = out.data_ptr(), None, dt
+    rc = lib().slim_norm(X.data_ptr(), dt, M, K, ldx, gp, bp, pdt, 1 if rms else 0, eps, yp, ydt, ldy, ye,
+                         None if rms else mean.data_ptr(), rstd.data_ptr(), _stream_on(dev, stream))
+    if rc:
+        raise SlimError(rc, "slim_norm")
     return out, mean, rstd
 
 
@@ -962,29 +1006,41 @@ def norm_bwd(dY, X, gamma, mean, rstd, out=None, ws=None, stream=None):
     """slim_norm_bwd: (dX, dgamma, dbeta) from dY [M, K], the forward's input X (dY's type, or its 8-bit checkpoint from
     quant8), gamma (or None) and the forward's mean and rstd; mean None: RMS norm, dbeta None. dX of dY's type, dgamma
     and dbeta fp32."""
-    torch = _torch()
-    lddy = _ld(dY, "dY")
-    M, K = dY.shape
-    dt, pdt = _float_code(dY.dtype), _params(K, gamma)
-    if isinstance(X, dict):
-        x, xe, m, k = _rows8(X)
-        xdt, ldx = SLIM_Q8_E4M3, 0
+    M, K, lddy, dev = _matrix(dY, "dY")
+    dt, pdt, gp, mp = _float_code(dY.dtype), SLIM_F32, None, None
+    if type(X) is dict:
+        x, xe, m, k, _ = _rows8(X, dev)
+        xp, xe, xdt, ldx = x.data_ptr(), xe.data_ptr(), SLIM_Q8_E4M3, 0
     else:
-        x, xe, xdt, ldx = X, None, _float_code(X.dtype), _ld(X, "X")
-        m, k = X.shape
+        xp, xe, xdt = X.data_ptr(), None, _float_code(X.dtype)
+        m, k, ldx, d = _matrix(X, "X")
+        if d != dev:
+            raise ValueError("dY and X must be on one device")
     if (m, k) != (M, K):
         raise ValueError("dY and X must have one shape")
-    for t in (mean, rstd):
-        if t is not None and (t.shape != (M,) or t.dtype != torch.float32 or not t.is_contiguous()):
-            raise ValueError("mean and rstd must be contiguous fp32 vectors of the number of rows")
-    out = _out(out, (M, K), dY.dtype, dY)
-    grads = torch.empty((1 if mean is None else 2, K), dtype=torch.float32, device=dY.device)
-    dgamma, dbeta = grads[0], None if mean is None else grads[1]
-    _one_device(dY, x, xe, gamma, mean, rstd, out)
-    need = slim_norm_bwd_workspace(M, K)
-    if ws is None:
-        ws = _workspace8(need, dY.device, stream)
-    _check(slim_norm_bwd(dY.data_ptr(), dt, lddy, x.data_ptr(), xdt, _ptr(xe), ldx, M, K, _ptr(gamma), pdt, _ptr(mean),
-                         rstd.data_ptr(), out.data_ptr(), _ld(out, "out"), dgamma.data_ptr(), _ptr(dbeta), _ptr(ws),
-                         0 if ws is None else ws.numel(), _stream(stream)), "slim_norm_bwd")
+    if gamma is not None:
+        _vector(gamma, K, dev, "gamma")
+        pdt, gp = _float_code(gamma.dtype), gamma.data_ptr()
+    f32 = _torch().float32
+    _vector(rstd, M, dev, "rstd")
+    if mean is not None:
+        _vector(mean, M, dev, "mean")
+        mp = mean.data_ptr()
+    if rstd.dtype != f32 or (mean is not None and mean.dtype != f32):
+        raise TypeError("mean and rstd must be fp32")
+    if out is None:
+        out, lddx = dY.new_empty((M, K)), K
+    else:
+        lddx = _matrix_out(out, M, K, dY.dtype, dev)
+    dgamma = dY.new_empty((K,), dtype=f32)
+    dbeta = None if mean is None else dY.new_empty((K,), dtype=f32)
+    L, st = lib(), _stream_on(dev, stream)
+    need = ctypes.c_size_t()
+    rc = L.slim_norm_bwd_workspace(M, K, need)
+    if not rc:
+        wp, wn = _given8(need.value, ws, dY, st)
+        rc = L.slim_norm_bwd(dY.data_ptr(), dt, lddy, xp, xdt, xe, ldx, M, K, gp, pdt, mp, rstd.data_ptr(), out.data_ptr(), lddx,
+                             dgamma.data_ptr(), None if dbeta is None else dbeta.data_ptr(), wp, wn, st)
+    if rc:
+        raise SlimError(rc, "slim_norm_bwd")
     return out, dgamma, dbeta

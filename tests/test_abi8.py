@@ -78,7 +78,7 @@ def test_grad_w8(kw, status):
 
 def test_grad_w8_workspace_is_for_odd_rows_and_short_layers():
     assert slim.slim_grad_w8_workspace(8192, 28672, 8192, 1, 1) == 0
-    assert slim.slim_grad_w8_workspace(100, 8193, 8192, 0, 0) == -(-100 * 8208 * 2 // 256) * 256
+    assert slim.slim_grad_w8_workspace(1000, 8193, 8192, 0, 0) == -(-1000 * 8208 * 2 // 256) * 256
     assert slim.slim_grad_w8_workspace(8192, 128, 128, 0, 1) > 0 and slim.slim_grad_w8_workspace(0, 128, 128, 0, 0) == 0
 
 
