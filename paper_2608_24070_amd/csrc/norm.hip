@@ -36,7 +36,9 @@ struct RowsOf {
 template <int DT, bool RAG>
 SLIM_DEV Raw8<DT> load_raw8(const RowsOf& r, int64_t row, int64_t col, int64_t K) {
   Raw8<DT> o;
-  const int64_t n = RAG ? K - col : col < K ? 8 : 0, i = row * r.ld + col;
+  int n = RAG ? (int)(K - col) : col < K ? 8 : 0;
+  const int64_t i = row * r.ld + col;
+  if constexpr (RAG) asm volatile("" : "+v"(n));      // compared here, not held as masks over a caller's loop
   if constexpr (DT == kQ8) {
     // rows are padded to whole groups with zeros
     o.c = u32x2_t{0, 0};
@@ -87,6 +89,22 @@ SLIM_DEV void values8(const Raw8<DT>& o, float* f) {
   } else {
     act8_to_f(o.v, DT == 1, f);
   }
+}
+
+// xh = (x - mu) rstd of eight elements, one fused operation each: `shift` = -mu rstd, and of 8-bit rows the group's power of
+// two goes into the factor.
+template <int DT>
+SLIM_DEV void xhat8(const Raw8<DT>& o, float rstd, float shift, float* f) {
+  float s = rstd;
+  if constexpr (DT == kQ8) {
+    q8_values4(o.c[0], 1.f, f);
+    q8_values4(o.c[1], 1.f, f + 4);
+    s = o.s * rstd;
+  } else {
+    values8<DT>(o, f);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = fmaf(f[e], s, shift);
 }
 
 // Eight parameters (gamma, beta) as fp32; `none` where there are none.
@@ -157,16 +175,20 @@ SLIM_DEV void store_row8(void* y, uint8_t* exps, int64_t row, int64_t ld, int64_
     }
     const uint32_t b = q8_exponent(row16_max_u32(m));
     const int64_t Kp = q8_row(K), Ge = q8_exp_row(K);
-    if (col < Kp) {
+    const int in = n + (int)(Kp - K);                 // columns from here to the end of the last group
+    if (in > 0) {
       const float s = q8_inverse(b);
       const u32x2_t c = {q8_codes4(f[0], f[1], f[2], f[3], s), q8_codes4(f[4], f[5], f[6], f[7], s)};
       *reinterpret_cast<u32x2_t*>(reinterpret_cast<uint8_t*>(y) + row * Kp + col) = c;
-      const int64_t g = col / 128, sub = (col & 127) / 8;
-      if (sub == 0) exps[row * Ge + g] = (uint8_t)b;
-      else if (g == Kp / 128 - 1 && g + sub < Ge) exps[row * Ge + g + sub] = 0;
+      const int sub = (int)(col & 127) / 8;
+      uint8_t* e = exps + row * Ge + col / 128;
+      if (sub == 0) *e = (uint8_t)b;
+      else if (in <= 128 && sub <= (int)(Ge - Kp / 128)) e[sub] = 0;      // the row's last word ends in zeros
     }
   } else {
-    if (col < K) store8<DT>(y, row * ld + col, RAG ? K - col : 8, f);
+    int n = RAG ? (int)(K - col) : 8;
+    if constexpr (RAG) asm volatile("" : "+v"(n));
+    if (col < K) store8<DT>(y, row * ld + col, n, f);
   }
 }
 
@@ -188,8 +210,11 @@ struct NormArgs {
 
 // Rows of up to 8 T V elements, T threads a row, V vectors of 8 a thread. Each wave sums its part of the row about its
 // own mean, and the waves' (count, mean, squares) are joined exactly as if about the row's mean: one barrier a row, and no
-// cancellation for rows far from zero. HOLD: gamma and beta stay in registers from row to row.
-template <int DT, int YT, int T, int V, bool HOLD, bool RAG>
+// cancellation for rows far from zero. HOLD: gamma and beta stay in registers from row to row; AHEAD: the next row is loaded
+// before the present one is worked on (both as registers allow).
+// Bound by memory: 8192 x 8192 in bf16 41.6 us (6.5 TB/s read and written), to 8 bits 46.9 us (4.3 TB/s); 2047 x 5120 in
+// fp16 15.0 us; one row of 4096 6.4 us, which is a launch and two trips to memory.
+template <int DT, int YT, int T, int V, bool HOLD, bool AHEAD, bool RAG>
 __global__ void __launch_bounds__(T == 64 ? 256 : T)
 k_norm(NormArgs a) {
   constexpr int kRows = T == 64 ? 4 : 1, kWaves = T / 64, H = HOLD ? V : 1;
@@ -203,7 +228,7 @@ k_norm(NormArgs a) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const int64_t col = (int64_t)(v * T + t) * 8;
-    if (first < a.M) nx[v] = load_raw8<DT, RAG>(a.x, first, col, a.K);
+    if (AHEAD && first < a.M) nx[v] = load_raw8<DT, RAG>(a.x, first, col, a.K);
     if constexpr (HOLD) {
       params8<RAG>(a.gamma, a.pdt, col, a.K, 1.f, gm[v]);
       params8<RAG>(a.beta, a.pdt, col, a.K, 0.f, bt[v]);
@@ -216,9 +241,12 @@ k_norm(NormArgs a) {
   int turn = 0;
   for (int64_t row = first; row < a.M; row += step, turn ^= 1) {
     float x[V][8];
+    if (!AHEAD)
+#pragma unroll
+      for (int v = 0; v < V; ++v) nx[v] = load_raw8<DT, RAG>(a.x, row, (int64_t)(v * T + t) * 8, a.K);
 #pragma unroll
     for (int v = 0; v < V; ++v) values8<DT>(nx[v], x[v]);
-    if (row + step < a.M)
+    if (AHEAD && row + step < a.M)
 #pragma unroll
       for (int v = 0; v < V; ++v) nx[v] = load_raw8<DT, RAG>(a.x, row + step, (int64_t)(v * T + t) * 8, a.K);
     float mu = 0.f, sq = 0.f;
@@ -282,7 +310,9 @@ k_norm(NormArgs a) {
   }
 }
 
-// Longer rows: one block a row reads it three times (mean, squares, result), the later times from the caches.
+// Longer rows: one block a row reads it three times (mean, squares, result), the later times from the caches. Also ragged
+// rows past 16384, where a vector's tests for the row's end cost the kernel above its scalar registers: 2048 x 28671 in
+// bf16 79 us (28672 in registers: 57.6 us).
 template <int DT, int YT>
 __global__ void __launch_bounds__(1024)
 k_norm_long(NormArgs a) {
@@ -339,11 +369,15 @@ struct NormBwdArgs {
   void* dx;
   int64_t lddx;
   float* part;          // column sums of each block: [blocks][2][K] (dgamma, dbeta)
+  float* dgamma;
+  float* dbeta;
 };
 
 // As k_norm: T threads a row, V vectors a thread; dgamma's and dbeta's sums over the block's rows stay in registers and
-// leave as one row of partial sums a block (k_norm_cols adds those in block order).
-template <int DT, int XT, int T, int V, bool RAG>
+// leave as one row of partial sums a block (k_norm_cols adds those in block order). Rows of up to 8192 take 256 threads of
+// four vectors rather than 512 of two: two blocks share a CU and do not wait at one barrier (8192 x 8192 in bf16 79.0 and
+// 96.7 us). That is 5.1 TB/s; k_norm_cols takes another 5.8 us. 8192 x 4096 33.2 + 4.5, 2047 x 5120 in fp16 20.8 + 4.0.
+template <int DT, int XT, int T, int V, bool HOLD, bool AHEAD, bool RAG>
 __global__ void __launch_bounds__(T == 64 ? 256 : T)
 k_norm_bwd(NormBwdArgs a) {
   constexpr int kRows = T == 64 ? 4 : 1;
@@ -351,32 +385,38 @@ k_norm_bwd(NormBwdArgs a) {
   __shared__ float join[kRows > 1 ? 3 : 1][kRows > 1 ? 2 : 1][kRows > 1 ? V * T * 8 : 1];
   const int t = threadIdx.x % T;
   const int64_t first = (int64_t)blockIdx.x * kRows + threadIdx.x / T, step = (int64_t)gridDim.x * kRows;
-  float gm[V][8], dg[V][8], db[V][8];
+  constexpr int H = HOLD ? V : 1;
+  float gm[H][8], dg[V][8], db[V][8];
   Raw8<DT> ny[V];
   Raw8<XT> nx[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const int64_t col = (int64_t)(v * T + t) * 8;
-    if (first < a.M) {
+    if (AHEAD && first < a.M) {
       ny[v] = load_raw8<DT, RAG>(a.dy, first, col, a.K);
       nx[v] = load_raw8<XT, RAG>(a.x, first, col, a.K);
     }
-    params8<RAG>(a.gamma, a.pdt, col, a.K, 1.f, gm[v]);
+    if constexpr (HOLD) params8<RAG>(a.gamma, a.pdt, col, a.K, 1.f, gm[v]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dg[v][e] = db[v][e] = 0.f;
   }
   const float inv_k = 1.f / (float)a.K;
   int turn = 0;
   for (int64_t row = first; row < a.M; row += step, turn ^= 1) {
-    const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
+    const float rstd = a.rstd[row], shift = a.mean ? -a.mean[row] * rstd : 0.f;
     Raw8<DT> y[V];
     Raw8<XT> x[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      y[v] = ny[v];
-      x[v] = nx[v];
+      if constexpr (AHEAD) {
+        y[v] = ny[v];
+        x[v] = nx[v];
+      } else {
+        y[v] = load_raw8<DT, RAG>(a.dy, row, (int64_t)(v * T + t) * 8, a.K);
+        x[v] = load_raw8<XT, RAG>(a.x, row, (int64_t)(v * T + t) * 8, a.K);
+      }
     }
-    if (row + step < a.M)
+    if (AHEAD && row + step < a.M)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         ny[v] = load_raw8<DT, RAG>(a.dy, row + step, (int64_t)(v * T + t) * 8, a.K);
@@ -387,11 +427,12 @@ k_norm_bwd(NormBwdArgs a) {
     for (int v = 0; v < V; ++v) {
       float d[8], h[8];
       values8<DT>(y[v], d);
-      values8<XT>(x[v], h);
+      xhat8<XT>(x[v], rstd, shift, h);
+      const int g = HOLD ? v : 0;
+      if constexpr (!HOLD) params8<RAG>(a.gamma, a.pdt, (int64_t)(v * T + t) * 8, a.K, 1.f, gm[0]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        h[e] = (h[e] - mu) * rstd;            // past K dy is zero, so h does not matter there
-        const float tt = d[e] * gm[v][e];
+        const float tt = d[e] * gm[g][e];     // zero past K, where h does not matter
         st += tt;
         sx = fmaf(tt, h[e], sx);
         dg[v][e] = fmaf(d[e], h[e], dg[v][e]);
@@ -404,12 +445,11 @@ k_norm_bwd(NormBwdArgs a) {
     for (int v = 0; v < V; ++v) {
       float d[8], h[8];
       values8<DT>(y[v], d);
-      values8<XT>(x[v], h);
+      xhat8<XT>(x[v], rstd, shift, h);
+      const int g = HOLD ? v : 0;
+      if constexpr (!HOLD) params8<RAG>(a.gamma, a.pdt, (int64_t)(v * T + t) * 8, a.K, 1.f, gm[0]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        h[e] = (h[e] - mu) * rstd;
-        d[e] = rstd * fmaf(-mx, h[e], fmaf(d[e], gm[v][e], -mt));
-      }
+      for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-mx, h[e], fmaf(d[e], gm[g][e], -mt));
       store_row8<DT, RAG>(a.dx, nullptr, row, a.lddx, (int64_t)(v * T + t) * 8, a.K, d);
     }
   }
@@ -436,18 +476,21 @@ k_norm_bwd(NormBwdArgs a) {
           db[v][e] += join[i][1][(v * 8 + e) * T + t];
         }
   }
-  float* out = a.part + (int64_t)blockIdx.x * 2 * a.K;
+  // one block: its sums are the gradients
+  float* const og = gridDim.x == 1 ? a.dgamma : a.part + (int64_t)blockIdx.x * 2 * a.K;
+  float* const ob = gridDim.x == 1 ? a.dbeta : a.part + ((int64_t)blockIdx.x * 2 + 1) * a.K;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const int64_t col = (int64_t)(v * T + t) * 8;
     if (col < a.K) {
-      store8<2>(out, col, a.K - col, dg[v]);
-      store8<2>(out + a.K, col, a.K - col, db[v]);
+      if (og) store8<2>(og, col, RAG ? a.K - col : 8, dg[v]);
+      if (ob) store8<2>(ob, col, RAG ? a.K - col : 8, db[v]);
     }
   }
 }
 
-// Longer rows, second kernel: dx, one block a row, which reads it twice.
+// Longer rows, second kernel: dx, one block a row, which reads it twice: 2048 x 28672 in bf16 85 us after 49 us for the
+// column sums. Sums of such rows do not fit the registers beside the row itself.
 template <int DT, int XT>
 __global__ void __launch_bounds__(1024)
 k_norm_bwd_long(NormBwdArgs a) {
@@ -502,9 +545,10 @@ k_norm_bwd_long_cols(NormBwdArgs a) {
       db[e] += d[e];
     }
   }
-  float* out = a.part + (int64_t)blockIdx.y * 2 * a.K;
-  store8<2>(out, col, a.K - col, dg);
-  store8<2>(out + a.K, col, a.K - col, db);
+  float* const og = gridDim.y == 1 ? a.dgamma : a.part + (int64_t)blockIdx.y * 2 * a.K;
+  float* const ob = gridDim.y == 1 ? a.dbeta : a.part + ((int64_t)blockIdx.y * 2 + 1) * a.K;
+  if (og) store8<2>(og, col, a.K - col, dg);
+  if (ob) store8<2>(ob, col, a.K - col, db);
 }
 
 // dgamma and dbeta from the blocks' column sums: 64 columns a block, 16 threads a column that each add every 16th block's
@@ -515,8 +559,18 @@ k_norm_cols(const float* __restrict__ part, int blocks, int64_t K, float* __rest
   const int c = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t i = (int64_t)blockIdx.x * 64 + c;     // column of [dgamma | dbeta]
   float v = 0.f;
-  if (i < 2 * K)
-    for (int b = w; b < blocks; b += 16) v += part[(int64_t)b * 2 * K + i];
+  if (i < 2 * K) {
+    const float* p = part + i;
+    int b = w;
+    for (; b + 112 < blocks; b += 128) {         // eight loads in flight
+      float t[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = p[(int64_t)(b + 16 * j) * 2 * K];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v += t[j];
+    }
+    for (; b < blocks; b += 16) v += p[(int64_t)b * 2 * K];
+  }
   s[w][c] = v;
   __syncthreads();
   if (w || i >= 2 * K) return;
@@ -536,16 +590,13 @@ size_t elem(int dt) { return dt == SLIM_F32 ? 4 : 2; }
 template <int DT, int YT, bool RAG>
 void norm_rows(const NormArgs& a, SlimKernelTimer& timer, hipStream_t s) {
   const auto grid = [&](int64_t units, int64_t most) { return dim3((unsigned)(units < most ? units : most)); };
-  if (a.K <= 512) SLIM_LAUNCH(timer, (k_norm<DT, YT, 64, 1, true, RAG>), grid((a.M + 3) / 4, 2048), dim3(256), s, a);
-  else if (a.K <= 1024) SLIM_LAUNCH(timer, (k_norm<DT, YT, 64, 2, true, RAG>), grid((a.M + 3) / 4, 2048), dim3(256), s, a);
-  else if (a.K <= 4096) SLIM_LAUNCH(timer, (k_norm<DT, YT, 256, 2, true, RAG>), grid(a.M, 1024), dim3(256), s, a);
-  else if (a.K <= 8192) SLIM_LAUNCH(timer, (k_norm<DT, YT, 512, 2, true, RAG>), grid(a.M, 512), dim3(512), s, a);
-  else if constexpr (!RAG) {
-    if (a.K <= 16384) SLIM_LAUNCH(timer, (k_norm<DT, YT, 512, 4, true, false>), grid(a.M, 256), dim3(512), s, a);
-    else SLIM_LAUNCH(timer, (k_norm_long<DT, YT>), dim3((unsigned)a.M), dim3(1024), s, a);
-  } else {
-    SLIM_LAUNCH(timer, (k_norm_long<DT, YT>), dim3((unsigned)a.M), dim3(1024), s, a);
-  }
+  if (a.K <= 512) SLIM_LAUNCH(timer, (k_norm<DT, YT, 64, 1, true, true, RAG>), grid((a.M + 3) / 4, 2048), dim3(256), s, a);
+  else if (a.K <= 1024) SLIM_LAUNCH(timer, (k_norm<DT, YT, 64, 2, true, true, RAG>), grid((a.M + 3) / 4, 2048), dim3(256), s, a);
+  else if (a.K <= 4096) SLIM_LAUNCH(timer, (k_norm<DT, YT, 256, 2, true, true, RAG>), grid(a.M, 1024), dim3(256), s, a);
+  else if (a.K <= 8192) SLIM_LAUNCH(timer, (k_norm<DT, YT, 512, 2, true, true, RAG>), grid(a.M, 512), dim3(512), s, a);
+  else if (a.K <= 16384) SLIM_LAUNCH(timer, (k_norm<DT, YT, 512, 4, true, true, RAG>), grid(a.M, 512), dim3(512), s, a);
+  else if (!RAG && a.K <= 32768) SLIM_LAUNCH(timer, (k_norm<DT, YT, 512, 8, false, false, false>), grid(a.M, 512), dim3(512), s, a);
+  else SLIM_LAUNCH(timer, (k_norm_long<DT, YT>), dim3((unsigned)a.M), dim3(1024), s, a);
 }
 
 template <int DT>
@@ -555,20 +606,23 @@ void norm_to(const NormArgs& a, int ydt, SlimKernelTimer& timer, hipStream_t s) 
   else rag ? norm_rows<DT, DT, true>(a, timer, s) : norm_rows<DT, DT, false>(a, timer, s);
 }
 
-// Blocks of the backward's column sums: each is one row of partial sums.
+// Blocks of the backward, each with a row of column sums that a second launch adds; up to four rounds of one block are
+// less than that launch takes.
 int64_t bwd_blocks(int64_t M, int64_t K) {
   const int64_t units = K <= 1024 ? (M + 3) / 4 : M, most = K <= 4096 ? 768 : K <= 8192 ? 512 : 256;
-  return units < most ? units : most;
+  return units <= 4 ? 1 : units < most ? units : most;
 }
 
 template <int DT, int XT, bool RAG>
 void norm_bwd_rows_of(const NormBwdArgs& a, hipStream_t s) {
   const unsigned blocks = (unsigned)bwd_blocks(a.M, a.K);
   SlimKernelTimer timer("norm_bwd", s);
-  if (a.K <= 512) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 64, 1, RAG>), dim3(blocks), dim3(256), s, a);
-  else if (a.K <= 1024) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 64, 2, RAG>), dim3(blocks), dim3(256), s, a);
-  else if (a.K <= 4096) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 256, 2, RAG>), dim3(blocks), dim3(256), s, a);
-  else if (a.K <= 8192) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 512, 2, RAG>), dim3(blocks), dim3(512), s, a);
+  if (a.K <= 512) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 64, 1, true, true, RAG>), dim3(blocks), dim3(256), s, a);
+  else if (a.K <= 1024) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 64, 2, true, true, RAG>), dim3(blocks), dim3(256), s, a);
+  else if (a.K <= 4096) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 256, 2, true, true, RAG>), dim3(blocks), dim3(256), s, a);
+  else if (a.K <= 8192) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 256, 4, true, true, RAG>), dim3(blocks), dim3(256), s, a);
+  else if (a.K <= 16384 && !(RAG && DT == 2))
+    SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 512, 4, DT != 2, DT != 2, RAG && DT != 2>), dim3(blocks), dim3(512), s, a);
   else {
     // the column sums first: dX may be written over dY
     SLIM_LAUNCH(timer, (k_norm_bwd_long_cols<DT, XT>), dim3((unsigned)((a.K + 2047) / 2048), blocks), dim3(256), s, a);
@@ -609,7 +663,8 @@ extern "C" int slim_norm(const void* X, int dtype, int64_t M, int64_t K, int64_t
 extern "C" int slim_norm_bwd_workspace(int64_t M, int64_t K, size_t* bytes) {
   if (!bytes) return SLIM_EINVAL;
   if (M < 0 || K < 1 || K > kMaxRow8 || M > 0x7FFFFFFF) return SLIM_ESHAPE;
-  *bytes = (size_t)bwd_blocks(M, K) * 2 * (size_t)K * 4;
+  const int64_t blocks = M > 0 ? bwd_blocks(M, K) : 0;
+  *bytes = blocks > 1 ? (size_t)blocks * 2 * (size_t)K * 4 : 0;
   return SLIM_OK;
 }
 
@@ -632,14 +687,14 @@ extern "C" int slim_norm_bwd(const void* dY, int dtype, int64_t lddy, const void
   if (need && !slim_aligned16(ws)) return SLIM_EALIGN;
   hipStream_t s = (hipStream_t)stream;
   const NormBwdArgs a{{dY, nullptr, lddy}, {X, xexps, q8 ? q8_row(K) : ldx}, gamma, pdtype, mean, rstd, M, K, dX, lddx,
-                      reinterpret_cast<float*>(ws)};
+                      reinterpret_cast<float*>(ws), dgamma, dbeta};
   if (M > 0) {
     if (dtype == SLIM_F16) q8 ? norm_bwd_rows<0, kQ8>(a, s) : norm_bwd_rows<0, 0>(a, s);
     else if (dtype == SLIM_BF16) q8 ? norm_bwd_rows<1, kQ8>(a, s) : norm_bwd_rows<1, 1>(a, s);
     else q8 ? norm_bwd_rows<2, kQ8>(a, s) : norm_bwd_rows<2, 2>(a, s);
     if (hipGetLastError() != hipSuccess) return SLIM_EDEVICE;
   }
-  if (dgamma || dbeta) {
+  if ((dgamma || dbeta) && (M == 0 || bwd_blocks(M, K) > 1)) {
     SlimKernelTimer timer("norm_cols", s);
     SLIM_LAUNCH(timer, k_norm_cols, dim3((unsigned)((2 * K + 63) / 64)), dim3(1024), s, reinterpret_cast<const float*>(ws),
                 (int)(M > 0 ? bwd_blocks(M, K) : 0), K, dgamma, dbeta);

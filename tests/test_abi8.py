@@ -99,7 +99,7 @@ def test_norm(kw, status):
     (dict(lddx=9), SHAPE), (dict(dY=ODD), ALIGN), (dict(X=MIS, xdt=Q8), ALIGN), (dict(dg=A + 2), ALIGN), (dict(ws=None), WS), (dict(short=1), WS),
     (dict(ws=MIS), ALIGN)])
 def test_norm_bwd(kw, status):
-    a = dict(dict(dY=A, dt=F16, lddy=10, X=A, xdt=F16, xe=A, ldx=10, M=3, K=10, gamma=A, pdt=F32, mean=A, rstd=A, dX=A, lddx=10, dg=A, db=A,
+    a = dict(dict(dY=A, dt=F16, lddy=10, X=A, xdt=F16, xe=A, ldx=10, M=30, K=10, gamma=A, pdt=F32, mean=A, rstd=A, dX=A, lddx=10, dg=A, db=A,
                   ws=A, short=0), **kw)
     try:
         need = slim.slim_norm_bwd_workspace(a["M"], a["K"])
