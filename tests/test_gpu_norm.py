@@ -180,6 +180,21 @@ def test_backward(m, k, dtype, rms, q8):
     check_backward(f64(dy), xv, f64(g), mean, rstd, rms, dx, dg, db, U[dtype])
 
 
+@pytest.mark.parametrize("m,k", [(600, 5001), (300, 8191), (5, 12287), (300, 16383), (3, 28671)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("q8", [False, True])
+def test_rows_that_end_inside_a_vector(m, k, dtype, q8):
+    print(f"norm and norm_bwd m={m} k={k} {dtype} q8={q8}", flush=True)
+    t, g, b = inputs(m, k, dtype, "fp32", seed=9)
+    y, mean, rstd = slim.norm(t.cuda(), g.cuda(), b.cuda())
+    check_forward(t, g, b, False, f64(y), mean, rstd, U[dtype])
+    dy = torch.from_numpy(synth.stream(10, f"norm/dy/{m}x{k}").standard_normal((m, k)).astype(np.float32)).to(DT[dtype])
+    x = slim.quant8(t.cuda()) if q8 else t.cuda()
+    xv = act8.values_rows(host(x["codes"]), host(x["exps"]), k) if q8 else f64(t)
+    dx, dg, db = slim.norm_bwd(dy.cuda(), x, g.cuda(), mean, rstd)
+    check_backward(f64(dy), xv, f64(g), mean, rstd, False, dx, dg, db, U[dtype])
+
+
 @pytest.mark.parametrize("rms", [False, True])
 def test_backward_against_differences(rms):
     # the kernel's gradients against differences of the 64-bit forward
