@@ -749,16 +749,23 @@ def _float_code(dt) -> int:
     return code
 
 
-def _stream_on(dev: int, stream):
-    """The hipStream_t of `stream`, or of device `dev`'s current stream."""
+def _stream_on(dev: int):
+    """The hipStream_t of device `dev`'s current stream."""
     global _raw_stream
-    if stream is not None:
-        return stream.cuda_stream
     if _raw_stream is None:
         torch = _torch()
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda d: torch.cuda.current_stream(d).cuda_stream)
     return _raw_stream(dev)
+
+
+def _on_its_stream(stream, call, X, *args):
+    """call(X, *args) with `stream` as the current one, so that what the call allocates belongs to the stream that uses it."""
+    t = X["codes"] if type(X) is dict else X
+    if stream.device.index != t.get_device():
+        raise ValueError("the stream must be of the tensors' device")
+    with _torch().cuda.stream(stream):
+        return call(X, *args)
 
 
 def _matrix(t, what: str):
@@ -814,6 +821,8 @@ def _empty_rows8(M: int, K: int, like) -> dict:
 def quant8(X, out: dict | None = None, stream=None) -> dict:
     """slim_quant8 of X [M, K] (fp16, bf16 or fp32; rows of any stride): {"codes" uint8 [M, K up to 128],
     "exps" uint8, "M", "K"}."""
+    if stream is not None:
+        return _on_its_stream(stream, quant8, X, out)
     M, K, ldx, dev = _matrix(X, "X")
     if out is None:
         out = _empty_rows8(M, K, X)
@@ -822,7 +831,7 @@ def quant8(X, out: dict | None = None, stream=None) -> dict:
         if (out["M"], out["K"]) != (M, K):
             raise ValueError("out is of another shape")
     st = lib().slim_quant8(X.data_ptr(), _float_code(X.dtype), M, K, ldx, out["codes"].data_ptr(), out["exps"].data_ptr(),
-                           _stream_on(dev, stream))
+                           _stream_on(dev))
     if st:
         raise SlimError(st, "slim_quant8")
     return out
@@ -830,6 +839,8 @@ def quant8(X, out: dict | None = None, stream=None) -> dict:
 
 def dequant8(q: dict, dtype=None, out=None, stream=None):
     """slim_dequant8: the values of 8-bit rows as [M, K] of `dtype` (bf16 if neither it nor `out` is given)."""
+    if stream is not None:
+        return _on_its_stream(stream, dequant8, q, dtype, out)
     codes, exps, M, K, dev = _rows8(q)
     if dtype is None:
         dtype = out.dtype if out is not None else _torch().bfloat16
@@ -838,7 +849,7 @@ def dequant8(q: dict, dtype=None, out=None, stream=None):
         out, ldy = codes.new_empty((M, K), dtype=dtype), K
     else:
         ldy = _matrix_out(out, M, K, dtype, dev)
-    st = lib().slim_dequant8(codes.data_ptr(), exps.data_ptr(), M, K, out.data_ptr(), code, ldy, _stream_on(dev, stream))
+    st = lib().slim_dequant8(codes.data_ptr(), exps.data_ptr(), M, K, out.data_ptr(), code, ldy, _stream_on(dev))
     if st:
         raise SlimError(st, "slim_dequant8")
     return out
@@ -847,6 +858,8 @@ def dequant8(q: dict, dtype=None, out=None, stream=None):
 def pack8(W, bwd: bool = False, stream=None) -> dict:
     """slim_pack8 of W [N, K] (fp16, bf16 or fp32): {"codes", "exps", "N", "K"}, with `bwd` also the input gradient's
     {"codesT", "expsT"}."""
+    if stream is not None:
+        return _on_its_stream(stream, pack8, W, bwd)
     torch = _torch()
     N, K, ldw, dev = _matrix(W, "W")
     up = lambda a, b: -(-a // b)
@@ -860,7 +873,7 @@ def pack8(W, bwd: bool = False, stream=None) -> dict:
     if bwd:
         out["codesT"], out["expsT"] = empty(K, N)
     _check(slim_pack8(W.data_ptr(), _float_code(W.dtype), N, K, ldw, _ptr(out["codes"]), _ptr(out["exps"]),
-                      _ptr(out.get("codesT")), _ptr(out.get("expsT")), _stream_on(dev, stream)), "slim_pack8")
+                      _ptr(out.get("codesT")), _ptr(out.get("expsT")), _stream_on(dev)), "slim_pack8")
     return out
 
 
@@ -886,7 +899,7 @@ def _given8(nbytes: int, ws, like, stream: int):
     return ws.data_ptr(), ws.numel()
 
 
-def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, stream, where: str):
+def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, where: str):
     if codes.shape != ((N + 15) // 16, (K + 127) // 128, 2, 4, 16, 16) or exps.shape != ((N + 127) // 128, (K + 511) // 512 * 4):
         raise ValueError("codes and exponents do not have the shape of the 8-bit weight")
     _on_gpu(codes, exps)
@@ -908,7 +921,7 @@ def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, stream, where: str
         out, ldy = x.new_empty((M, N), dtype=dtype), N
     else:
         ldy = _matrix_out(out, M, N, dtype, dev)
-    L, st = lib(), _stream_on(dev, stream)
+    L, st = lib(), _stream_on(dev)
     need = ctypes.c_size_t()
     rc = L.slim_linear8_workspace(xdt, M, N, K, need)
     if not rc:
@@ -923,17 +936,23 @@ def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, stream, where: str
 def linear8(X, p: dict, dtype=None, out=None, ws=None, stream=None):
     """slim_linear8: Y [M, N] = X W^T with an 8-bit weight (pack8). X [M, K]: 8-bit rows (quant8, norm) or an fp16, bf16
     or fp32 tensor, which the call turns into 8 bits. Y in `dtype`, fp16 or bf16 (default: fp16 for fp16 X, else bf16)."""
-    return _product8(X, p["codes"], p["exps"], p["N"], p["K"], dtype, out, ws, stream, "slim_linear8")
+    if stream is not None:
+        return _on_its_stream(stream, linear8, X, p, dtype, out, ws)
+    return _product8(X, p["codes"], p["exps"], p["N"], p["K"], dtype, out, ws, "slim_linear8")
 
 
 def bwd_dx8(dY, p: dict, dtype=None, out=None, ws=None, stream=None):
     """slim_linear8 on the transposed pack: dX [M, K] = dY W for dY [M, N] (pack8 with bwd=True); types as linear8."""
-    return _product8(dY, p["codesT"], p["expsT"], p["K"], p["N"], dtype, out, ws, stream, "slim_linear8")
+    if stream is not None:
+        return _on_its_stream(stream, bwd_dx8, dY, p, dtype, out, ws)
+    return _product8(dY, p["codesT"], p["expsT"], p["K"], p["N"], dtype, out, ws, "slim_linear8")
 
 
 def grad_w8(dY, q: dict, p: dict | None = None, out=None, ws=None, stream=None):
     """slim_grad_w8: dY^T X for dY [M, N] (fp16, bf16) and X [M, K] in 8 bits: fp32 [N, K], or with a value pack `p`
     (pack16) fp32 [N, K/2] at the positions it keeps."""
+    if stream is not None:
+        return _on_its_stream(stream, grad_w8, dY, q, p, out, ws)
     m, N, ldy, dev = _matrix(dY, "dY")
     xc, xe, M, K, _ = _rows8(q, dev)
     if m != M:
@@ -952,7 +971,7 @@ def grad_w8(dY, q: dict, p: dict | None = None, out=None, ws=None, stream=None):
     else:
         _on_gpu(out)
         _matrix_out(out, N, cols, _torch().float32, dev)
-    y, L, st = dY.data_ptr(), lib(), _stream_on(dev, stream)
+    y, L, st = dY.data_ptr(), lib(), _stream_on(dev)
     aligned = 1 if y % 16 == 0 and ldy % 8 == 0 and ldy < 1 << 22 else 0
     need = ctypes.c_size_t()
     rc = L.slim_grad_w8_workspace(M, N, K, 0 if p is None else 1, aligned, need)
@@ -967,6 +986,8 @@ def grad_w8(dY, q: dict, p: dict | None = None, out=None, ws=None, stream=None):
 def norm(X, gamma=None, beta=None, eps: float = 1e-5, rms: bool = False, q8: bool = False, out=None, stream=None):
     """slim_norm over the rows of X [M, K] (fp16, bf16 or fp32): layer norm, or with `rms` the RMS norm. Returns (Y, mean,
     rstd): Y of X's type, or with `q8` 8-bit rows (as quant8); mean and rstd fp32 [M] for norm_bwd, mean None with `rms`."""
+    if stream is not None:
+        return _on_its_stream(stream, norm, X, gamma, beta, eps, rms, q8, out)
     M, K, ldx, dev = _matrix(X, "X")
     dt = _float_code(X.dtype)
     pdt, gp, bp = SLIM_F32, None, None
@@ -996,7 +1017,7 @@ def norm(X, gamma=None, beta=None, eps: float = 1e-5, rms: bool = False, q8: boo
             ldy = _matrix_out(out, M, K, X.dtype, dev)
         yp, ye, ydt = out.data_ptr(), None, dt
     rc = lib().slim_norm(X.data_ptr(), dt, M, K, ldx, gp, bp, pdt, 1 if rms else 0, eps, yp, ydt, ldy, ye,
-                         None if rms else mean.data_ptr(), rstd.data_ptr(), _stream_on(dev, stream))
+                         None if rms else mean.data_ptr(), rstd.data_ptr(), _stream_on(dev))
     if rc:
         raise SlimError(rc, "slim_norm")
     return out, mean, rstd
@@ -1006,6 +1027,8 @@ def norm_bwd(dY, X, gamma, mean, rstd, out=None, ws=None, stream=None):
     """slim_norm_bwd: (dX, dgamma, dbeta) from dY [M, K], the forward's input X (dY's type, or its 8-bit checkpoint from
     quant8), gamma (or None) and the forward's mean and rstd; mean None: RMS norm, dbeta None. dX of dY's type, dgamma
     and dbeta fp32."""
+    if stream is not None:
+        return _on_its_stream(stream, norm_bwd, dY, X, gamma, mean, rstd, out, ws)
     M, K, lddy, dev = _matrix(dY, "dY")
     dt, pdt, gp, mp = _float_code(dY.dtype), SLIM_F32, None, None
     if type(X) is dict:
@@ -1034,7 +1057,7 @@ def norm_bwd(dY, X, gamma, mean, rstd, out=None, ws=None, stream=None):
         lddx = _matrix_out(out, M, K, dY.dtype, dev)
     dgamma = dY.new_empty((K,), dtype=f32)
     dbeta = None if mean is None else dY.new_empty((K,), dtype=f32)
-    L, st = lib(), _stream_on(dev, stream)
+    L, st = lib(), _stream_on(dev)
     need = ctypes.c_size_t()
     rc = L.slim_norm_bwd_workspace(M, K, need)
     if not rc:
