@@ -56,9 +56,9 @@ SLIM_DEV void store_grad4(float* gW, bool masked, uint32_t byte, int64_t n, int6
   }
 }
 
-// COUNT rows n, n + step, ... of a tile kept in LDS as [n][k] (32 16-byte slots a row, XOR-swizzled by the row), positions
+// COUNT rows n, n + step, ... of a tile kept in LDS as [n][k] (SLOTS 16-byte slots a row, XOR-swizzled by the row), positions
 // k .. k + 3 of each by this lane: the pattern's bytes first, so that their loads are in flight together.
-template <int COUNT>
+template <int COUNT, int SLOTS>
 SLIM_DEV void store_rows(float* gW, const uint8_t* meta, const f4_t* tile, int row, int step, int64_t n0, int64_t N, int slot, int64_t k,
                          int64_t K) {
   if (k >= K) return;
@@ -72,56 +72,61 @@ SLIM_DEV void store_rows(float* gW, const uint8_t* meta, const f4_t* tile, int r
 #pragma unroll
   for (int j = 0; j < COUNT; ++j) {
     const int i = row + j * step;
-    if (n0 + i < N) store_grad4(gW, meta != nullptr, byte[j], n0 + i, k, K, tile[i * 32 + (slot ^ (i & 31))]);
+    if (n0 + i < N) store_grad4(gW, meta != nullptr, byte[j], n0 + i, k, K, tile[i * SLOTS + (slot ^ (i & (SLOTS - 1)))]);
   }
 }
 
 // ------------------------------------------------------------------------------------- small layers
-// 128 (k) x 128 (n) tiles over a slice of the rows, eight waves in two groups: of each chunk of 64 rows group g takes the 32
-// from 32 g on, as 2 x 2 waves of 64 x 64, and group 1's sums go through LDS to group 0 at the end. Both operands go through
-// registers, where X is widened (and dY's rows may start anywhere), into two LDS slots; registers are loaded three chunks
-// ahead, since a lone chunk takes less than a load's time to come (more would cost the second block on a CU). One barrier a chunk. A split launch writes its sums as one
-// array a slice, which k_wgrad8_sum adds in slice order.
+// TK (k) x 128 (n) tiles over a slice of the rows, eight waves in groups of TK / 32 that each hold the whole tile, 64 x 64 a
+// wave: of each chunk of 64 rows a group takes its share (32 or 16), and the groups' sums are added through LDS at the end, in
+// a fixed order. Both operands go through registers, where X is widened (and dY's rows may start anywhere), into two LDS slots;
+// registers are loaded two chunks ahead of the slots. One barrier a chunk. A split launch writes its sums as one array a
+// slice, which k_wgrad8_sum adds in slice order.
+// TK 128: two blocks a CU hide each other's LDS and barriers. TK 64: for layers of so few tiles that a block stands alone
+// on its CU anyway, where reads, products and writes of a chunk follow one another: half of each, on twice the CUs.
 template <int DT, int HI>
 SLIM_DEV uint32_t widen2(uint32_t c, float s);
 
-template <int DT>
+template <int DT, int TK>
 __global__ void __launch_bounds__(512, 4)
 k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xe,
          int64_t M, int64_t N, int64_t K, const uint8_t* __restrict__ meta, float* __restrict__ gW, int64_t slice, int64_t slice_out) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int kRows = 2 * kWM, kAhead = 2;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kRows * 256];      // X slots, dY slots; at the end group 1's sums
+  constexpr int kRows = 2 * kWM, kAhead = 2, kGroups = 256 / TK, kSteps = 4 / kGroups, kSlots = TK / 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kRows * 256];      // X slots, dY slots; at the end the sums
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t Kp = q8_row(K), Ge = q8_exp_row(K);
-  const uint32_t tk = (uint32_t)(Kp / 128), nt = blockIdx.x / tk;
+  const uint32_t tk = (uint32_t)((K + TK - 1) / TK), nt = blockIdx.x / tk;
   const int64_t n0 = (int64_t)__builtin_amdgcn_readfirstlane((int)nt) * 128;
-  const int64_t k0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x - nt * tk)) * 128;
+  const int64_t k0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x - nt * tk)) * TK;
   const int64_t mb = blockIdx.y * slice, me = mb + slice < M ? mb + slice : M;
   gW += blockIdx.y * slice_out;
-  // staging: row tid / 8 of the chunk, columns 16 (tid % 8) .. + 15
-  const int row = tid >> 3, col = 16 * (tid & 7);
+  // staging: row tid / 8 of the chunk, columns 16 (tid % 8) .. + 15 of dY, TK / 8 (tid % 8) .. of X
+  const int row = tid >> 3, col = 16 * (tid & 7), xcol = TK / 8 * (tid & 7);
   const int nleft = (int)(cols - n0 - col < 16 ? cols - n0 - col : 16);     // cols: readable columns of dY, at least 16
   struct Stage {
-    u32x4_t y0, y1, c;
+    u32x4_t y0, y1;
+    std::conditional_t<TK == 128, u32x4_t, u32x2_t> c;
     uint32_t e;
   };
   // the next chunk's row of this thread: rows are loaded in order
   int left = (int)(me - mb) - row, to_last = (int)(M - 1 - mb) - row;
-  const uint16_t* py = dY + (mb + row) * lddy + n0 + col;
+  int64_t at = (mb + row) * lddy + n0 + col;
   // X by resources that move on with the chunk and end with the slice: rows past it read as zero
-  const uint32_t xo = (uint32_t)row * (uint32_t)Kp + (uint32_t)(k0 + col), eo = (uint32_t)row * (uint32_t)Ge + (uint32_t)(k0 / 128);
+  const uint32_t xo = (uint32_t)row * (uint32_t)Kp + (uint32_t)(k0 + xcol), eo = (uint32_t)row * (uint32_t)Ge + (uint32_t)(k0 / 128);
   int64_t xm = mb;
   auto load = [&](Stage& S) {
     S.y0 = S.y1 = u32x4_t{0, 0, 0, 0};
-    S.c = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(xc + xm * Kp, (me - xm) * Kp), xo, 0, 0);
+    const rsrc_t rx = make_rsrc(xc + xm * Kp, (me - xm) * Kp);
+    if constexpr (TK == 128) S.c = __builtin_amdgcn_raw_buffer_load_b128(rx, xo, 0, 0);
+    else S.c = __builtin_amdgcn_raw_buffer_load_b64(rx, xo, 0, 0);
     S.e = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(xe + xm * Ge, (me - xm) * Ge), eo, 0, 0);
     xm += kRows;
     if (left > 0 && nleft > 0) {
       // past N the next row's values do no harm (results there are not stored); the last row's last piece is taken 16 values
       // from its end (N >= 16) and moved into place
       const int past = to_last == 0 ? 16 - nleft : 0;
-      const uint16_t* p = py - past;
+      const uint16_t* p = dY + (at - past);
       __builtin_memcpy(&S.y0, p, 16);
       __builtin_memcpy(&S.y1, p + 8, 16);
       if (past) {
@@ -137,18 +142,19 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     }
     left -= kRows;
     to_last -= kRows;
-    py += kRows * lddy;
-    asm volatile("" : "+v"(py));       // one pointer, not one for each chunk of a round
+    at += kRows * lddy;
+    asm volatile("" : "+v"(at));       // one offset, not one for each chunk of a round (and no pointer, whose loads would be generic)
   };
-  uint8_t* const lx = lds + lds_at(row, col);
+  uint8_t* const lx = lds + lds_at(row, xcol);
+  uint8_t* const ly = lds + 2 * (kRows * 256) + lds_at(row, col);
   auto put = [&](const Stage& S, int z) {
     uint8_t* x = lx + z * (kRows * 256);
-    uint8_t* y = x + 2 * (kRows * 256);
+    uint8_t* y = ly + z * (kRows * 256);
     *reinterpret_cast<u32x4_t*>(y) = S.y0;
     *reinterpret_cast<u32x4_t*>(y + 16) = S.y1;
     const float s = q8_pow2(S.e);
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < TK / 64; ++h)
       *reinterpret_cast<u32x4_t*>(x + 16 * h) = u32x4_t{widen2<DT, 0>(S.c[2 * h], s), widen2<DT, 1>(S.c[2 * h], s),
                                                         widen2<DT, 0>(S.c[2 * h + 1], s), widen2<DT, 1>(S.c[2 * h + 1], s)};
   };
@@ -157,8 +163,9 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[i >> 1][i & 1][e] = 0.f;
-  const int G = lane >> 4, q = lane & 15, grp = wave >> 2, wk = 64 * (wave & 1), wn = 64 * ((wave >> 1) & 1);
-  const int rr = 32 * grp + 8 * (G >> 1) + (q >> 2), cr = 16 * (G & 1) + 4 * (q & 3);
+  const int G = lane >> 4, q = lane & 15, grp = wave / (TK / 32);
+  const int wk = TK == 128 ? 64 * (wave & 1) : 0, wn = 64 * ((TK == 128 ? wave >> 1 : wave) & 1);
+  const int rr = 16 * kSteps * grp + 8 * (G >> 1) + (q >> 2), cr = 16 * (G & 1) + 4 * (q & 3);
   const uint8_t* ax[2] = {lds + lds_at(rr, wk + cr), lds + lds_at(rr, wk + 32 + cr)};
   const uint8_t* by[2] = {lds + 2 * (kRows * 256) + lds_at(rr, wn + cr), lds + 2 * (kRows * 256) + lds_at(rr, wn + 32 + cr)};
   Stage S[kAhead];
@@ -174,7 +181,7 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     put(S[(j + 1) % kAhead], z ^ 1);
     load(S[(j + 1) % kAhead]);
 #pragma unroll
-    for (int st = 0; st < 2; ++st) {
+    for (int st = 0; st < kSteps; ++st) {
       __builtin_amdgcn_sched_barrier(0);        // one step's operands at a time: 128 registers for two blocks a CU
       u32x2_t a[2][2], b[2][2];
 #pragma unroll
@@ -199,28 +206,28 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     chunk(std::integral_constant<int, 0>{});
     chunk(std::integral_constant<int, 1>{});
   }
-  // The tile as [n][k] in LDS (512 bytes a row, 16-byte slots XOR-swizzled by n): group 1's sums, then both groups', which
-  // leave in whole rows.
+  // The tile as [n][k] in LDS (16-byte slots XOR-swizzled by n): the groups' sums, last group first, which leave in whole
+  // rows.
   __syncthreads();
   f4_t* const tile = reinterpret_cast<f4_t*>(lds);
   const int nl = wn + (lane & 31), sl = wk / 4 + (lane >> 5);
 #pragma unroll
-  for (int g = 1; g >= 0; --g) {
+  for (int g = kGroups - 1; g >= 0; --g) {
     if (grp == g) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const f16_t& c = acc[i >> 3][(i >> 2) & 1];
-        f4_t& t = tile[(nl + 32 * ((i >> 2) & 1)) * 32 + ((sl + 8 * (i >> 3) + 2 * (i & 3)) ^ (nl & 31))];
+        f4_t& t = tile[(nl + 32 * ((i >> 2) & 1)) * kSlots + ((sl + 8 * (i >> 3) + 2 * (i & 3)) ^ (nl & (kSlots - 1)))];
         const f4_t v = {c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
-        if (g == 1) t = v;
+        if (g == kGroups - 1) t = v;
         else t += v;
       }
     }
     __syncthreads();
   }
-  const int slot = tid & 31;
+  const int slot = tid & (kSlots - 1);
   const int64_t k = k0 + 4 * slot;
-  store_rows<8>(gW, meta, tile, tid >> 5, 16, n0, N, slot, k, K);
+  store_rows<TK / 16, kSlots>(gW, meta, tile, tid / kSlots, 512 / kSlots, n0, N, slot, k, K);
 #endif
 }
 
@@ -509,7 +516,7 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
     }
     // (in a loop: written out, the stores of partial groups are more instructions than the products)
 #pragma unroll 1
-    for (int i = lane >> 5; i < 64; i += 16) store_rows<8>(gW, meta, mine, i, 2, n0 + wn + 64 * y2, N, slot, k, K);
+    for (int i = lane >> 5; i < 64; i += 16) store_rows<8, 32>(gW, meta, mine, i, 2, n0 + wn + 64 * y2, N, slot, k, K);
   }
 #endif
 }
@@ -517,7 +524,7 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
 // How a gradient is computed: 256 x 256 tiles (dY's rows aligned, if need be in a copy of them), or 128 x 128 tiles over
 // `slices` slices of the rows.
 struct GradPlan {
-  bool wide, copy;
+  bool wide, copy, narrow;
   int64_t slices, slice, slice_out;
   size_t off_part, bytes;   // workspace: the copied rows, the slices' sums from off_part on
 };
@@ -543,6 +550,10 @@ GradPlan grad_plan(int64_t M, int64_t N, int64_t K, bool masked, bool aligned) {
   p.slices = std::max<int64_t>(1, std::min(256 / tiles, M / 512));
   p.slice = cdiv(cdiv(M, p.slices), 2 * kWM) * 2 * kWM;
   p.slices = std::max<int64_t>(1, cdiv(M, std::max<int64_t>(p.slice, 1)));
+  // half as wide tiles on twice the CUs where the others would leave half of them idle (999 x 2051 x 768 14.4 us against 16.9,
+  // 8192 x 256 x 256 in 16 slices 16.3 against 18.3; with every CU taken already 2048 x 2048 x 2048 34.0 against 31.0), but not
+  // over few rows, where the more groups' sums cost more than that saves (100 x 300 x 300 8.5 against 6.8)
+  p.narrow = tiles * p.slices <= 128 && M >= 512;
   p.slice_out = cdiv(N * (masked ? K / 2 : K), 64) * 64;
   p.off_part = p.bytes;
   if (p.slices > 1) p.bytes += (size_t)p.slices * (size_t)p.slice_out * 4;
@@ -575,11 +586,12 @@ int grad(const GradPlan& p, const uint16_t* dY, int64_t lddy, const uint8_t* xc,
                 M, N, K, meta, gW);
     return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
   }
-  const dim3 grid((unsigned)(cdiv(N, 128) * cdiv(K, 128)), (unsigned)p.slices);
+  const dim3 grid((unsigned)(cdiv(N, 128) * cdiv(K, p.narrow ? 64 : 128)), (unsigned)p.slices);
   float* out = p.slices > 1 ? reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + p.off_part) : gW;
   {
     SlimKernelTimer timer("grad_w8", s);
-    SLIM_LAUNCH(timer, (k_wgrad8<DT>), grid, dim3(512), s, dY, lddy, cols, xc, xe, M, N, K, meta, out, p.slice, p.slice_out);
+    if (p.narrow) SLIM_LAUNCH(timer, (k_wgrad8<DT, 64>), grid, dim3(512), s, dY, lddy, cols, xc, xe, M, N, K, meta, out, p.slice, p.slice_out);
+    else SLIM_LAUNCH(timer, (k_wgrad8<DT, 128>), grid, dim3(512), s, dY, lddy, cols, xc, xe, M, N, K, meta, out, p.slice, p.slice_out);
   }
   if (p.slices > 1) {
     const int64_t count = N * (meta ? K / 2 : K);

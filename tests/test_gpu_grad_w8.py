@@ -94,6 +94,31 @@ def test_large_layer_of_no_rows():
     assert g.shape == (8200, 1024) and bool((g == 0).all())
 
 
+# 128 x 128 tiles that fill the chip, over one slice of the rows and over three; then at least 256 tiles of 256 x 256, and at
+# least 128 of them over more rows
+MANY = [(520, 2000, 1040), (513, 2051, 1030), (3000, 1000, 1040), (2999, 1003, 1041),
+        (193, 4100, 4090), (200, 8192, 2048), (255, 4097, 4112), (1537, 2301, 3888)]
+
+
+@pytest.mark.parametrize("m,n,k", MANY)
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_many_tiles(m, n, k, dtype):
+    print(f"grad_w8 many tiles m={m} n={n} k={k} {dtype}", flush=True)
+    dy, x = inputs(m, n, k, dtype, seed=11)
+    q = slim.quant8(x.cuda())
+    xv = act8.values_rows(*act8.quant_rows(x.double().numpy()), k)
+    got = slim.grad_w8(dy.cuda(), q)
+    check(got, dy.double().numpy(), xv)
+    if k % 16 == 0:
+        p, pick = kept(n, k)
+        assert np.array_equal(host(slim.grad_w8(dy.cuda(), q, p)), pick(host(got)))
+    # rows that are aligned, as part of wider ones that NaN fills, and rows that start anywhere: the same bits
+    for start, width in ((8, n + 24 - n % 8), (3, n + 7)):
+        buf = torch.full((m, width), float("nan"), dtype=DT[dtype], device="cuda")
+        buf[:, start:start + n] = dy.cuda()
+        assert torch.equal(slim.grad_w8(buf[:, start:start + n], q), got), start
+
+
 @pytest.mark.parametrize("n", [1, 7, 15, 16, 17, 130])
 def test_narrow_layers_over_many_rows(n):
     # slices of the rows, joined; rows shorter than a load
