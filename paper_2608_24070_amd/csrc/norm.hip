@@ -10,6 +10,7 @@
 // the present one. All arithmetic is fp32; y and dx are rounded once. Sums have a fixed order, so results repeat bit for
 // bit. Bound by HBM.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 
 #include "slim_launch.h"
 #include "slim_q8.h"
@@ -489,8 +490,8 @@ k_norm_bwd(NormBwdArgs a) {
   }
 }
 
-// Longer rows, second kernel: dx, one block a row, which reads it twice: 2048 x 28672 in bf16 85 us after 49 us for the
-// column sums. Sums of such rows do not fit the registers beside the row itself.
+// Longer rows, second kernel: dx, one block a row, which reads it twice (400 x 65536 in bf16: 38.7 us). The column sums of
+// such rows do not fit the registers beside the row itself, and have a kernel of their own.
 template <int DT, int XT>
 __global__ void __launch_bounds__(1024)
 k_norm_bwd_long(NormBwdArgs a) {
@@ -522,6 +523,52 @@ k_norm_bwd_long(NormBwdArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-mx, (h[e] - mu) * rstd, fmaf(d[e], g[e], -mt));
     store_row8<DT, true>(a.dx, nullptr, row, a.lddx, col, a.K, d);
+  }
+}
+
+// The same for whole vectors and rows of up to 32768: the row stays in registers between its sums and its result. 2048 x 28672
+// in bf16 72 us (read twice: 80), 4.9 TB/s, after 43 for the column sums; 3221 x 20832 in fp32 165 us (196).
+template <int DT, int XT>
+__global__ void __launch_bounds__(1024)
+k_norm_bwd_dx(NormBwdArgs a) {
+  constexpr int V = 4;
+  __shared__ f2_t part[2][16];
+  const int64_t row = blockIdx.x;
+  const float rstd = a.rstd[row], shift = a.mean ? -a.mean[row] * rstd : 0.f;
+  Raw8<DT> y[V];
+  Raw8<XT> x[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int64_t col = (int64_t)(v * 1024 + threadIdx.x) * 8;
+    y[v] = load_raw8<DT, false>(a.dy, row, col, a.K);
+    x[v] = load_raw8<XT, false>(a.x, row, col, a.K);
+  }
+  float st = 0.f, sx = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    float d[8], h[8], g[8];
+    params8<false>(a.gamma, a.pdt, (int64_t)(v * 1024 + threadIdx.x) * 8, a.K, 1.f, g);
+    values8<DT>(y[v], d);
+    xhat8<XT>(x[v], rstd, shift, h);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float tt = d[e] * g[e];
+      st += tt;
+      sx = fmaf(tt, h[e], sx);
+    }
+  }
+  const f2_t sums = row_sums<1024>(st, sx, part, 0);
+  const float mt = a.mean ? sums[0] / (float)a.K : 0.f, mx = sums[1] / (float)a.K;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int64_t col = (int64_t)(v * 1024 + threadIdx.x) * 8;
+    float d[8], h[8], g[8];
+    params8<false>(a.gamma, a.pdt, col, a.K, 1.f, g);
+    values8<DT>(y[v], d);
+    xhat8<XT>(x[v], rstd, shift, h);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-mx, h[e], fmaf(d[e], g[e], -mt));
+    store_row8<DT, false>(a.dx, nullptr, row, a.lddx, col, a.K, d);
   }
 }
 
@@ -607,9 +654,10 @@ void norm_to(const NormArgs& a, int ydt, SlimKernelTimer& timer, hipStream_t s) 
 }
 
 // Blocks of the backward, each with a row of column sums that a second launch adds; up to four rounds of one block are
-// less than that launch takes.
+// less than that launch takes. Long rows: about 1024 blocks of column sums, 2048 columns wide (2048 x 28672 in bf16, sums and
+// their joining: 512 blocks 48 us, 1024 47, 2048 54, 4096 67).
 int64_t bwd_blocks(int64_t M, int64_t K) {
-  const int64_t units = K <= 1024 ? (M + 3) / 4 : M, most = K <= 4096 ? 768 : K <= 8192 ? 512 : 256;
+  const int64_t units = K <= 1024 ? (M + 3) / 4 : M, most = K <= 4096 ? 768 : K <= 8192 ? 512 : K <= 16384 ? 256 : std::max<int64_t>(1024 / ((K + 2047) / 2048), 1);
   return units <= 4 ? 1 : units < most ? units : most;
 }
 
@@ -627,7 +675,8 @@ void norm_bwd_rows_of(const NormBwdArgs& a, hipStream_t s) {
     // the column sums first: dX may be written over dY
     SLIM_LAUNCH(timer, (k_norm_bwd_long_cols<DT, XT>), dim3((unsigned)((a.K + 2047) / 2048), blocks), dim3(256), s, a);
     SlimKernelTimer timer2("norm_bwd_dx", s);
-    SLIM_LAUNCH(timer2, (k_norm_bwd_long<DT, XT>), dim3((unsigned)a.M), dim3(1024), s, a);
+    if (!RAG && a.K <= 32768) SLIM_LAUNCH(timer2, (k_norm_bwd_dx<DT, XT>), dim3((unsigned)a.M), dim3(1024), s, a);
+    else SLIM_LAUNCH(timer2, (k_norm_bwd_long<DT, XT>), dim3((unsigned)a.M), dim3(1024), s, a);
   }
 }
 
