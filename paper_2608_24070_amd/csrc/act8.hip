@@ -44,8 +44,27 @@ k_dequant8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ exps, 
   const uint32_t u = blockIdx.x * 32 + (threadIdx.x >> 3), sub = threadIdx.x & 7;
   if (u >= total) return;
   const uint32_t row = u / G, g = u - row * G, col = g * 128 + sub * 16;
-  const u32x4_t c = *reinterpret_cast<const u32x4_t*>(codes + ((int64_t)row * G + g) * 128 + sub * 16);
   const float s = q8_pow2(exps[(int64_t)row * ((G + 3) & ~3u) + g]);
+  if constexpr (DT == 2) {
+    // eight lanes write 128 bytes together, four times
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t at = 32 * e + 4 * sub;
+      float f[4];
+      q8_values4(*reinterpret_cast<const uint32_t*>(codes + ((int64_t)row * G + g) * 128 + at), s, f);
+      const int64_t k = g * 128 + at;
+      float* y = reinterpret_cast<float*>(Y) + (int64_t)row * ldy + k;
+      if (k + 4 <= K) {
+        __builtin_memcpy(y, f, 16);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (k + i < K) y[i] = f[i];
+      }
+    }
+    return;
+  }
+  const u32x4_t c = *reinterpret_cast<const u32x4_t*>(codes + ((int64_t)row * G + g) * 128 + sub * 16);
   float f[16];
 #pragma unroll
   for (int e = 0; e < 4; ++e) q8_values4(c[e], s, f + 4 * e);
