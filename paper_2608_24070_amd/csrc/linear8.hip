@@ -71,6 +71,7 @@ SLIM_DEV void quant16(const void* X, int64_t at, int64_t left, u32x4_t& c, uint3
 // and add their sums through LDS in wave order. Nothing is shared within the reduction, so weight tiles (2 KiB of
 // consecutive bytes) and X fragments go straight from memory to registers, U groups of a wave in flight at once. Bound by
 // the weight's bytes, and for more than a few rows by those of X, which every block reads: two tiles a block halve them.
+// 28672 x 8192: M 1 40.3 us (5.8 TB/s), M 16 47.4; 4096 x 4096, M 1 9.8 us, of which a launch is half.
 // XT: the type of X. 3 (codes): rows are read as they are. Otherwise every block first turns the whole of X into codes in
 // LDS, while its first weight tiles are on their way: worth it for the few rows whose codes fit kFewLds.
 constexpr int kFewLds = 32768;
@@ -186,16 +187,23 @@ SLIM_DEV void mfma8_in_place(f4_t& c, i32x8_t a, i32x8_t b, uint32_t sa, uint32_
 #endif
 }
 
-// Tiles of 16 FM rows of X by 256 columns, four waves of 64 columns each. A wave's weight tiles are its own: they go from
-// memory to registers in whole tiles, a group ahead. X is shared by the four waves: per group a [16 FM][128] slab goes to
-// LDS by direct loads (16 bytes a lane), three groups ahead in a ring of four, 16-byte slots XOR-swizzled by half the row:
-// LDS gives 16 lanes a cycle (256 bytes, two rows), and so the 16 rows of one q fall in distinct banks (by the whole row
-// they would meet in pairs: counted as half of all LDS cycles). Exponents of X go the same way, one 32-bit word (four
-// groups) a row; the unit picks the group's byte by itself. Fragments of X are read three ahead of their four MFMAs.
-// LDS reads are written out with counted waits (the compiler cannot tell the ring's slots apart and would wait for every
-// load in flight). Rows and weight tiles past the ends repeat the last one; their results are not stored.
+// What the 16-byte slots of LDS rows of 128 bytes are XORed by. A read of 16 bytes a lane takes lanes 0-3, 12-15 and 20-27 in
+// one cycle, 4-11, 16-19 and 28-31 in another, and lanes 32 on alike: with this every such sixteen falls in distinct banks
+// (conflicts are counted as 3 % of the LDS cycles; by the whole row they were half).
 SLIM_DEV int swizzle8(int row) { return ((row >> 1) & 7) ^ (((row >> 2) ^ (row >> 3)) & 1) * 2; }
 
+// Tiles of 16 FM rows of X by 64 WN columns, four waves of 16 FM x 64 each: WN side by side, and as many of those as are
+// left over 4 / WN parts of the reduction, whose sums are added in part order at the end. A wave's weight tiles are its own:
+// they go from memory to registers in whole tiles, three groups ahead. X is shared by the WN waves: per group a [16 FM][128]
+// slab goes to LDS by direct loads (16 bytes a lane), three groups ahead in a ring of four. Exponents of X go the same way, one
+// 32-bit word (four groups) a row; the unit picks the group's byte by itself. Fragments of X are read three ahead of their
+// four MFMAs. LDS reads are written out with counted waits (the compiler cannot tell the ring's slots apart and would wait for
+// every load in flight). Rows and weight tiles past the ends repeat the last one; their results are not stored.
+// 256 x 256 tiles are bound by the matrix unit and by the power it draws: 8192 x 28672 x 8192 1.31 ms, 2.9 PFLOP/s (a library
+// product of unscaled fp8 2.66): it is busy for 78 % of the cycles (8192 x 8192 x 8192) at the 1.6 GHz that the card then keeps,
+// LDS for 22 %. Shorter tiles and parts of the reduction are for fewer rows, where the weight's bytes come to count: 512 x
+// 28672 x 8192 94 us (2.6 PFLOP/s), 64 x 28672 x 8192 52 us (4.5 TB/s of weights), 45 x 13824 x 5120 19.9 us, 2048 x 4096 x 4096
+// 34 us (2.0).
 template <int FM, int WN, int DT>
 __global__ void __launch_bounds__(256, 1)
 k_linear8_tile(const uint8_t* __restrict__ X, const uint8_t* __restrict__ ex, const uint8_t* __restrict__ W,
