@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import threading
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libslim.so")
@@ -877,16 +878,19 @@ def pack8(W, bwd: bool = False, stream=None) -> dict:
     return out
 
 
-_ws8: dict = {}
+_ws8 = threading.local()
 
 
 def _workspace8(nbytes: int, like, stream: int):
-    """The 8-bit calls' workspace, kept per (device, stream). Its contents are of no interest between calls, so it is not
-    slim_linear's, whose counters have to stay zero."""
+    """The 8-bit calls' workspace, kept per thread, device and stream: a call's launches follow each other on the stream, but
+    another thread's may come between. Its contents are of no interest between calls, so it is not slim_linear's, whose
+    counters have to stay zero. (A captured call holds the workspace of its capture: where the graph is to run beside other
+    work of that stream, the call is given one of its own.)"""
+    cache = _ws8.__dict__
     key = (like.get_device(), stream)
-    ws = _ws8.get(key)
+    ws = cache.get(key)
     if ws is None or ws.numel() < nbytes:
-        ws = _ws8[key] = like.new_empty(max(nbytes, 1 << 16), dtype=_torch().uint8)
+        ws = cache[key] = like.new_empty(max(nbytes, 1 << 16), dtype=_torch().uint8)
     return ws
 
 

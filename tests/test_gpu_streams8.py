@@ -1,4 +1,6 @@
 """The 8-bit helpers on a stream that is given: what they allocate belongs to it, and it must be of the tensors' device."""
+import threading
+
 import pytest
 import torch
 
@@ -48,3 +50,22 @@ def test_results_belong_to_the_given_stream():
 def test_a_tensor_elsewhere_is_refused():
     with pytest.raises(ValueError, match="device"):
         slim.quant8(torch.zeros((2, 128)), stream=torch.cuda.Stream())
+
+
+def test_threads_on_one_stream_keep_apart():
+    # rows that are quantised into the workspace before the product: no thread may fill it between another's two launches
+    p = slim.pack8(torch.randn((256, 640), device="cuda"))
+    xs = [torch.randn((40, 640), device="cuda").bfloat16() for _ in range(4)]
+    want = [slim.linear8(x, p) for x in xs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        wrong.extend(j for j in range(200) if not torch.equal(slim.linear8(xs[i], p), want[i]))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
