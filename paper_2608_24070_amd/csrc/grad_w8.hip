@@ -57,22 +57,15 @@ SLIM_DEV void store_grad4(float* gW, bool masked, uint32_t byte, int64_t n, int6
 }
 
 // COUNT rows n, n + step, ... of a tile kept in LDS as [n][k] (SLOTS 16-byte slots a row, XOR-swizzled by the row), positions
-// k .. k + 3 of each by this lane: the pattern's bytes first, so that their loads are in flight together.
+// k .. k + 3 of each by this lane; `byte`: the pattern's byte for the positions 8 (k / 8) .. of each row.
 template <int COUNT, int SLOTS>
-SLIM_DEV void store_rows(float* gW, const uint8_t* meta, const f4_t* tile, int row, int step, int64_t n0, int64_t N, int slot, int64_t k,
-                         int64_t K) {
+SLIM_DEV void store_rows(float* gW, bool masked, const uint32_t (&byte)[COUNT], const f4_t* tile, int row, int step, int64_t n0, int64_t N,
+                         int slot, int64_t k, int64_t K) {
   if (k >= K) return;
-  uint32_t byte[COUNT];
-  if (meta)
-#pragma unroll
-    for (int j = 0; j < COUNT; ++j) {
-      const int64_t n = n0 + row + j * step;
-      byte[j] = meta[(n < N ? n : N - 1) * (K / 8) + k / 8];
-    }
 #pragma unroll
   for (int j = 0; j < COUNT; ++j) {
     const int i = row + j * step;
-    if (n0 + i < N) store_grad4(gW, meta != nullptr, byte[j], n0 + i, k, K, tile[i * SLOTS + (slot ^ (i & (SLOTS - 1)))]);
+    if (n0 + i < N) store_grad4(gW, masked, byte[j], n0 + i, k, K, tile[i * SLOTS + (slot ^ (i & (SLOTS - 1)))]);
   }
 }
 
@@ -207,6 +200,16 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     chunk(std::integral_constant<int, 0>{});
     chunk(std::integral_constant<int, 1>{});
   }
+  // what this thread stores, and the pattern's bytes for it, on their way while the sums are added
+  const int slot = tid & (kSlots - 1), r0 = tid / kSlots;
+  const int64_t k = k0 + 4 * slot;
+  uint32_t byte[TK / 16];
+  if (meta)
+#pragma unroll
+    for (int j = 0; j < TK / 16; ++j) {
+      const int64_t n = n0 + r0 + j * (512 / kSlots);
+      byte[j] = meta[(n < N ? n : N - 1) * (K / 8) + (k < K ? k : K - 1) / 8];
+    }
   // The tile as [n][k] in LDS (16-byte slots XOR-swizzled by n): the groups' sums, last group first, which leave in whole
   // rows.
   __syncthreads();
@@ -226,9 +229,7 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
     }
     __syncthreads();
   }
-  const int slot = tid & (kSlots - 1);
-  const int64_t k = k0 + 4 * slot;
-  store_rows<TK / 16, kSlots>(gW, meta, tile, tid / kSlots, 512 / kSlots, n0, N, slot, k, K);
+  store_rows<TK / 16, kSlots>(gW, meta != nullptr, byte, tile, r0, 512 / kSlots, n0, N, slot, k, K);
 #endif
 }
 
@@ -319,6 +320,7 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr uint32_t kSlot = kWM * 512, kY = 4 * kSlot;
   __shared__ __attribute__((aligned(16))) uint8_t lds[8 * kSlot];
+  __shared__ __attribute__((aligned(16))) uint8_t pattern[256][32];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wk = 128 * (wave & 1), wn = 128 * (wave >> 1);
   const uint32_t Kp = (uint32_t)q8_row(K), Ge = (uint32_t)q8_exp_row(K);
@@ -330,6 +332,18 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
   const int64_t n0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(band * 4 + q0 - kt * width)) * 256;
   const int64_t k0 = (int64_t)__builtin_amdgcn_readfirstlane((int)kt) * 256;
   const int nch = (int)((M + kWM - 1) / kWM);
+
+  // the pattern's bytes of one row of the tile a thread (past a row's end the next row's, which no result asks for)
+  u32x4_t pat[2] = {};
+  if (meta) {
+    const int64_t bytes = N * (K / 8), at = (n0 + tid < N ? n0 + tid : N - 1) * (K / 8) + k0 / 8;
+    if (at + 32 <= bytes) {
+      __builtin_memcpy(pat, meta + at, 32);
+    } else {
+#pragma unroll
+      for (int b = 0; b < 32; ++b) pat[b >> 4][(b >> 2) & 3] |= (uint32_t)(at + b < bytes ? meta[at + b] : 0) << (8 * (b & 3));
+    }
+  }
 
   // direct loads of dY: four pieces of 1 KiB (two rows) a wave; lane L writes LDS bytes 16 L of its piece, row L / 32,
   // physical slot L % 32, which holds logical slot (L % 32) ^ 4 (row % 4)
@@ -492,6 +506,7 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
   __builtin_amdgcn_sched_barrier(0);
   each<16>([&](auto ic) { read_i(A, ic, std::integral_constant<uint32_t, 0>{}); });
   landed(A);
+  asm volatile("" : "+v"(pat[0]), "+v"(pat[1]));          // loaded by now
   int c = 0;
   do {                  // at least once: no way around the loop, on which the sums would be moved
     if (c) rebase(c);
@@ -509,8 +524,11 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
   __builtin_amdgcn_sched_barrier(0);
   // the sums leave through LDS in whole rows, half of the wave's columns n at a time (see k_wgrad8)
   f4_t* const mine = reinterpret_cast<f4_t*>(lds) + wave * 2048;
+  *reinterpret_cast<u32x4_t*>(&pattern[tid][0]) = pat[0];
+  *reinterpret_cast<u32x4_t*>(&pattern[tid][16]) = pat[1];
   const int slot = lane & 31;
   const int64_t k = k0 + wk + 4 * slot;
+  const bool inside = n0 + 256 <= N && k0 + 256 <= K;
 #pragma unroll
   for (int y2 = 0; y2 < 2; ++y2) {
     __syncthreads();
@@ -520,9 +538,55 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
       mine[((lane & 31) + 32 * ((i >> 2) & 1)) * 32 + ((8 * (i >> 3) + 2 * (i & 3) + (lane >> 5)) ^ (lane & 31))] =
           f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
     }
+    // Inside the matrix a store takes a few instructions: with one wave on a SIMD they are what the end of a tile costs
+    // (rows of a step differ from the first's by a constant XOR and offset in LDS, by a uniform address in memory).
+    if (inside && !meta) {
+      const uint8_t* const t0 = reinterpret_cast<const uint8_t*>(mine);
+      const uint32_t at = (uint32_t)(lane >> 5) * 512u + (uint32_t)((slot ^ (lane >> 5)) * 16);
+      const uint32_t to = (uint32_t)(lane >> 5) * (uint32_t)K + 4u * slot;
+      float* g = gW + (n0 + wn + 64 * y2) * K + k0 + wk;
+#pragma unroll 1
+      for (int u = 0; u < 4; ++u) {
+        f4_t v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const f4_t*>(t0 + u * 8192 + j * 1024 + (at ^ (uint32_t)(((16 * u + 2 * j) & 31) * 16)));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) __builtin_memcpy(g + (16 * u + 2 * j) * K + to, &v[j], 16);
+      }
+      continue;
+    }
+    if (inside) {
+      // eight positions, four kept, a lane
+      const uint8_t* const t0 = reinterpret_cast<const uint8_t*>(mine);
+      const int r = lane >> 4, q = lane & 15;
+      const uint32_t at = (uint32_t)r * 512u + (uint32_t)(((2 * q) ^ r) * 16);
+      const uint32_t to = (uint32_t)r * (uint32_t)(K / 2) + 4u * q;
+      const uint8_t* const pb = &pattern[wn + 64 * y2 + r][wk / 8 + q];
+      float* g = gW + (n0 + wn + 64 * y2) * (K / 2) + (k0 + wk) / 2;
+#pragma unroll 1
+      for (int u = 0; u < 2; ++u) {
+        uint32_t b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = pb[u * 1024 + j * 128];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint8_t* const t1 = t0 + u * 16384 + j * 2048;
+          const uint32_t a0 = at ^ (uint32_t)(((4 * j) & 31) * 16), a1 = a0 ^ 16u;
+          const f4_t o = {*reinterpret_cast<const float*>(t1 + (a0 | (b[j] & 3u) * 4)), *reinterpret_cast<const float*>(t1 + (a0 | (b[j] & 12u))),
+                          *reinterpret_cast<const float*>(t1 + (a1 | ((b[j] >> 4) & 3u) * 4)), *reinterpret_cast<const float*>(t1 + (a1 | ((b[j] >> 4) & 12u)))};
+          *reinterpret_cast<f4_t*>(g + (32 * u + 4 * j) * (K / 2) + to) = o;
+        }
+      }
+      continue;
+    }
     // (in a loop: written out, the stores of partial groups are more instructions than the products)
 #pragma unroll 1
-    for (int i = lane >> 5; i < 64; i += 16) store_rows<8, 32>(gW, meta, mine, i, 2, n0 + wn + 64 * y2, N, slot, k, K);
+    for (int i = lane >> 5; i < 64; i += 16) {
+      uint32_t byte[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) byte[j] = pattern[wn + 64 * y2 + i + 2 * j][(wk + 4 * slot) / 8];
+      store_rows<8, 32>(gW, meta != nullptr, byte, mine, i, 2, n0 + wn + 64 * y2, N, slot, k, K);
+    }
   }
 #endif
 }
