@@ -207,7 +207,8 @@ SLIM_DEV int swizzle8(int row) { return ((row >> 1) & 7) ^ (((row >> 2) ^ (row >
 template <int FM, int WN, int DT>
 __global__ void __launch_bounds__(256, 1)
 k_linear8_tile(const uint8_t* __restrict__ X, const uint8_t* __restrict__ ex, const uint8_t* __restrict__ W,
-               const uint8_t* __restrict__ ew, int64_t M, int64_t N, int G, uint16_t* __restrict__ Y, int64_t ldy) {
+               const uint8_t* __restrict__ ew, int64_t M, int64_t N, int G, int fours, uint16_t* __restrict__ Y, int64_t ldy,
+               float* __restrict__ sums) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host compiler takes no part in the written-out instructions below
   constexpr int TM = 16 * FM, TN = 64 * WN, WK = 4 / WN;     // rows and columns of a tile; parts of the reduction
   // a group's barrier stands before fragment FB, since the next slab's fragments are read three ahead; a wave's P direct
@@ -341,8 +342,8 @@ k_linear8_tile(const uint8_t* __restrict__ X, const uint8_t* __restrict__ ex, co
   using I1 = std::integral_constant<int, 1>;
   using I2 = std::integral_constant<int, 2>;
   using I3 = std::integral_constant<int, 3>;
-  // this part's groups: the same number for each, in whole fours; the last part's end is past the last group
-  const int per = ((G + 3) / 4 + WK - 1) / WK * 4, g0 = part * per;
+  // this part's groups: the same number for each of the slice's `fours` times four; the last ones may be past the last group
+  const int per = fours / WK * 4, g0 = (int)blockIdx.y * fours * 4 + part * per;
   issue_e(g0 / 4);
   each<P>([&](auto pc) { issue_x(g0, I0{}, pc); });
   each<kAhead>([&](auto gc) { each<8>([&](auto ic) { load_w(wr[decltype(gc)::value], g0 + decltype(gc)::value, ic); }); });
@@ -429,10 +430,25 @@ k_linear8_tile(const uint8_t* __restrict__ X, const uint8_t* __restrict__ ex, co
       for (int k = 1; k < WK; ++k) v += all[(((k * WN + wi) * FM + f) * 4 + n) * 64 + el];
       const int row = 16 * f + er;
       const int64_t col = n0 + 64 * wi + 16 * n + 4 * eq;
-      if (row < rows && col < N) store4_16<DT>(Y, (m0 + row) * ldy + col, N - col, v);
+      if (row < rows && col < N) {
+        if (sums) *reinterpret_cast<f4_t*>(sums + ((int64_t)blockIdx.y * M + m0 + row) * ((N + 3) & ~3) + col) = v;
+        else store4_16<DT>(Y, (m0 + row) * ldy + col, N - col, v);
+      }
     }
   }
 #endif
+}
+
+// The slices' sums in slice order, four columns a thread, `quads` of them a row.
+template <int DT>
+__global__ void __launch_bounds__(256)
+k_linear8_sum(const f4_t* __restrict__ sums, int slices, uint32_t total, uint32_t quads, int64_t N, uint16_t* __restrict__ Y, int64_t ldy) {
+  const uint32_t u = blockIdx.x * 256 + threadIdx.x;
+  if (u >= total) return;
+  f4_t v = sums[u];
+  for (int i = 1; i < slices; ++i) v += sums[(int64_t)i * total + u];
+  const uint32_t row = u / quads, col = 4 * (u - row * quads);
+  store4_16<DT>(Y, (int64_t)row * ldy + col, N - col, v);
 }
 
 // ------------------------------------------------------------------------------------- host
@@ -450,19 +466,69 @@ struct TileKind {
 };
 constexpr TileKind kTiles[] = {{16, 4, 256, 10.7, 0.93, 1.48}, {12, 4, 256, 10.8, 0.70, 1.15}, {8, 4, 256, 10.1, 0.54, 0.90},
                                {8, 2, 256, 9.3, 0.57, 1.10},   {4, 2, 512, 8.2, 0.35, 1.33},   {4, 1, 256, 7.2, 0.57, 1.02}};
-double tile_time(const TileKind& k, int64_t M, int64_t N, int64_t G) {
-  const int64_t T = cdiv(M, 16 * k.fm) * cdiv(N, 64 * k.wn), steps = cdiv(cdiv(G, 4), 4 / k.wn) * 4;
+double tile_time(const TileKind& k, int64_t M, int64_t N, int64_t G, int slices) {
+  const int wk = 4 / k.wn;
+  const int64_t T = cdiv(M, 16 * k.fm) * cdiv(N, 64 * k.wn) * slices, steps = cdiv(cdiv(G, 4), wk * slices) * 4;
   const int64_t rounds = T / k.blocks, rest = T % k.blocks;
   const double t = rounds * k.full + (rest ? k.alone + (k.full - k.alone) * rest / k.blocks : 0);
-  return k.fixed + std::max(steps * t, (double)N * G * 128 / 6.0e6);
+  const double sum = slices > 1 ? 3.5 + 2.0 * slices * M * N * 4 / 4e6 : 0;
+  return k.fixed + std::max(steps * t, (double)N * G * 128 / 6.0e6) + sum;
+}
+
+// The kernel for a product: k_linear8_few with `few` fragments of rows, or tile kernel `kind` over slices of the reduction of
+// `fours` times four groups.
+struct Plan {
+  int few, kind, slices, fours;
+  size_t bytes;       // the slices' sums
+};
+Plan plan(int64_t M, int64_t N, int64_t K) {
+  const int64_t G = q8_row(K) / 128, F = cdiv(G, 4);
+  Plan p{0, 0, 1, 0, 0};
+  double best = 1e30;
+  for (int i = 0; i < 6; ++i) {
+    const TileKind& k = kTiles[i];
+    const int64_t T = cdiv(M, 16 * k.fm) * cdiv(N, 64 * k.wn);
+    // slices where the reduction is in parts already, as long as their blocks run at once
+    for (int s = 1; s == 1 || (k.wn < 4 && s * T <= k.blocks && s * (4 / k.wn) <= F && s <= 32); s += s < 4 ? 1 : s / 2) {
+      const double t = tile_time(k, M, N, G, s);
+      if (t < best) {
+        best = t;
+        p.kind = i;
+        p.slices = s;
+      }
+    }
+  }
+  // (64 x 1024 x 28672 in 16 slices 12 us and 3 for their sum, unsliced 73; 512 x 512 x 28672 27 against 40, 1024 x 1024 x 28672
+  // 43 against 60)
+  // The few kernel: the weight's bytes, for more rows X's too (two tiles and 32 rows read as many of X as of the weight, one
+  // and 64 four times as many), and not less than its 16 groups at a time take where few blocks share a long reduction.
+  const double w = (double)N * G * 128, turns = (double)cdiv(G, 16);
+  if (M <= 16 && std::max(4 + w * (1 + 0.013 * M) / 6.5e6, 4.5 + (0.75 + 0.035 * M) * turns) < best) p.few = 1;
+  else if (M > 16 && M <= 32 && std::max(7 + 2 * w / 8.6e6, 5 + 2.5 * turns) < best) p.few = 2;
+  else if (M > 32 && M <= 64 && std::max(6 + 5 * w / 6e6, 5 + 4.2 * turns) < best) p.few = 4;
+  const int wk = 4 / kTiles[p.kind].wn;
+  p.fours = (int)(cdiv(F, p.slices * wk) * wk);
+  p.slices = p.few ? 1 : (int)cdiv(F, p.fours);
+  if (p.slices > 1) p.bytes = (size_t)p.slices * (size_t)M * (size_t)((N + 3) & ~int64_t(3)) * 4;
+  return p;
 }
 
 template <int FM, int WN, int DT>
-void launch_tile(const uint8_t* X, const uint8_t* ex, const uint8_t* W, const uint8_t* ew, int64_t M, int64_t N, int64_t G,
-                 uint16_t* Y, int64_t ldy, hipStream_t s) {
+void launch_tile(const Plan& p, const uint8_t* X, const uint8_t* ex, const uint8_t* W, const uint8_t* ew, int64_t M, int64_t N,
+                 int64_t G, uint16_t* Y, int64_t ldy, float* ws, hipStream_t s) {
   const int64_t T = cdiv(M, 16 * FM) * cdiv(N, 64 * WN);
-  SlimKernelTimer timer("linear8_tile", s);
-  SLIM_LAUNCH(timer, (k_linear8_tile<FM, WN, DT>), dim3((unsigned)(8 * cdiv(T, 8))), dim3(256), s, X, ex, W, ew, M, N, (int)G, Y, ldy);
+  float* const sums = p.slices > 1 ? ws : nullptr;
+  {
+    SlimKernelTimer timer("linear8_tile", s);
+    SLIM_LAUNCH(timer, (k_linear8_tile<FM, WN, DT>), dim3((unsigned)(8 * cdiv(T, 8)), (unsigned)p.slices), dim3(256), s, X, ex, W, ew,
+                M, N, (int)G, p.fours, Y, ldy, sums);
+  }
+  if (sums) {
+    const int64_t quads = cdiv(N, 4), total = M * quads;
+    SlimKernelTimer timer("linear8_sum", s);
+    SLIM_LAUNCH(timer, k_linear8_sum<DT>, dim3((unsigned)cdiv(total, 256)), dim3(256), s, reinterpret_cast<const f4_t*>(sums), p.slices,
+                (uint32_t)total, (uint32_t)quads, N, Y, ldy);
+  }
 }
 
 // Blocks of up to 16 FM rows and NT weight tiles. Two tiles a block from 4096 columns on, where that leaves a block for
@@ -481,26 +547,21 @@ void launch_few(const void* X, const uint8_t* ex, int64_t ldx, const uint8_t* W,
   else launch_few_of<1, 1, XT, DT>(X, ex, ldx, W, ew, M, N, K, Y, ldy, s);
 }
 
-// X as codes. Up to 16 rows: k_linear8_few. Up to 64: it or a tile kernel, whichever is thought to take less (the few
-// kernel's blocks all read all of X: with two tiles and 32 rows as many bytes as of the weight, with one and 64 four times).
+// X as codes.
 template <int DT>
-void launch(const uint8_t* X, const uint8_t* ex, const uint8_t* W, const uint8_t* ew, int64_t M, int64_t N, int64_t K,
-            uint16_t* Y, int64_t ldy, hipStream_t s) {
+void launch(const Plan& p, const uint8_t* X, const uint8_t* ex, const uint8_t* W, const uint8_t* ew, int64_t M, int64_t N, int64_t K,
+            uint16_t* Y, int64_t ldy, float* ws, hipStream_t s) {
   const int64_t G = q8_row(K) / 128;
-  if (M <= 16) return launch_few<SLIM_Q8_E4M3, DT>(X, ex, 0, W, ew, M, N, K, Y, ldy, s);
-  int best = 0;
-  for (int i = 1; i < 6; ++i)
-    if (tile_time(kTiles[i], M, N, G) < tile_time(kTiles[best], M, N, G)) best = i;
-  const double w = (double)N * G * 128, t = tile_time(kTiles[best], M, N, G);
-  if (M <= 32 && 7 + 2 * w / 8.6e6 < t) return launch_few_of<2, 2, SLIM_Q8_E4M3, DT>(X, ex, 0, W, ew, M, N, K, Y, ldy, s);
-  if (M <= 64 && 6 + 5 * w / 6e6 < t) return launch_few_of<4, 1, SLIM_Q8_E4M3, DT>(X, ex, 0, W, ew, M, N, K, Y, ldy, s);
-  switch (best) {
-    case 0: return launch_tile<16, 4, DT>(X, ex, W, ew, M, N, G, Y, ldy, s);
-    case 1: return launch_tile<12, 4, DT>(X, ex, W, ew, M, N, G, Y, ldy, s);
-    case 2: return launch_tile<8, 4, DT>(X, ex, W, ew, M, N, G, Y, ldy, s);
-    case 3: return launch_tile<8, 2, DT>(X, ex, W, ew, M, N, G, Y, ldy, s);
-    case 4: return launch_tile<4, 2, DT>(X, ex, W, ew, M, N, G, Y, ldy, s);
-    default: return launch_tile<4, 1, DT>(X, ex, W, ew, M, N, G, Y, ldy, s);
+  if (p.few == 1) return launch_few<SLIM_Q8_E4M3, DT>(X, ex, 0, W, ew, M, N, K, Y, ldy, s);
+  if (p.few == 2) return launch_few_of<2, 2, SLIM_Q8_E4M3, DT>(X, ex, 0, W, ew, M, N, K, Y, ldy, s);
+  if (p.few == 4) return launch_few_of<4, 1, SLIM_Q8_E4M3, DT>(X, ex, 0, W, ew, M, N, K, Y, ldy, s);
+  switch (p.kind) {
+    case 0: return launch_tile<16, 4, DT>(p, X, ex, W, ew, M, N, G, Y, ldy, ws, s);
+    case 1: return launch_tile<12, 4, DT>(p, X, ex, W, ew, M, N, G, Y, ldy, ws, s);
+    case 2: return launch_tile<8, 4, DT>(p, X, ex, W, ew, M, N, G, Y, ldy, ws, s);
+    case 3: return launch_tile<8, 2, DT>(p, X, ex, W, ew, M, N, G, Y, ldy, ws, s);
+    case 4: return launch_tile<4, 2, DT>(p, X, ex, W, ew, M, N, G, Y, ldy, ws, s);
+    default: return launch_tile<4, 1, DT>(p, X, ex, W, ew, M, N, G, Y, ldy, ws, s);
   }
 }
 
@@ -524,7 +585,10 @@ extern "C" int slim_linear8_workspace(int xdtype, int64_t M, int64_t N, int64_t 
   if (!bytes) return SLIM_EINVAL;
   const int rc = check_sizes(xdtype, M, N, K);
   if (rc != SLIM_OK) return rc;
-  *bytes = xdtype == SLIM_Q8_E4M3 || quant_in_launch(xdtype, M, K) ? 0 : code_bytes(M, K) + round256((size_t)M * (size_t)q8_exp_row(K));
+  *bytes = 0;
+  if (M == 0 || quant_in_launch(xdtype, M, K)) return SLIM_OK;
+  *bytes = plan(M, N, K).bytes;
+  if (xdtype != SLIM_Q8_E4M3) *bytes += code_bytes(M, K) + round256((size_t)M * (size_t)q8_exp_row(K));
   return SLIM_OK;
 }
 
@@ -560,15 +624,18 @@ extern "C" int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int
     else to(std::integral_constant<int, SLIM_F32>{});
     return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
   }
+  const Plan p = plan(M, N, K);
+  float* sums = reinterpret_cast<float*>(ws);
   if (!packed) {
     uint8_t* c = reinterpret_cast<uint8_t*>(ws);
     uint8_t* e = c + code_bytes(M, K);
+    sums = reinterpret_cast<float*>(e + round256((size_t)M * (size_t)q8_exp_row(K)));
     const int q = slim_quant8(X, xdtype, M, K, ldx, c, e, stream);
     if (q != SLIM_OK) return q;
     xc = c;
     xe = e;
   }
-  if (ydtype == SLIM_F16) launch<0>(xc, xe, codes, exps, M, N, K, y, ldy, s);
-  else launch<1>(xc, xe, codes, exps, M, N, K, y, ldy, s);
+  if (ydtype == SLIM_F16) launch<0>(p, xc, xe, codes, exps, M, N, K, y, ldy, sums, s);
+  else launch<1>(p, xc, xe, codes, exps, M, N, K, y, ldy, sums, s);
   return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
 }

@@ -21,9 +21,12 @@ SIZES = [(65, 17, 129), (100, 513, 1300), (200, 130, 4100),
          (400, 8200, 129), (2047, 2050, 300), (8192, 513, 640),
          (1000, 8200, 129), (2500, 4100, 900), (4097, 2050, 1300),
          (1500, 8200, 129), (2500, 5000, 640), (6001, 2050, 1100)]
+# few tiles and a long reduction, which is then sliced: of each tile kernel that can be, with slices that end past the last group
+SLICED = [(5, 130, 28672), (24, 512, 14336), (64, 1000, 28001), (100, 513, 28672), (300, 131, 9000), (512, 515, 28672), (1024, 770, 20001),
+          (2000, 200, 12345)]
 
 
-@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("m,n,k", SIZES + SLICED)
 def test_small_integers_are_exact(m, n, k):
     print(f"linear8 tiles m={m} n={n} k={k}", flush=True)
     gen = torch.Generator("cuda").manual_seed(m + n + k)
@@ -35,7 +38,7 @@ def test_small_integers_are_exact(m, n, k):
     assert bool((buf[m] == 9).all()) and bool((buf[:, n:] == 9).all())
 
 
-@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("m,n,k", SIZES + SLICED)
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float16])
 def test_values_of_any_size(m, n, k, out):
     print(f"linear8 tiles m={m} n={n} k={k} {out}", flush=True)
@@ -48,3 +51,22 @@ def test_values_of_any_size(m, n, k, out):
     xv = act8.values_rows(*act8.quant_rows(host(x)[rows].astype(np.float64)), k)
     wv = act8.values_weight(*act8.quant_weight(host(w).astype(np.float64)))
     check(Y[torch.from_numpy(rows).cuda()], xv, wv, "bf16" if out is torch.bfloat16 else "fp16")
+
+
+@pytest.mark.parametrize("m,n,k", SLICED)
+def test_slices_are_what_runs(m, n, k):
+    x, p = torch.zeros((m, k), dtype=torch.bfloat16, device="cuda"), slim.pack8(torch.zeros((n, k), device="cuda"))
+    slim.slim_timing_reset()
+    slim.slim_timing_enable(True)
+    Y = slim.linear8(x, p)
+    torch.cuda.synchronize()
+    slim.slim_timing_enable(False)
+    assert {"linear8_tile", "linear8_sum"} <= set(slim.slim_timing_read()) and not bool(Y.any())
+    # the workspace is exactly what is asked for: nothing is written past it
+    q = slim.quant8(x)
+    need = slim.slim_linear8_workspace(slim.SLIM_Q8_E4M3, m, n, k)
+    ws = torch.full((need + 256,), 7, dtype=torch.uint8, device="cuda")
+    slim.linear8(q, p, ws=ws[:need])
+    assert need > 0 and bool((ws[need:] == 7).all())
+    with pytest.raises(slim.SlimError):
+        slim.linear8(q, p, ws=ws[:need - 16])
