@@ -77,7 +77,7 @@ SLIM_DEV void store_rows(float* gW, bool masked, const uint32_t (&byte)[COUNT], 
 // slice, which k_wgrad8_sum adds in slice order.
 // TK 128: two blocks a CU hide each other's LDS and barriers. TK 64: for layers of so few tiles that a block stands alone
 // on its CU anyway, where reads, products and writes of a chunk follow one another: half of each, on twice the CUs. 999 x 2051 x
-// 768 14.5 us, 0.5 us a chunk of 64 rows; M 64, 28672 x 8192 197 us, of which writing the result is 184.
+// 768 14.5 us, 0.5 us a chunk of 64 rows; 64 x 28672 x 8192 225 us with TK 128, of which writing the result is 184.
 template <int DT, int HI>
 SLIM_DEV uint32_t widen2(uint32_t c, float s);
 
@@ -311,8 +311,8 @@ SLIM_DEV uint32_t lds_at_wide(int r, int c) {
 // and K read what lies there or zero; their results are not stored.
 // Bound by the matrix unit, busy for 65 % of the cycles at the 1.6 GHz that the card then keeps (LDS for 33 %), and by its waits
 // for operands: 8192 x 8192 x 8192 in bf16 874 us (1.26 PFLOP/s; a library product of bf16 operands 1.23), 8192 x 28672 x 8192
-// at kept positions 3.10 ms (1.24). Over few rows the first loads and last stores of every round of tiles show: 512 x 28672 x
-// 8192 347 us, of which writing the result is 184.
+// at kept positions 2.87 ms (1.34). Over few rows the first loads and last stores of every round of tiles show: 512 x 28672 x
+// 8192 331 us, of which writing the result is 184; at kept positions 290.
 template <int DT>
 __global__ void __launch_bounds__(256, 1)
 k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xe,
@@ -603,12 +603,15 @@ size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
 
 GradPlan grad_plan(int64_t M, int64_t N, int64_t K, bool masked, bool aligned) {
   GradPlan p{};
-  // A wide tile's block stands alone on its CU, so its first loads and last stores show: over few rows two small blocks to a CU
-  // are as fast or faster (9776 x 5786, M 64: 56 us against 58, M 128: 62 against 66, M 256: 95 against 77), and over more
-  // where the wide tiles leave CUs idle (2048 x 4096, 128 of them: M 512 20 against 23, M 1024 32 against 33, M 2048 55
-  // against 53; 22736 x 128, 89: 82 against 95 still at M 4096).
+  // A wide tile's block stands alone on its CU, so its first loads and last stores show, and so do CUs left idle in the last
+  // round of blocks; the small kernel has two on each. `use`: the share of the rounds' CUs that have a wide tile. us, wide
+  // against small: 128 tiles of a possible 256, 2048 x 4096, M 4096 91 against 84; 160, 2560 x 4096, M 1024 35 against 40; 289 of
+  // 512, 4100 x 4090, M 512 49 against 39; 304, 4096 x 4864, M 256 33 against 30, M 1024 68 both, M 4096 212 against 253; 897,
+  // 9776 x 5786, M 64 57 against 53, M 96 60 both, M 192 71 against 84. At kept positions its stores are the shorter ones too:
+  // 4096 x 4096, M 64 15 against 25.
   const int64_t wide = cdiv(N, 256) * cdiv(K, 256);
-  p.wide = (wide >= 256 ? M >= 192 : wide >= 128 && M >= 1536) && N < (int64_t(1) << 22) - 16;
+  const double use = (double)wide / (double)(cdiv(wide, 256) * 256);
+  p.wide = M > 0 && use >= 0.58 && M >= (wide >= 256 && use >= 0.65 ? (masked ? 1 : 96) : 768) && N < (int64_t(1) << 22) - 16;
   p.copy = M > 0 && (p.wide ? !aligned : N < 16);        // (the other kernel takes pieces of 16)
   p.slices = 1;
   p.slice = M;

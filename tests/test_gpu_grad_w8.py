@@ -94,10 +94,10 @@ def test_large_layer_of_no_rows():
     assert g.shape == (8200, 1024) and bool((g == 0).all())
 
 
-# 128 x 128 tiles that fill the chip, over one slice of the rows and over three; then at least 256 tiles of 256 x 256, and at
-# least 128 of them over more rows
-MANY = [(520, 2000, 1040), (513, 2051, 1030), (3000, 1000, 1040), (2999, 1003, 1041),
-        (193, 4100, 4090), (200, 8192, 2048), (255, 4097, 4112), (1537, 2301, 3888)]
+# 128 x 128 tiles that fill the chip, over one slice of the rows and over three, then 256 x 256 tiles: whole rounds of them, one
+# round not quite full, and rounds that leave most of the last idle
+MANY = [(520, 2000, 1040), (513, 2051, 1030), (3000, 1000, 1040), (2999, 1003, 1041), (255, 4097, 4112),
+        (97, 4096, 4090), (200, 8192, 2048), (131, 3961, 3888), (1537, 2301, 4352), (769, 4099, 2549), (800, 4352, 4096)]
 
 
 @pytest.mark.parametrize("m,n,k", MANY)
