@@ -93,9 +93,16 @@ SLIM_DEV void values8(const Raw8<DT>& o, float* f) {
 }
 
 // xh = (x - mu) rstd of eight elements, one fused operation each: `shift` = -mu rstd, and of 8-bit rows the group's power of
-// two goes into the factor.
+// two goes into the factor. The rounding of mu rstd is below a step of x in 16 and 8 bits; fp32 rows far from zero would lose
+// by it, and take the difference first.
 template <int DT>
-SLIM_DEV void xhat8(const Raw8<DT>& o, float rstd, float shift, float* f) {
+SLIM_DEV void xhat8(const Raw8<DT>& o, float mu, float rstd, float shift, float* f) {
+  if constexpr (DT == 2) {
+    values8<DT>(o, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = (f[e] - mu) * rstd;
+    return;
+  }
   float s = rstd;
   if constexpr (DT == kQ8) {
     q8_values4(o.c[0], 1.f, f);
@@ -404,7 +411,7 @@ k_norm_bwd(NormBwdArgs a) {
   const float inv_k = 1.f / (float)a.K;
   int turn = 0;
   for (int64_t row = first; row < a.M; row += step, turn ^= 1) {
-    const float rstd = a.rstd[row], shift = a.mean ? -a.mean[row] * rstd : 0.f;
+    const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row], shift = -mu * rstd;
     Raw8<DT> y[V];
     Raw8<XT> x[V];
 #pragma unroll
@@ -428,7 +435,7 @@ k_norm_bwd(NormBwdArgs a) {
     for (int v = 0; v < V; ++v) {
       float d[8], h[8];
       values8<DT>(y[v], d);
-      xhat8<XT>(x[v], rstd, shift, h);
+      xhat8<XT>(x[v], mu, rstd, shift, h);
       const int g = HOLD ? v : 0;
       if constexpr (!HOLD) params8<RAG>(a.gamma, a.pdt, (int64_t)(v * T + t) * 8, a.K, 1.f, gm[0]);
 #pragma unroll
@@ -446,7 +453,7 @@ k_norm_bwd(NormBwdArgs a) {
     for (int v = 0; v < V; ++v) {
       float d[8], h[8];
       values8<DT>(y[v], d);
-      xhat8<XT>(x[v], rstd, shift, h);
+      xhat8<XT>(x[v], mu, rstd, shift, h);
       const int g = HOLD ? v : 0;
       if constexpr (!HOLD) params8<RAG>(a.gamma, a.pdt, (int64_t)(v * T + t) * 8, a.K, 1.f, gm[0]);
 #pragma unroll
@@ -534,7 +541,7 @@ k_norm_bwd_dx(NormBwdArgs a) {
   constexpr int V = 4;
   __shared__ f2_t part[2][16];
   const int64_t row = blockIdx.x;
-  const float rstd = a.rstd[row], shift = a.mean ? -a.mean[row] * rstd : 0.f;
+  const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row], shift = -mu * rstd;
   Raw8<DT> y[V];
   Raw8<XT> x[V];
 #pragma unroll
@@ -549,7 +556,7 @@ k_norm_bwd_dx(NormBwdArgs a) {
     float d[8], h[8], g[8];
     params8<false>(a.gamma, a.pdt, (int64_t)(v * 1024 + threadIdx.x) * 8, a.K, 1.f, g);
     values8<DT>(y[v], d);
-    xhat8<XT>(x[v], rstd, shift, h);
+    xhat8<XT>(x[v], mu, rstd, shift, h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float tt = d[e] * g[e];
@@ -565,7 +572,7 @@ k_norm_bwd_dx(NormBwdArgs a) {
     float d[8], h[8], g[8];
     params8<false>(a.gamma, a.pdt, col, a.K, 1.f, g);
     values8<DT>(y[v], d);
-    xhat8<XT>(x[v], rstd, shift, h);
+    xhat8<XT>(x[v], mu, rstd, shift, h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-mx, h[e], fmaf(d[e], g[e], -mt));
     store_row8<DT, false>(a.dx, nullptr, row, a.lddx, col, a.K, d);

@@ -214,6 +214,21 @@ def test_backward_against_differences(rms):
         assert abs(want - (f64(grad) * d).sum()) < 1e-6 + 64 * V * 10 * 222
 
 
+@pytest.mark.parametrize("k", [100, 4096, 12288, 20000])
+def test_backward_of_rows_far_from_zero(k):
+    # fp32 rows about 1000 with deviations of 1: xh is (x - mean) rstd with the difference taken first, exact but for the mean's
+    # own rounding (2^-25 of it) and a rounding each, so off by (1000 + 4 |xh|) 2^-24 at most
+    rng = synth.stream(13, f"norm/far/{k}")
+    x = (1000 + rng.standard_normal((4, k))).astype(np.float32)
+    dy = rng.standard_normal((4, k)).astype(np.float32)
+    _, mean, rstd = slim.norm(dev(x))
+    dg = f64(slim.norm_bwd(dev(dy), dev(x), None, mean, rstd)[1])
+    mu, rs = x.astype(np.float64).mean(1, keepdims=True), f64(rstd)[:, None]
+    xh = (x.astype(np.float64) - f64(mean)[:, None]) * rs
+    assert np.all(np.abs(f64(mean)[:, None] - mu) <= 40 * V * 1010)
+    assert np.all(np.abs(dg - (dy * xh).sum(0)) <= V * (np.abs(dy) * (8 * np.abs(xh))).sum(0) + 8 * V * np.abs(dy * xh).sum(0))
+
+
 def test_backward_in_place_and_strided():
     for k in (601, 9000):
         t, g, b = inputs(12, 2 * k, "bf16", seed=10)
