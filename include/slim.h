@@ -509,8 +509,10 @@ int slim_linear_hybrid(const void* X, int64_t M, int64_t N, int64_t K, const uin
  *             uint8 [N/128 up][K/128 rounded up to 4], the bytes past the last block zero.
  * 16-bit and fp32 operands may have rows of any stride >= their width (in elements) and start at
  * any element; codes and exponents are 16-byte aligned. M = 0 is allowed: nothing is read, and
- * sums over rows are zero. Rows are at most 2^22 columns. Every call is asynchronous, allocates
- * nothing, may be captured into a graph, and gives the same bits for the same inputs.
+ * sums over rows are zero. Rows are at most 2^22 columns. What one launch cannot take returns
+ * SLIM_EUNSUPPORTED: 2^29 groups in slim_quant8 and slim_dequant8, 2^22 rows of more than 16384 columns
+ * in the norms, 2^36 elements of dY in slim_grad_w8. Every call is asynchronous, allocates nothing, may
+ * be captured into a graph, and gives the same bits for the same inputs.
  * ----
  *
  * slim_quant8 - X [M, K] (`dtype` SLIM_F16, SLIM_BF16 or SLIM_F32, row stride ldx) in 8 bits.

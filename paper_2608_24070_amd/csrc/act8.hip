@@ -150,7 +150,7 @@ extern "C" int slim_quant8(const void* X, int dtype, int64_t M, int64_t K, int64
   if (!X || !codes || !exps) return SLIM_EINVAL;
   if (!slim_aligned_to(X, dtype == SLIM_F32 ? 4 : 2) || !slim_aligned16(codes) || !slim_aligned16(exps)) return SLIM_EALIGN;
   const int64_t G = (K + 127) / 128;
-  if (M > kMaxGroups8 / G) return SLIM_EUNSUPPORTED;
+  if (M > kMaxQuant8 / G) return SLIM_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   const uint32_t total = (uint32_t)(M * G);
   const dim3 grid((unsigned)((M * G + 31) / 32));
@@ -172,7 +172,7 @@ extern "C" int slim_dequant8(const uint8_t* codes, const uint8_t* exps, int64_t 
   if (!codes || !exps || !Y) return SLIM_EINVAL;
   if (!slim_aligned_to(Y, dtype == SLIM_F32 ? 4 : 2) || !slim_aligned16(codes) || !slim_aligned16(exps)) return SLIM_EALIGN;
   const int64_t G = (K + 127) / 128;
-  if (M > kMaxGroups8 / G) return SLIM_EUNSUPPORTED;
+  if (M > kMaxQuant8 / G) return SLIM_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   const uint32_t total = (uint32_t)(M * G);
   const dim3 grid((unsigned)((M * G + 31) / 32));

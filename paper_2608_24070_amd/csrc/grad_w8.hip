@@ -635,7 +635,7 @@ GradPlan grad_plan(int64_t M, int64_t N, int64_t K, bool masked, bool aligned) {
 
 int check_grad(int64_t M, int64_t N, int64_t K, bool masked) {
   if (M < 0 || N < 1 || K < 1 || N > kMaxRow8 || K > kMaxRow8 || (masked && K % 16)) return SLIM_ESHAPE;
-  if (cdiv(N, 128) * cdiv(K, 128) > 0x7FFFFFFF || M >= (int64_t(1) << 31) || M > (int64_t(1) << 36) / cdiv(N, 16))
+  if (cdiv(N, 128) * cdiv(K, 128) > 0x7FFFFFFF || M >= (int64_t(1) << 31) || M > ((int64_t(1) << 32) - 256) / cdiv(N, 16))      // (pieces of a copy are counted in 32 bits)
     return SLIM_EUNSUPPORTED;
   return SLIM_OK;
 }

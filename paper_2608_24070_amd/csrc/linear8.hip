@@ -574,7 +574,7 @@ size_t code_bytes(int64_t M, int64_t K) { return round256((size_t)M * (size_t)q8
 int check_sizes(int xdtype, int64_t M, int64_t N, int64_t K) {
   if (xdtype != SLIM_F16 && xdtype != SLIM_BF16 && xdtype != SLIM_F32 && xdtype != SLIM_Q8_E4M3) return SLIM_EDTYPE;
   if (M < 0 || N < 1 || K < 1 || N > kMaxRow8 || K > kMaxRow8) return SLIM_ESHAPE;
-  if (M > kMaxGroups8 / (q8_row(K) / 128) || M > kMaxGroups8 / 128) return SLIM_EUNSUPPORTED;
+  if (M > (xdtype == SLIM_Q8_E4M3 ? kMaxGroups8 : kMaxQuant8) / (q8_row(K) / 128) || M > kMaxGroups8 / 128) return SLIM_EUNSUPPORTED;
   if (cdiv(M, 64) * cdiv(N, 64) >= (int64_t(1) << 31)) return SLIM_EUNSUPPORTED;      // tiles are counted in 32 bits
   return SLIM_OK;
 }

@@ -92,27 +92,21 @@ SLIM_DEV void values8(const Raw8<DT>& o, float* f) {
   }
 }
 
-// xh = (x - mu) rstd of eight elements, one fused operation each: `shift` = -mu rstd, and of 8-bit rows the group's power of
-// two goes into the factor. The rounding of mu rstd is below a step of x in 16 and 8 bits; fp32 rows far from zero would lose
-// by it, and take the difference first.
+// xh = (x - mu) rstd of eight elements, the difference first: x rstd - mu rstd in one operation would leave a rounding of
+// mu rstd, which in rows far from zero with little or no variance passes xh itself. (A second operation for each element: see
+// k_norm_bwd for what it costs.)
 template <int DT>
-SLIM_DEV void xhat8(const Raw8<DT>& o, float mu, float rstd, float shift, float* f) {
-  if constexpr (DT == 2) {
-    values8<DT>(o, f);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = (f[e] - mu) * rstd;
-    return;
-  }
-  float s = rstd;
+SLIM_DEV void xhat8(const Raw8<DT>& o, float mu, float rstd, float* f) {
   if constexpr (DT == kQ8) {
     q8_values4(o.c[0], 1.f, f);
     q8_values4(o.c[1], 1.f, f + 4);
-    s = o.s * rstd;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = fmaf(f[e], o.s, -mu) * rstd;
   } else {
     values8<DT>(o, f);
-  }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = fmaf(f[e], s, shift);
+    for (int e = 0; e < 8; ++e) f[e] = (f[e] - mu) * rstd;
+  }
 }
 
 // Eight parameters (gamma, beta) as fp32; `none` where there are none.
@@ -218,7 +212,8 @@ struct NormArgs {
 
 // Rows of up to 8 T V elements, T threads a row, V vectors of 8 a thread. Each wave sums its part of the row about its
 // own mean, and the waves' (count, mean, squares) are joined exactly as if about the row's mean: one barrier a row, and no
-// cancellation for rows far from zero. HOLD: gamma and beta stay in registers from row to row; AHEAD: the next row is loaded
+// cancellation for rows far from zero. Means are quotients, not products with 1 / K, so that a row of one value has that
+// value as its mean wherever its sum is exact, and results of beta. HOLD: gamma and beta stay in registers from row to row; AHEAD: the next row is loaded
 // before the present one is worked on (both as registers allow).
 // Bound by memory: 8192 x 8192 in bf16 41.6 us (6.5 TB/s read and written), to 8 bits 46.9 us (4.3 TB/s); 2047 x 5120 in
 // fp16 15.0 us; one row of 4096 6.4 us, which is a launch and two trips to memory.
@@ -245,7 +240,7 @@ k_norm(NormArgs a) {
     mine += n <= 0 ? 0 : n > 512 ? 512 : (int)n;
   }
   if (T > 64 && (t & 63) == 0) count[t >> 6] = (float)mine;
-  const float inv_mine = mine ? 1.f / (float)mine : 0.f, inv_k = 1.f / (float)a.K;
+  const float held = mine ? (float)mine : 1.f, inv_k = 1.f / (float)a.K;
   int turn = 0;
   for (int64_t row = first; row < a.M; row += step, turn ^= 1) {
     float x[V][8];
@@ -264,7 +259,7 @@ k_norm(NormArgs a) {
       for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += x[v][e];
-      mu = wave_sum(s) * inv_mine;
+      mu = wave_sum(s) / held;
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -289,7 +284,7 @@ k_norm(NormArgs a) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) sum = fmaf(count[i], part[turn][i][0], sum);
-      mu = sum * inv_k;
+      mu = sum / (float)a.K;
       sq = 0.f;
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) {
@@ -411,7 +406,7 @@ k_norm_bwd(NormBwdArgs a) {
   const float inv_k = 1.f / (float)a.K;
   int turn = 0;
   for (int64_t row = first; row < a.M; row += step, turn ^= 1) {
-    const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row], shift = -mu * rstd;
+    const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
     Raw8<DT> y[V];
     Raw8<XT> x[V];
 #pragma unroll
@@ -435,7 +430,7 @@ k_norm_bwd(NormBwdArgs a) {
     for (int v = 0; v < V; ++v) {
       float d[8], h[8];
       values8<DT>(y[v], d);
-      xhat8<XT>(x[v], mu, rstd, shift, h);
+      xhat8<XT>(x[v], mu, rstd, h);
       const int g = HOLD ? v : 0;
       if constexpr (!HOLD) params8<RAG>(a.gamma, a.pdt, (int64_t)(v * T + t) * 8, a.K, 1.f, gm[0]);
 #pragma unroll
@@ -453,7 +448,7 @@ k_norm_bwd(NormBwdArgs a) {
     for (int v = 0; v < V; ++v) {
       float d[8], h[8];
       values8<DT>(y[v], d);
-      xhat8<XT>(x[v], mu, rstd, shift, h);
+      xhat8<XT>(x[v], mu, rstd, h);
       const int g = HOLD ? v : 0;
       if constexpr (!HOLD) params8<RAG>(a.gamma, a.pdt, (int64_t)(v * T + t) * 8, a.K, 1.f, gm[0]);
 #pragma unroll
@@ -541,7 +536,7 @@ k_norm_bwd_dx(NormBwdArgs a) {
   constexpr int V = 4;
   __shared__ f2_t part[2][16];
   const int64_t row = blockIdx.x;
-  const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row], shift = -mu * rstd;
+  const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
   Raw8<DT> y[V];
   Raw8<XT> x[V];
 #pragma unroll
@@ -556,7 +551,7 @@ k_norm_bwd_dx(NormBwdArgs a) {
     float d[8], h[8], g[8];
     params8<false>(a.gamma, a.pdt, (int64_t)(v * 1024 + threadIdx.x) * 8, a.K, 1.f, g);
     values8<DT>(y[v], d);
-    xhat8<XT>(x[v], mu, rstd, shift, h);
+    xhat8<XT>(x[v], mu, rstd, h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float tt = d[e] * g[e];
@@ -572,7 +567,7 @@ k_norm_bwd_dx(NormBwdArgs a) {
     float d[8], h[8], g[8];
     params8<false>(a.gamma, a.pdt, col, a.K, 1.f, g);
     values8<DT>(y[v], d);
-    xhat8<XT>(x[v], mu, rstd, shift, h);
+    xhat8<XT>(x[v], mu, rstd, h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-mx, h[e], fmaf(d[e], g[e], -mt));
     store_row8<DT, false>(a.dx, nullptr, row, a.lddx, col, a.K, d);
@@ -641,6 +636,9 @@ k_norm_cols(const float* __restrict__ part, int blocks, int64_t K, float* __rest
 bool float_type(int dt) { return dt == SLIM_F16 || dt == SLIM_BF16 || dt == SLIM_F32; }
 size_t elem(int dt) { return dt == SLIM_F32 ? 4 : 2; }
 
+// Rows past 16384 may take a block of 1024 threads each, and a launch holds fewer than 2^32 threads.
+bool too_many(int64_t M, int64_t K) { return K > 16384 && M >= int64_t(1) << 22; }
+
 template <int DT, int YT, bool RAG>
 void norm_rows(const NormArgs& a, SlimKernelTimer& timer, hipStream_t s) {
   const auto grid = [&](int64_t units, int64_t most) { return dim3((unsigned)(units < most ? units : most)); };
@@ -703,6 +701,7 @@ extern "C" int slim_norm(const void* X, int dtype, int64_t M, int64_t K, int64_t
   const bool q8 = ydtype == SLIM_Q8_E4M3;
   if (M < 0 || K < 1 || K > kMaxRow8 || M > 0x7FFFFFFF || ldx < K || (!q8 && ldy < K)) return SLIM_ESHAPE;
   if (!(eps >= 0.f) || (rms && beta)) return SLIM_EINVAL;
+  if (too_many(M, K)) return SLIM_EUNSUPPORTED;
   if (M == 0) return SLIM_OK;
   if (!X || !Y || !rstd || (q8 && !yexps)) return SLIM_EINVAL;
   if (!slim_aligned_to(X, elem(dtype)) || !slim_aligned_to(Y, q8 ? 16 : elem(dtype)) || !slim_aligned16(yexps) ||
@@ -721,6 +720,7 @@ extern "C" int slim_norm(const void* X, int dtype, int64_t M, int64_t K, int64_t
 extern "C" int slim_norm_bwd_workspace(int64_t M, int64_t K, size_t* bytes) {
   if (!bytes) return SLIM_EINVAL;
   if (M < 0 || K < 1 || K > kMaxRow8 || M > 0x7FFFFFFF) return SLIM_ESHAPE;
+  if (too_many(M, K)) return SLIM_EUNSUPPORTED;
   const int64_t blocks = M > 0 ? bwd_blocks(M, K) : 0;
   *bytes = blocks > 1 ? (size_t)blocks * 2 * (size_t)K * 4 : 0;
   return SLIM_OK;

@@ -6,9 +6,11 @@
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef float f2_t __attribute__((ext_vector_type(2)));
 
-// Most columns of a row kept in 8 bits (256 rows stay within 32-bit byte offsets), and most groups of one call.
+// Most columns of a row kept in 8 bits (256 rows stay within 32-bit byte offsets), most groups of one operand, and most that
+// one launch of eight lanes a group takes (a launch holds fewer than 2^32 threads).
 constexpr int64_t kMaxRow8 = int64_t(1) << 22;
 constexpr int64_t kMaxGroups8 = (int64_t(1) << 32) - 64;
+constexpr int64_t kMaxQuant8 = (int64_t(1) << 29) - 64;
 
 // Fitted sizes: codes per row (whole groups) and exponent bytes per row (whole 32-bit words).
 constexpr int64_t q8_row(int64_t k) { return (k + 127) / 128 * 128; }

@@ -116,3 +116,24 @@ def test_binding_refuses_host_tensors():
                  lambda: slim.norm_bwd(x, x, None, None, torch.zeros(2))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_sizes_past_one_launch():
+    # eight threads a group of 128, and fewer than 2^32 threads a launch: refused before anything is read
+    for m, k, status in ((1 << 29, 128, UNSUP), (1 << 22, 128 << 7, UNSUP), (1 << 29, 1, UNSUP)):
+        assert slim.slim_quant8(A, F16, m, k, k, A, A, None) == status
+        assert slim.slim_dequant8(A, A, m, k, A, F16, k, None) == status
+    for xdt, m, n, k in ((BF16, 1 << 22, 16, 128 << 7), (Q8, 1 << 25, 16, 128 << 7)):
+        with pytest.raises(slim.SlimError) as e:
+            slim.slim_linear8_workspace(xdt, m, n, k)
+        assert e.value.status == UNSUP
+    # the pieces of a copy of dY are counted in 32 bits
+    for m, n in (((1 << 31) - 1, 128), (1 << 20, 1 << 16)):
+        with pytest.raises(slim.SlimError) as e:
+            slim.slim_grad_w8_workspace(m, n, 128, 0, 0)
+        assert e.value.status == UNSUP
+    # a block of 1024 threads a row
+    assert slim.slim_norm(A, F16, 1 << 22, 16385, 16385, None, None, F32, 0, 1e-5, A, F16, 16385, None, None, A, None) == UNSUP
+    with pytest.raises(slim.SlimError) as e:
+        slim.slim_norm_bwd_workspace(1 << 22, 16385)
+    assert e.value.status == UNSUP

@@ -265,3 +265,20 @@ def test_another_stream_and_repeats():
             again = slim.norm_bwd(y, x, g.cuda(), mean, rstd)
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(again, first))
+
+
+@pytest.mark.parametrize("k", [100, 1000, 1025, 4097, 5120, 12289, 20000, 28680, 40001])
+@pytest.mark.parametrize("dtype,q8", [("bf16", False), ("fp16", False), ("fp32", False), ("bf16", True), ("fp16", True)])
+def test_rows_of_one_value_far_from_zero(k, dtype, q8):
+    # 13 * 4096: exact in every type, in 8 bits too, and so is its sum over a row (13 k < 2^24). Then the mean is the value and
+    # xh is zero exactly, while rstd = 316 would make 0.5 of a rounding step of mean * rstd
+    value = 13 * 4096.0
+    t = torch.full((5, k), value, dtype=DT[dtype], device="cuda")
+    rng = synth.stream(14, f"norm/one/{k}")
+    b = dev((0.3 * rng.standard_normal(k)).astype(np.float32))
+    dy = torch.from_numpy(rng.standard_normal((5, k)).astype(np.float32)).to(DT[dtype]).cuda()
+    y, mean, rstd = slim.norm(t, None, b)
+    assert bool((mean == value).all()) and torch.equal(y, b.to(DT[dtype]).expand(5, k))
+    _, dg, db = slim.norm_bwd(dy, slim.quant8(t) if q8 else t, None, mean, rstd)
+    assert bool((dg == 0).all())
+    assert np.all(np.abs(f64(db) - f64(dy).sum(0)) <= 69 * V * np.abs(f64(dy)).sum(0))
