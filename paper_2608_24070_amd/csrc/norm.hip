@@ -93,8 +93,8 @@ SLIM_DEV void values8(const Raw8<DT>& o, float* f) {
 }
 
 // xh = (x - mu) rstd of eight elements, the difference first: x rstd - mu rstd in one operation would leave a rounding of
-// mu rstd, which in rows far from zero with little or no variance passes xh itself. (A second operation for each element: see
-// k_norm_bwd for what it costs.)
+// mu rstd, which in rows far from zero with little or no variance passes xh itself. (The second operation for each element
+// hides behind memory: 8192 x 8192 in bf16 82.8 us for both launches before, 83.0 with it.)
 template <int DT>
 SLIM_DEV void xhat8(const Raw8<DT>& o, float mu, float rstd, float* f) {
   if constexpr (DT == kQ8) {
