@@ -881,13 +881,25 @@ def pack8(W, bwd: bool = False, stream=None) -> dict:
 _ws8 = threading.local()
 
 
+def _capturing(dev: int) -> bool:
+    """Whether device `dev`'s current stream is being captured into a graph."""
+    cuda = _torch().cuda
+    if cuda.current_device() == dev:
+        return cuda.is_current_stream_capturing()
+    with cuda.device(dev):
+        return cuda.is_current_stream_capturing()
+
+
 def _workspace8(nbytes: int, like, stream: int):
     """The 8-bit calls' workspace, kept per thread, device and stream: a call's launches follow each other on the stream, but
     another thread's may come between. Its contents are of no interest between calls, so it is not slim_linear's, whose
-    counters have to stay zero. (A captured call holds the workspace of its capture: where the graph is to run beside other
-    work of that stream, the call is given one of its own.)"""
+    counters have to stay zero. A captured call has one of its own, from its graph's memory: a kept one is replaced when a
+    larger call needs more and goes with its thread, and the graph would then write to memory that others were given."""
+    dev = like.get_device()
+    if _capturing(dev):
+        return like.new_empty(nbytes, dtype=_torch().uint8)
     cache = _ws8.__dict__
-    key = (like.get_device(), stream)
+    key = (dev, stream)
     ws = cache.get(key)
     if ws is None or ws.numel() < nbytes:
         ws = cache[key] = like.new_empty(max(nbytes, 1 << 16), dtype=_torch().uint8)

@@ -1,0 +1,37 @@
+"""The memory that a captured call's kernels write is its graph's for as long as the graph lives. The binding's kept workspaces
+are not: a larger call replaces them, and a thread takes its own with it. Here with host tensors in the place of device ones
+and a stream that says it is captured (no kernel runs)."""
+import pytest
+import torch
+
+from paper_2608_24070_amd import slim
+
+STREAM = 7          # a handle nobody uses
+
+
+@pytest.fixture
+def capture(monkeypatch):
+    """capture(True): from here on the stream is being captured."""
+    state = [False]
+    monkeypatch.setattr(slim, "_capturing", lambda dev: state[0], raising=False)
+    return lambda on: state.__setitem__(0, on)
+
+
+def overlap(a, b):
+    return a.data_ptr() < b.data_ptr() + b.numel() and b.data_ptr() < a.data_ptr() + a.numel()
+
+
+def test_the_8_bit_calls(capture):
+    like = torch.empty(0, dtype=torch.uint8)
+    kept = slim._workspace8(1000, like, STREAM)
+    assert slim._workspace8(500, like, STREAM) is kept
+    capture(True)
+    mine = slim._workspace8(1000, like, STREAM)
+    assert mine.numel() >= 1000 and not overlap(mine, kept)
+    larger = slim._workspace8(1 << 20, like, STREAM)
+    assert larger.numel() >= 1 << 20 and not overlap(larger, mine)
+    capture(False)
+    # nothing of the capture is kept, and what was kept before it still is
+    assert slim._workspace8(1000, like, STREAM) is kept
+    grown = slim._workspace8(1 << 20, like, STREAM)
+    assert not any(overlap(grown, t) for t in (mine, larger))
