@@ -365,14 +365,33 @@ def _on_gpu(*ts):
             raise ValueError("tensors must be contiguous and on the GPU")
 
 
+def _capturing(dev: int | None) -> bool:
+    """Whether the current stream of device `dev` (None: the current one) is being captured into a graph."""
+    cuda = _torch().cuda
+    if dev is None or cuda.current_device() == dev:
+        return cuda.is_current_stream_capturing()
+    with cuda.device(dev):
+        return cuda.is_current_stream_capturing()
+
+
 _ws_cache: dict = {}
+CONTROL_BYTES = 4096 * 4      # a workspace's leading control words, which start at zero
 
 
 def workspace(nbytes: int, device=None, stream=None):
-    """A zero-initialised workspace of at least nbytes, cached per (device, stream)."""
+    """A zero-initialised workspace of at least nbytes, cached per (device, stream), whose stream clears it. Under capture into
+    a graph a workspace of that call alone, from the graph's memory: a cached one is replaced when a larger call needs more.
+    The graph clears its leading control words on each replay (4096 x 4096, 16 rows: 11.2 us against 9.7); a call that is given a workspace does without."""
     torch = _torch()
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return workspace(nbytes, device)
     dev = device if isinstance(device, torch.device) else torch.device(device if device is not None else "cuda")
-    key = (dev, _stream(stream))
+    if _capturing(None):
+        ws = torch.empty(max(nbytes, CONTROL_BYTES), dtype=torch.uint8, device=dev)
+        ws[:CONTROL_BYTES].zero_()
+        return ws
+    key = (dev, _stream())
     ws = _ws_cache.get(key)
     if ws is None or ws.numel() < nbytes:
         ws = torch.zeros(max(nbytes, 1 << 16), dtype=torch.uint8, device=dev)
@@ -879,15 +898,6 @@ def pack8(W, bwd: bool = False, stream=None) -> dict:
 
 
 _ws8 = threading.local()
-
-
-def _capturing(dev: int) -> bool:
-    """Whether device `dev`'s current stream is being captured into a graph."""
-    cuda = _torch().cuda
-    if cuda.current_device() == dev:
-        return cuda.is_current_stream_capturing()
-    with cuda.device(dev):
-        return cuda.is_current_stream_capturing()
 
 
 def _workspace8(nbytes: int, like, stream: int):

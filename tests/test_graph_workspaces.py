@@ -35,3 +35,20 @@ def test_the_8_bit_calls(capture):
     assert slim._workspace8(1000, like, STREAM) is kept
     grown = slim._workspace8(1 << 20, like, STREAM)
     assert not any(overlap(grown, t) for t in (mine, larger))
+
+
+def test_the_compressed_layer(capture, monkeypatch):
+    monkeypatch.setattr(slim, "_stream", lambda stream=None: STREAM)
+    monkeypatch.setattr(slim, "_ws_cache", {})
+    kept = slim.workspace(100000, "cpu")
+    assert slim.workspace(70000, "cpu") is kept and not kept.any()
+    kept[0] = 1
+    capture(True)
+    mine = slim.workspace(100000, "cpu")
+    assert mine.numel() >= 100000 and not overlap(mine, kept)
+    assert not mine[:4096 * 4].any()          # the control words start at zero
+    assert slim.workspace(100, "cpu").numel() >= 4096 * 4
+    capture(False)
+    assert slim.workspace(100000, "cpu") is kept
+    grown = slim.workspace(1 << 20, "cpu")
+    assert not overlap(grown, mine) and not grown.any()
