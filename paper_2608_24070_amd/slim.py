@@ -381,7 +381,8 @@ CONTROL_BYTES = 4096 * 4      # a workspace's leading control words, which start
 def workspace(nbytes: int, device=None, stream=None):
     """A zero-initialised workspace of at least nbytes, cached per (device, stream), whose stream clears it. Under capture into
     a graph a workspace of that call alone, from the graph's memory: a cached one is replaced when a larger call needs more.
-    The graph clears its leading control words on each replay (4096 x 4096, 16 rows: 11.2 us against 9.7); a call that is given a workspace does without."""
+    The graph clears its leading control words on each replay (4096 x 4096, 16 rows: 11.2 us, 9.7 without); a call that is
+    given a workspace does not."""
     torch = _torch()
     if stream is not None:
         with torch.cuda.stream(stream):
@@ -499,6 +500,23 @@ def pack_hybrid(W, kinds, stream=None) -> dict:
 _hybrid_ws: dict = {}
 
 
+def _hybrid_workspace(nbytes: int, dev, stream=None):
+    """slim_linear_hybrid's workspace of at least nbytes, cached per (device, stream); a captured call's own, as in
+    ``workspace``. A cache of its own: the split partials must not land in slim_linear's workspace, whose control words have
+    to stay zero between calls."""
+    torch = _torch()
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _hybrid_workspace(nbytes, dev)
+    if _capturing(None):
+        return torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    key = (dev, _stream())
+    ws = _hybrid_ws.get(key)
+    if ws is None or ws.numel() < nbytes:
+        ws = _hybrid_ws[key] = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    return ws
+
+
 def linear_hybrid(X, p: dict, out=None, stream=None):
     """slim_linear_hybrid: Y fp32 [M, N] = X Wp^T for fp16 X [M, K] and a hybrid pack."""
     torch = _torch()
@@ -511,15 +529,7 @@ def linear_hybrid(X, p: dict, out=None, stream=None):
         raise ValueError("X width does not match the pack")
     Y = out if out is not None else torch.empty((M, N), dtype=torch.float32, device=X.device)
     nb = slim_linear_hybrid_workspace(M, N, K)
-    ws = None
-    if nb:
-        # its own cache: the split partials must not land in slim_linear's workspace, whose counter
-        # region has to stay zero between calls
-        key = (X.device, _stream(stream))
-        ws = _hybrid_ws.get(key)
-        if ws is None or ws.numel() < nb:
-            ws = torch.empty(nb, dtype=torch.uint8, device=X.device)
-            _hybrid_ws[key] = ws
+    ws = _hybrid_workspace(nb, X.device, stream) if nb else None
     _check(slim_linear_hybrid(_ptr(X), M, N, K, _ptr(p["tile_info"]), _ptr(p["payload"]), p["payload"].numel(),
                               _ptr(Y), _ptr(ws), nb, _stream(stream)), "slim_linear_hybrid")
     return Y

@@ -1,5 +1,6 @@
 """Graphs of calls that were given no workspace, replayed after larger calls on the stream of their capture: right results, and
 no write to memory that others hold by then."""
+import numpy as np
 import pytest
 import torch
 
@@ -119,3 +120,12 @@ def test_a_given_stream_clears_its_workspace():
     s.synchronize()
     assert torch.equal(got, want) and slim.workspace(1, a.device, s).is_cuda
     assert s.cuda_stream in {stream for dev, stream in slim._ws_cache}
+
+
+def test_linear_hybrid():
+    # a reduction in splits, whose partials are in the workspace
+    kinds = np.ones((4, 32), dtype=np.uint8)
+    p = slim.pack_hybrid(torch.randn((512, 4096), generator=torch.Generator("cuda").manual_seed(0), device="cuda"), kinds)
+    a, b = rows(128, 4096).half(), rows(2048, 4096, 1).half()
+    assert 0 < slim.slim_linear_hybrid_workspace(128, 512, 4096) < slim.slim_linear_hybrid_workspace(2048, 512, 4096)
+    replays_keep_to_their_own(lambda: slim.linear_hybrid(a, p), lambda: slim.linear_hybrid(b, p), lambda y: [y])

@@ -52,3 +52,30 @@ def test_the_compressed_layer(capture, monkeypatch):
     assert slim.workspace(100000, "cpu") is kept
     grown = slim.workspace(1 << 20, "cpu")
     assert not overlap(grown, mine) and not grown.any()
+
+
+def test_the_hybrid_layer(capture, monkeypatch):
+    dev = torch.device("cpu")
+    sizes = []
+
+    def call(nbytes):
+        """The workspace that linear_hybrid takes for a call that needs nbytes."""
+        given = []
+        monkeypatch.setattr(slim, "slim_linear_hybrid_workspace", lambda M, N, K: nbytes)
+        monkeypatch.setattr(slim, "slim_linear_hybrid", lambda *a: given.append((a[8], a[9])) or slim.SLIM_OK)
+        slim.linear_hybrid(x, {"N": 128, "K": 128, "tile_info": x, "payload": x})
+        sizes.append(given[0][1])
+        return given[0][0]
+
+    monkeypatch.setattr(slim, "_on_gpu", lambda *ts: None)
+    monkeypatch.setattr(slim, "_stream", lambda stream=None: STREAM)
+    monkeypatch.setattr(slim, "_hybrid_ws", {})
+    x = torch.zeros((2, 128), dtype=torch.float16)
+    kept = call(1000)
+    assert call(1000) == kept == slim._hybrid_ws[(dev, STREAM)].data_ptr()
+    capture(True)
+    assert call(1000) != kept
+    call(1 << 20)
+    capture(False)
+    assert call(1000) == kept == slim._hybrid_ws[(dev, STREAM)].data_ptr()
+    assert sizes == [1000, 1000, 1000, 1 << 20, 1000]
