@@ -552,8 +552,11 @@ int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int
 
 /*
  * slim_grad_w8 - the weight gradient dY^T X with X [M, K] an 8-bit checkpoint (xcodes, xexps).
- *   dY, dtype   [M, N], SLIM_F16 or SLIM_BF16, row stride lddy. X is widened to the same type (exact
- *               in bf16; in fp16 as slim_dequant8); products are exact, sums fp32 along M.
+ *   dY, dtype   [M, N], SLIM_F16 or SLIM_BF16, row stride lddy. X is widened to the same type: exact in
+ *               bf16 from 2^-133 on; in fp16 values below its normal range are rounded to multiples of
+ *               2^-24, and in a group of 128 columns with values past 448 2^7 to less than 2^-39 of its
+ *               largest over the rows (no value of X is lost to fp16's range). Products are exact, sums
+ *               fp32 along M.
  *   meta        NULL: gW fp32 [N, K], all of it. Else the index words of a value pack (slim_pack16,
  *               [N, K/8], K % 16 == 0): gW fp32 [N, K/2] at the positions they keep, as slim_grad_w.
  *   ws          slim_grad_w8_workspace(M, N, K, meta != NULL, aligned) bytes, where `aligned` says that

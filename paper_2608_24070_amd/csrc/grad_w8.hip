@@ -2,8 +2,14 @@
 //
 // D[k][n] = sum_m X[m][k] dY[m][n] (= grad W^T). The reduction runs along the stored rows of both operands, so a power of
 // two for each row and group cannot be taken out of the sum: the codes are widened to dY's 16-bit type with their exponent
-// on the way into LDS (exact in bf16, and in fp16 for checkpoints of fp16 values below 63488), and the products run on
-// v_mfma_f32_32x32x16 with fp32 accumulators. X moves at half the bytes of a 16-bit activation.
+// on the way into LDS, and the products run on v_mfma_f32_32x32x16 with fp32 accumulators. X moves at half the bytes of a
+// 16-bit activation.
+//
+// Widening is exact in bf16. fp16 holds 448 2^7 at most, so that where a block's rows have a larger exponent than 7 in a group
+// of 128 columns, it lowers all of that group's exponents by `down`, as much as the largest needs, and multiplies the group's
+// sums by 2^down at the end: finite gradients stay finite (fp16 activations come there from 63488 on, whose nearest code is
+// 65536). Values below fp16's normal range are rounded to its steps, 2^-24, or 2^(down - 24) in such a group: less than 2^-39
+// of the group's largest value.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <type_traits>
@@ -18,6 +24,7 @@ typedef short s4_t __attribute__((ext_vector_type(4)));
 namespace {
 
 constexpr int kWM = 32;       // rows of one chunk of the reduction
+constexpr uint32_t kTop16 = 127 + 7;      // the largest exponent byte whose values fp16 holds
 
 template <int DT>
 SLIM_DEV f16_t mfma_acc(u32x2_t a0, u32x2_t a1, u32x2_t b0, u32x2_t b1, f16_t c) {
@@ -81,6 +88,61 @@ SLIM_DEV void store_rows(float* gW, bool masked, const uint32_t (&byte)[COUNT], 
 template <int DT, int HI>
 SLIM_DEV uint32_t widen2(uint32_t c, float s);
 
+// Barrier of a block's LDS accesses that leaves loads from memory in flight.
+SLIM_DEV void sync_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// fp16: what the exponents of a group, or of GROUPS = 2 next to each other, are lowered by, found by a block of THREADS threads
+// from their bytes (the first at xe + at, a multiple of GROUPS, for `rows` rows ge bytes apart, ge a multiple of four). FLY loads a
+// thread are issued at construction and, for most calls all there are, land while the block's first operands are on their way.
+template <int THREADS, int FLY, int GROUPS>
+struct Lowered {
+  uint32_t b[FLY], top[GROUPS] = {};
+  SLIM_DEV void load(const uint8_t* xe, uint32_t at, uint32_t ge, int64_t rows) {
+    const rsrc_t r = make_rsrc(xe, rows * ge);          // rows past the last read as zero
+    const uint32_t o = threadIdx.x * ge + at;
+#pragma unroll
+    for (int i = 0; i < FLY; ++i) {
+      if constexpr (GROUPS == 2) b[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, o + i * THREADS * ge, 0, 0);
+      else b[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r, o + i * THREADS * ge, 0, 0);
+    }
+  }
+  SLIM_DEV void take() {
+#pragma unroll
+    for (int i = 0; i < FLY; ++i)
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) top[g] = max(top[g], b[i] >> (8 * g) & 255u);
+  }
+  SLIM_DEV Lowered(const uint8_t* xe, uint32_t at, uint32_t ge, int64_t rows) {
+    load(xe, at, ge, rows);
+    while (rows > FLY * THREADS) {
+      take();
+      rows -= FLY * THREADS;
+      xe += (int64_t)(FLY * THREADS) * ge;
+      load(xe, at, ge, rows);
+    }
+  }
+  // `part`: LDS of GROUPS THREADS / 64 words that nothing else reads or writes up to the block's next barrier
+  SLIM_DEV void get(uint32_t* part, uint32_t (&down)[GROUPS]) {
+    take();
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      top[g] = wave_max_u32(top[g]);
+      if ((threadIdx.x & 63) == 0) part[g * (THREADS / 64) + (threadIdx.x >> 6)] = top[g];
+    }
+    sync_lds();
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) top[g] = max(top[g], part[g * (THREADS / 64) + w]);
+      down[g] = (uint32_t)__builtin_amdgcn_readfirstlane((int)__builtin_elementwise_sub_sat(top[g], kTop16));
+    }
+  }
+};
+
 template <int DT, int TK>
 __global__ void __launch_bounds__(512, 4)
 k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xe,
@@ -141,12 +203,13 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
   };
   uint8_t* const lx = lds + lds_at(row, xcol);
   uint8_t* const ly = lds + 2 * (kRows * 256) + lds_at(row, col);
+  uint32_t down[1] = {0};
   auto put = [&](const Stage& S, int z) {
     uint8_t* x = lx + z * (kRows * 256);
     uint8_t* y = ly + z * (kRows * 256);
     *reinterpret_cast<u32x4_t*>(y) = S.y0;
     *reinterpret_cast<u32x4_t*>(y + 16) = S.y1;
-    const float s = q8_pow2(S.e);
+    const float s = q8_pow2(DT == 0 ? __builtin_elementwise_sub_sat(S.e, down[0]) : S.e);
 #pragma unroll
     for (int h = 0; h < TK / 64; ++h)
       *reinterpret_cast<u32x4_t*>(x + 16 * h) = u32x4_t{widen2<DT, 0>(S.c[2 * h], s), widen2<DT, 1>(S.c[2 * h], s),
@@ -163,15 +226,10 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
   const uint8_t* ax[2] = {lds + lds_at(rr, wk + cr), lds + lds_at(rr, wk + 32 + cr)};
   const uint8_t* by[2] = {lds + 2 * (kRows * 256) + lds_at(rr, wn + cr), lds + 2 * (kRows * 256) + lds_at(rr, wn + 32 + cr)};
   Stage S[kAhead];
-  auto sync = [] {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-  };
   // a chunk in slot j % 2; after its barrier no wave reads the other slot, which the next chunk takes
   auto chunk = [&](auto jc) {
     constexpr int j = decltype(jc)::value, z = j & 1;
-    sync();
+    sync_lds();
     put(S[(j + 1) % kAhead], z ^ 1);
     load(S[(j + 1) % kAhead]);
 #pragma unroll
@@ -191,8 +249,17 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
         for (int y = 0; y < 2; ++y) acc[x][y] = mfma_acc<DT>(a[x][0], a[x][1], b[y][0], b[y][1], acc[x][y]);
     }
   };
+  if constexpr (DT == 0) {
+    Lowered<512, 4, 1> l(xe + mb * Ge, (uint32_t)(k0 / 128), (uint32_t)Ge, me - mb);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) load(S[i]);
+    for (int i = 0; i < kAhead; ++i) load(S[i]);
+    __builtin_amdgcn_sched_barrier(0);
+    l.get(reinterpret_cast<uint32_t*>(lds + kRows * 256), down);     // the second slot, written after the next barrier
+  } else {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load(S[i]);
+  }
   put(S[0], 0);
   load(S[0]);
   // chunks past the last are zeros
@@ -222,7 +289,8 @@ k_wgrad8(const uint16_t* __restrict__ dY, int64_t lddy, int64_t cols, const uint
       for (int i = 0; i < 16; ++i) {
         const f16_t& c = acc[i >> 3][(i >> 2) & 1];
         f4_t& t = tile[(nl + 32 * ((i >> 2) & 1)) * kSlots + ((sl + 8 * (i >> 3) + 2 * (i & 3)) ^ (nl & (kSlots - 1)))];
-        const f4_t v = {c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+        f4_t v = {c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+        if constexpr (DT == 0) v *= q8_pow2(127 + down[0]);
         if (g == kGroups - 1) t = v;
         else t += v;
       }
@@ -398,11 +466,12 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
     S.e[j] = __builtin_amdgcn_raw_buffer_load_b8(re, or_past(c, eo[j]), g * estep, 0);
   };
   // step i (0 .. 15) of a chunk's widening: two codes, and after each eighth the 16 bytes to LDS
+  uint32_t down[2] = {0, 0}, low = 0;       // of the tile's two groups, and of this thread's columns
   u32x4_t wide;
   auto put_x = [&](const Stage& S, auto zc, auto ic) {
     constexpr uint32_t off = decltype(zc)::value * kSlot;
     constexpr int i = decltype(ic)::value, j = i >> 3, h = (i >> 2) & 1, e = i & 3;
-    wide[e] = widen2<DT, e & 1>(S.x[j][2 * h + (e >> 1)], q8_pow2(S.e[j]));
+    wide[e] = widen2<DT, e & 1>(S.x[j][2 * h + (e >> 1)], q8_pow2(DT == 0 ? __builtin_elementwise_sub_sat(S.e[j], low) : S.e[j]));
     if constexpr (e == 3) {
       const uint32_t at = xw[j][h];
       const u32x4_t v = wide;
@@ -491,11 +560,23 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
     landed(A);
   };
   rebase(0);
-  each<4>([&](auto ic) { issue_y(0, I0{}, ic); });
-  each<4>([&](auto ic) { issue_y(1, I1{}, ic); });
-  each<4>([&](auto ic) { issue_y(2, I2{}, ic); });
-  each<2>([&](auto jc) { load_x(S[0], 0, jc); });
-  each<2>([&](auto jc) { load_x(S[1], 1, jc); });
+  auto first = [&] {
+    each<4>([&](auto ic) { issue_y(0, I0{}, ic); });
+    each<4>([&](auto ic) { issue_y(1, I1{}, ic); });
+    each<4>([&](auto ic) { issue_y(2, I2{}, ic); });
+    each<2>([&](auto jc) { load_x(S[0], 0, jc); });
+    each<2>([&](auto jc) { load_x(S[1], 1, jc); });
+  };
+  if constexpr (DT == 0) {
+    Lowered<256, 8, 2> l(xe, (uint32_t)(k0 / 128), Ge, M);
+    __builtin_amdgcn_sched_barrier(0);
+    first();
+    __builtin_amdgcn_sched_barrier(0);
+    l.get(reinterpret_cast<uint32_t*>(&pattern[0][0]), down);        // (written after the last product)
+    low = down[(tid >> 3) & 1];
+  } else {
+    first();
+  }
   each<16>([&](auto ic) { put_x(S[0], I0{}, ic); });
   each<16>([&](auto ic) { put_x(S[1], I1{}, ic); });
   each<2>([&](auto jc) { load_x(S[0], 2, jc); });
@@ -535,8 +616,9 @@ k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __re
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const f16_t& c = acc[i >> 3][2 * y2 + ((i >> 2) & 1)];
-      mine[((lane & 31) + 32 * ((i >> 2) & 1)) * 32 + ((8 * (i >> 3) + 2 * (i & 3) + (lane >> 5)) ^ (lane & 31))] =
-          f4_t{c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+      f4_t v = {c[4 * (i & 3)], c[4 * (i & 3) + 1], c[4 * (i & 3) + 2], c[4 * (i & 3) + 3]};
+      if constexpr (DT == 0) v *= q8_pow2(127 + down[wave & 1]);
+      mine[((lane & 31) + 32 * ((i >> 2) & 1)) * 32 + ((8 * (i >> 3) + 2 * (i & 3) + (lane >> 5)) ^ (lane & 31))] = v;
     }
     // Inside the matrix a store takes a few instructions: with one wave on a SIMD they are what the end of a tile costs
     // (rows of a step differ from the first's by a constant XOR and offset in LDS, by a uniform address in memory).
