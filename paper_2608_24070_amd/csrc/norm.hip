@@ -33,25 +33,34 @@ struct RowsOf {
 };
 
 // Vector `col` .. `col` + 7 of a row, zeros past its end. RAG: rows may end inside a vector (K % 8 != 0); the kernels are
-// built apart for it, since the tests of single elements cost the others their scalar registers.
-template <int DT, bool RAG>
+// built apart for it, since the tests of single elements cost the others their scalar registers. FILL: values of the row past its
+// end (a vector's first, or the row's; rows in 8 bits that end inside a vector have zeros there); whole vectors and 8-bit rows
+// are then loaded without a test (8-bit rows, 8192 x 8192: both launches 73 us, with it 93).
+template <int DT, bool RAG, bool FILL = false>
 SLIM_DEV Raw8<DT> load_raw8(const RowsOf& r, int64_t row, int64_t col, int64_t K) {
   Raw8<DT> o;
-  int n = RAG ? (int)(K - col) : col < K ? 8 : 0;
+  if constexpr (FILL) col = col < K ? col : 0;
+  int n = RAG ? (int)(K - col) : FILL || col < K ? 8 : 0;
   const int64_t i = row * r.ld + col;
-  if constexpr (RAG) asm volatile("" : "+v"(n));      // compared here, not held as masks over a caller's loop
+  if constexpr (RAG && !(FILL && DT == kQ8)) asm volatile("" : "+v"(n));      // compared here, not held as masks over a caller's loop
   if constexpr (DT == kQ8) {
     // rows are padded to whole groups with zeros
     o.c = u32x2_t{0, 0};
     o.s = 0.f;
-    if (n > 0) {
+    if (FILL || n > 0) {
       o.c = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint8_t*>(r.p) + i);
       o.s = q8_pow2(r.exps[row * ((r.ld + 511) / 512 * 4) + col / 128]);
     }
   } else if constexpr (DT == 2) {
     if (RAG) {
       float f[8];
-      load8<2>(r.p, i, n, f);
+      if (!FILL || n >= 8) {
+        load8<2>(r.p, i, n, f);
+      } else {
+        const float* p = reinterpret_cast<const float*>(r.p) + i;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = p[e < n ? e : 0];
+      }
       o.a = f4_t{f[0], f[1], f[2], f[3]};
       o.b = f4_t{f[4], f[5], f[6], f[7]};
     } else {
@@ -67,6 +76,9 @@ SLIM_DEV Raw8<DT> load_raw8(const RowsOf& r, int64_t row, int64_t col, int64_t K
     if (!RAG || n >= 8) {
       o.v = u32x4_t{0, 0, 0, 0};
       if (RAG || n > 0) __builtin_memcpy(&o.v, p, 16);
+    } else if (FILL) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o.v[e] = (uint32_t)p[2 * e < n ? 2 * e : 0] | (uint32_t)p[2 * e + 1 < n ? 2 * e + 1 : 0] << 16;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -95,6 +107,8 @@ SLIM_DEV void values8(const Raw8<DT>& o, float* f) {
 // xh = (x - mu) rstd of eight elements, the difference first: x rstd - mu rstd in one operation would leave a rounding of
 // mu rstd, which in rows far from zero with little or no variance passes xh itself. (The second operation for each element
 // hides behind memory: 8192 x 8192 in bf16 82.8 us for both launches before, 83.0 with it.)
+// Past a row's end dy is zero, but xh has to be finite for a sum over the row to leave it out, and of x = 0 it would be
+// -mu rstd: so x is loaded with FILL there.
 template <int DT>
 SLIM_DEV void xhat8(const Raw8<DT>& o, float mu, float rstd, float* f) {
   if constexpr (DT == kQ8) {
@@ -108,6 +122,21 @@ SLIM_DEV void xhat8(const Raw8<DT>& o, float mu, float rstd, float* f) {
     for (int e = 0; e < 8; ++e) f[e] = (f[e] - mu) * rstd;
   }
 }
+
+// What FILL leaves of rows in 8 bits that end inside a vector (RAG): the codes from the n-th on are set to the first one's, in
+// rows whose mu rstd is infinite (or NaN), few if any.
+template <int DT, bool RAG>
+SLIM_DEV void fill8(Raw8<DT>& o, int n) {
+  if constexpr (DT == kQ8 && RAG) {
+    if (n < 8) {
+      const uint64_t keep = (uint64_t(1) << (8 * n)) - 1, first = (uint64_t)((o.c[0] & 255u) * 0x01010101u);
+      const uint64_t c = (((uint64_t)o.c[1] << 32 | o.c[0]) & keep) | ((first << 32 | first) & ~keep);
+      o.c = u32x2_t{(uint32_t)c, (uint32_t)(c >> 32)};
+    }
+  }
+}
+template <int DT, bool RAG>
+SLIM_DEV bool needs_fill8(float mu, float rstd) { return DT == kQ8 && RAG && !(fabsf(mu * rstd) < __builtin_inff()); }
 
 // Eight parameters (gamma, beta) as fp32; `none` where there are none.
 template <bool RAG>
@@ -397,7 +426,7 @@ k_norm_bwd(NormBwdArgs a) {
     const int64_t col = (int64_t)(v * T + t) * 8;
     if (AHEAD && first < a.M) {
       ny[v] = load_raw8<DT, RAG>(a.dy, first, col, a.K);
-      nx[v] = load_raw8<XT, RAG>(a.x, first, col, a.K);
+      nx[v] = load_raw8<XT, RAG, true>(a.x, first, col, a.K);
     }
     if constexpr (HOLD) params8<RAG>(a.gamma, a.pdt, col, a.K, 1.f, gm[v]);
 #pragma unroll
@@ -416,14 +445,20 @@ k_norm_bwd(NormBwdArgs a) {
         x[v] = nx[v];
       } else {
         y[v] = load_raw8<DT, RAG>(a.dy, row, (int64_t)(v * T + t) * 8, a.K);
-        x[v] = load_raw8<XT, RAG>(a.x, row, (int64_t)(v * T + t) * 8, a.K);
+        x[v] = load_raw8<XT, RAG, true>(a.x, row, (int64_t)(v * T + t) * 8, a.K);
       }
     }
     if (AHEAD && row + step < a.M)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         ny[v] = load_raw8<DT, RAG>(a.dy, row + step, (int64_t)(v * T + t) * 8, a.K);
-        nx[v] = load_raw8<XT, RAG>(a.x, row + step, (int64_t)(v * T + t) * 8, a.K);
+        nx[v] = load_raw8<XT, RAG, true>(a.x, row + step, (int64_t)(v * T + t) * 8, a.K);
+      }
+    if (needs_fill8<XT, RAG>(mu, rstd))
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int n = (int)a.K - (v * T + t) * 8;
+        fill8<XT, RAG>(x[v], n > 0 ? n : (int)a.K);          // vectors past the end hold the row's first
       }
     float st = 0.f, sx = 0.f;
 #pragma unroll
@@ -435,7 +470,7 @@ k_norm_bwd(NormBwdArgs a) {
       if constexpr (!HOLD) params8<RAG>(a.gamma, a.pdt, (int64_t)(v * T + t) * 8, a.K, 1.f, gm[0]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float tt = d[e] * gm[g][e];     // zero past K, where h does not matter
+        const float tt = d[e] * gm[g][e];     // zero past K
         st += tt;
         sx = fmaf(tt, h[e], sx);
         dg[v][e] = fmaf(d[e], h[e], dg[v][e]);
@@ -504,13 +539,15 @@ k_norm_bwd_long(NormBwdArgs a) {
   for (int64_t col = threadIdx.x * 8; col < a.K; col += 8192) {
     float d[8], h[8], g[8], p = 0.f, q = 0.f;
     values8<DT>(load_raw8<DT, true>(a.dy, row, col, a.K), d);
-    values8<XT>(load_raw8<XT, true>(a.x, row, col, a.K), h);
+    Raw8<XT> x = load_raw8<XT, true, true>(a.x, row, col, a.K);
+    if (needs_fill8<XT, true>(mu, rstd)) fill8<XT, true>(x, (int)(a.K - col));
+    xhat8<XT>(x, mu, rstd, h);
     params8<true>(a.gamma, a.pdt, col, a.K, 1.f, g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float tt = d[e] * g[e];
       p += tt;
-      q = fmaf(tt, (h[e] - mu) * rstd, q);
+      q = fmaf(tt, h[e], q);
     }
     st += p;
     sx += q;
@@ -520,10 +557,10 @@ k_norm_bwd_long(NormBwdArgs a) {
   for (int64_t col = threadIdx.x * 8; col < a.K; col += 8192) {
     float d[8], h[8], g[8];
     values8<DT>(load_raw8<DT, true>(a.dy, row, col, a.K), d);
-    values8<XT>(load_raw8<XT, true>(a.x, row, col, a.K), h);
+    xhat8<XT>(load_raw8<XT, true>(a.x, row, col, a.K), mu, rstd, h);
     params8<true>(a.gamma, a.pdt, col, a.K, 1.f, g);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-mx, (h[e] - mu) * rstd, fmaf(d[e], g[e], -mt));
+    for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-mx, h[e], fmaf(d[e], g[e], -mt));
     store_row8<DT, true>(a.dx, nullptr, row, a.lddx, col, a.K, d);
   }
 }
@@ -543,7 +580,7 @@ k_norm_bwd_dx(NormBwdArgs a) {
   for (int v = 0; v < V; ++v) {
     const int64_t col = (int64_t)(v * 1024 + threadIdx.x) * 8;
     y[v] = load_raw8<DT, false>(a.dy, row, col, a.K);
-    x[v] = load_raw8<XT, false>(a.x, row, col, a.K);
+    x[v] = load_raw8<XT, false, true>(a.x, row, col, a.K);
   }
   float st = 0.f, sx = 0.f;
 #pragma unroll
@@ -676,8 +713,9 @@ void norm_bwd_rows_of(const NormBwdArgs& a, hipStream_t s) {
   else if (a.K <= 1024) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 64, 2, true, true, RAG>), dim3(blocks), dim3(256), s, a);
   else if (a.K <= 4096) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 256, 2, true, true, RAG>), dim3(blocks), dim3(256), s, a);
   else if (a.K <= 8192) SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 256, 4, true, true, RAG>), dim3(blocks), dim3(256), s, a);
+  // (8-bit rows that end inside a vector without the next row ahead, which would spill: 2000 x 12287 44 us, 53 with it)
   else if (a.K <= 16384 && !(RAG && DT == 2))
-    SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 512, 4, DT != 2, DT != 2, RAG && DT != 2>), dim3(blocks), dim3(512), s, a);
+    SLIM_LAUNCH(timer, (k_norm_bwd<DT, XT, 512, 4, DT != 2, DT != 2 && !(RAG && XT == kQ8), RAG && DT != 2>), dim3(blocks), dim3(512), s, a);
   else {
     // the column sums first: dX may be written over dY
     SLIM_LAUNCH(timer, (k_norm_bwd_long_cols<DT, XT>), dim3((unsigned)((a.K + 2047) / 2048), blocks), dim3(256), s, a);
