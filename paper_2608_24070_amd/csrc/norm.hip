@@ -673,8 +673,11 @@ k_norm_cols(const float* __restrict__ part, int blocks, int64_t K, float* __rest
 bool float_type(int dt) { return dt == SLIM_F16 || dt == SLIM_BF16 || dt == SLIM_F32; }
 size_t elem(int dt) { return dt == SLIM_F32 ? 4 : 2; }
 
-// Rows past 16384 may take a block of 1024 threads each, and a launch holds fewer than 2^32 threads.
-bool too_many(int64_t M, int64_t K) { return K > 16384 && M >= int64_t(1) << 22; }
+// Rows past 16384, and in the backward fp32 rows past 8192 that end inside a vector, may take a block of 1024 threads each, and a
+// launch holds fewer than 2^32 threads.
+constexpr int64_t kMostLong = int64_t(1) << 22;
+bool too_many(int64_t M, int64_t K) { return K > 16384 && M >= kMostLong; }
+bool too_many_bwd(int64_t M, int64_t K, int dtype) { return dtype == SLIM_F32 && K > 8192 && K % 8 && M >= kMostLong; }
 
 template <int DT, int YT, bool RAG>
 void norm_rows(const NormArgs& a, SlimKernelTimer& timer, hipStream_t s) {
@@ -774,6 +777,7 @@ extern "C" int slim_norm_bwd(const void* dY, int dtype, int64_t lddy, const void
   const bool q8 = xdtype == SLIM_Q8_E4M3;
   if (!float_type(dtype) || !float_type(pdtype) || (xdtype != dtype && !q8)) return SLIM_EDTYPE;
   if (lddy < K || (!q8 && ldx < K) || lddx < K) return SLIM_ESHAPE;
+  if (too_many_bwd(M, K, dtype)) return SLIM_EUNSUPPORTED;
   if (M > 0 && (!dY || !X || !rstd || !dX || (q8 && !xexps))) return SLIM_EINVAL;
   if (!slim_aligned_to(dY, elem(dtype)) || !slim_aligned_to(X, q8 ? 16 : elem(dtype)) || !slim_aligned16(xexps) ||
       !slim_aligned_to(gamma, elem(pdtype)) || !slim_aligned_to(mean, 4) || !slim_aligned_to(rstd, 4) ||
