@@ -512,8 +512,9 @@ int slim_linear_hybrid(const void* X, int64_t M, int64_t N, int64_t K, const uin
  * sums over rows are zero. Rows are at most 2^22 columns. What one launch cannot take returns
  * SLIM_EUNSUPPORTED: 2^29 groups in slim_quant8 and slim_dequant8, 2^22 rows of more than 16384 columns
  * in the norms (slim_norm_bwd in fp32: of more than 8192 that are no multiple of 8), 2^36 elements of dY
- * in slim_grad_w8. Every call is asynchronous, allocates nothing, may
- * be captured into a graph, and gives the same bits for the same inputs.
+ * in slim_grad_w8, 2^23 tiles in slim_grad_w8 and 2^24 in slim_linear8 (2^36 results at least). Every call
+ * is asynchronous, allocates nothing, may be captured into a graph, and gives the same bits for the same
+ * inputs.
  * ----
  *
  * slim_quant8 - X [M, K] (`dtype` SLIM_F16, SLIM_BF16 or SLIM_F32, row stride ldx) in 8 bits.

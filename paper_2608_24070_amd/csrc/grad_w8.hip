@@ -715,11 +715,14 @@ GradPlan grad_plan(int64_t M, int64_t N, int64_t K, bool masked, bool aligned) {
   return p;
 }
 
-int check_grad(int64_t M, int64_t N, int64_t K, bool masked) {
+int check_grad(int64_t M, int64_t N, int64_t K, bool masked, bool aligned, GradPlan* p) {
   if (M < 0 || N < 1 || K < 1 || N > kMaxRow8 || K > kMaxRow8 || (masked && K % 16)) return SLIM_ESHAPE;
   if (cdiv(N, 128) * cdiv(K, 128) > 0x7FFFFFFF || M >= (int64_t(1) << 31) || M > ((int64_t(1) << 32) - 256) / cdiv(N, 16))      // (pieces of a copy are counted in 32 bits)
     return SLIM_EUNSUPPORTED;
-  return SLIM_OK;
+  *p = grad_plan(M, N, K, masked, aligned);
+  const bool fits = p->wide ? one_launch(8 * cdiv(cdiv(N, 256) * cdiv(K, 256), 8), 256)
+                            : one_launch(cdiv(N, 128) * cdiv(K, p->narrow ? 64 : 128), 512);
+  return fits ? SLIM_OK : SLIM_EUNSUPPORTED;
 }
 
 template <int DT>
@@ -763,23 +766,24 @@ bool aligned_rows(const void* dY, int64_t lddy) { return slim_aligned16(dY) && l
 
 extern "C" int slim_grad_w8_workspace(int64_t M, int64_t N, int64_t K, int masked, int aligned, size_t* bytes) {
   if (!bytes) return SLIM_EINVAL;
-  const int rc = check_grad(M, N, K, masked != 0);
+  GradPlan p;
+  const int rc = check_grad(M, N, K, masked != 0, aligned != 0, &p);
   if (rc != SLIM_OK) return rc;
-  *bytes = grad_plan(M, N, K, masked != 0, aligned != 0).bytes;
+  *bytes = p.bytes;
   return SLIM_OK;
 }
 
 extern "C" int slim_grad_w8(const void* dY, int dtype, int64_t lddy, const uint8_t* xcodes, const uint8_t* xexps, int64_t M,
                             int64_t N, int64_t K, const uint8_t* meta, float* gW, void* ws, size_t ws_bytes, void* stream) {
   if (dtype != SLIM_F16 && dtype != SLIM_BF16) return SLIM_EDTYPE;
-  const int rc = check_grad(M, N, K, meta != nullptr);
+  GradPlan p;
+  const int rc = check_grad(M, N, K, meta != nullptr, aligned_rows(dY, lddy), &p);
   if (rc != SLIM_OK) return rc;
   if (lddy < N) return SLIM_ESHAPE;
   if (!gW || (M > 0 && (!dY || !xcodes || !xexps))) return SLIM_EINVAL;
   if (!slim_aligned_to(dY, 2) || !slim_aligned16(xcodes) || !slim_aligned16(xexps) || !slim_aligned16(meta) ||
       !slim_aligned16(gW))
     return SLIM_EALIGN;
-  const GradPlan p = grad_plan(M, N, K, meta != nullptr, aligned_rows(dY, lddy));
   if (p.bytes && (!ws || ws_bytes < p.bytes)) return SLIM_EWORKSPACE;
   if (p.bytes && !slim_aligned16(ws)) return SLIM_EALIGN;
   const uint16_t* y = reinterpret_cast<const uint16_t*>(dY);

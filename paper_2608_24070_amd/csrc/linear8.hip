@@ -587,7 +587,10 @@ extern "C" int slim_linear8_workspace(int xdtype, int64_t M, int64_t N, int64_t 
   if (rc != SLIM_OK) return rc;
   *bytes = 0;
   if (M == 0 || quant_in_launch(xdtype, M, K)) return SLIM_OK;
-  *bytes = plan(M, N, K).bytes;
+  const Plan p = plan(M, N, K);
+  const TileKind& k = kTiles[p.kind];
+  if (!p.few && !one_launch(8 * cdiv(cdiv(M, 16 * k.fm) * cdiv(N, 64 * k.wn), 8), 256)) return SLIM_EUNSUPPORTED;
+  *bytes = p.bytes;
   if (xdtype != SLIM_Q8_E4M3) *bytes += code_bytes(M, K) + round256((size_t)M * (size_t)q8_exp_row(K));
   return SLIM_OK;
 }

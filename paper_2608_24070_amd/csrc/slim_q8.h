@@ -12,6 +12,9 @@ constexpr int64_t kMaxRow8 = int64_t(1) << 22;
 constexpr int64_t kMaxGroups8 = (int64_t(1) << 32) - 64;
 constexpr int64_t kMaxQuant8 = (int64_t(1) << 29) - 64;
 
+// Whether one launch takes so many blocks side by side: it holds fewer than 2^32 threads.
+constexpr bool one_launch(int64_t blocks, int64_t threads) { return blocks < (int64_t(1) << 32) / threads; }
+
 // Fitted sizes: codes per row (whole groups) and exponent bytes per row (whole 32-bit words).
 constexpr int64_t q8_row(int64_t k) { return (k + 127) / 128 * 128; }
 constexpr int64_t q8_exp_row(int64_t k) { return (k + 511) / 512 * 4; }
