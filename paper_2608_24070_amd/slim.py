@@ -830,12 +830,21 @@ def _vector(t, n: int, dev: int, what: str):
         raise ValueError(f"{what} must be on device {dev}")
 
 
+def _bytes_on_gpu(*ts):
+    """Codes, exponents and index words: uint8, whose bytes are what they mean. (Values of another type would be read as such.)"""
+    u8 = _torch().uint8
+    for t in ts:
+        if t.dtype is not u8:
+            raise TypeError(f"codes, exponents and index words must be uint8, got {t.dtype}")
+    _on_gpu(*ts)
+
+
 def _rows8(q: dict, dev: int | None = None):
     """Checked parts of 8-bit rows: codes, exps, M, K, device (`dev` if given)."""
     codes, exps, M, K = q["codes"], q["exps"], q["M"], q["K"]
     if codes.shape != (M, (K + 127) // 128 * 128) or exps.shape != (M, (K + 511) // 512 * 4):
         raise ValueError("codes and exponents do not have the shape of the 8-bit rows")
-    _on_gpu(codes, exps)
+    _bytes_on_gpu(codes, exps)
     d = codes.get_device()
     if d != exps.get_device() or (dev is not None and d != dev):
         raise ValueError("8-bit rows must be on one device with the other tensors")
@@ -938,7 +947,7 @@ def _given8(nbytes: int, ws, like, stream: int):
 def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, where: str):
     if codes.shape != ((N + 15) // 16, (K + 127) // 128, 2, 4, 16, 16) or exps.shape != ((N + 127) // 128, (K + 511) // 512 * 4):
         raise ValueError("codes and exponents do not have the shape of the 8-bit weight")
-    _on_gpu(codes, exps)
+    _bytes_on_gpu(codes, exps)
     if type(X) is dict:
         x, xe, M, k, dev = _rows8(X)
         xe, xdt, ldx = xe.data_ptr(), SLIM_Q8_E4M3, 0
@@ -998,7 +1007,7 @@ def grad_w8(dY, q: dict, p: dict | None = None, out=None, ws=None, stream=None):
         meta, cols = p["meta"], K // 2
         if meta.shape != (N, K // 8):
             raise ValueError("the value pack does not match dY and the checkpoint")
-        _on_gpu(meta)
+        _bytes_on_gpu(meta)
         if meta.get_device() != dev:
             raise ValueError("dY and the value pack must be on one device")
         meta = meta.data_ptr()
