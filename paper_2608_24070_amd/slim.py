@@ -606,7 +606,7 @@ def linear(X, packed: dict, adapter: dict | None = None, out=None, ws=None, stre
     torch = _torch()
     Lt = None if adapter is None else adapter["Lt"]
     Rt = None if adapter is None else adapter["Rt"]
-    _on_gpu(X, Lt, Rt, out)
+    _on_gpu(X, Lt, Rt, out, ws)
     M, K = X.shape
     N = packed["N"]
     r = 0 if Lt is None else Lt.shape[0]
@@ -624,7 +624,7 @@ def linear(X, packed: dict, adapter: dict | None = None, out=None, ws=None, stre
 def bwd_dx(dY, packed_bwd: dict, L=None, R=None, out=None, ws=None, stream=None):
     """dX = dY W^{R,C} + (dY R^T) L^T through slim_linear_bwd_dx. dX fp32 [M, K]."""
     torch = _torch()
-    _on_gpu(dY, L, R, out)
+    _on_gpu(dY, L, R, out, ws)
     M, N = dY.shape
     K = packed_bwd["K"]
     r = 0 if L is None else L.shape[1]
@@ -678,7 +678,7 @@ def pack_adapter_q(L, R, stream=None) -> dict:
 def linear_qa(X, packed: dict, qadapter: dict, out=None, ws=None, stream=None):
     """Y = X Wc^T + (X L^Q) R^Q through slim_linear_qa (qadapter from pack_adapter_q). Y fp32 [M, N]."""
     torch = _torch()
-    _on_gpu(X, out)
+    _on_gpu(X, out, ws)
     M, K = X.shape
     N, r = packed["N"], qadapter["r"]
     if out is None:
@@ -941,7 +941,11 @@ def _given8(nbytes: int, ws, like, stream: int):
         if not nbytes:
             return None, 0
         ws = _workspace8(nbytes, like, stream)
-    return ws.data_ptr(), ws.numel()
+        return ws.data_ptr(), ws.numel()
+    _on_gpu(ws)
+    if ws.get_device() != like.get_device():
+        raise ValueError("the workspace must be on the tensors' device")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, where: str):

@@ -44,3 +44,53 @@ def test_codes_and_exponents_are_bytes(on_gpu, kw):
             call(rows8(), weight8())
         with pytest.raises(TypeError, match="uint8"):
             call(rows8(**kw), weight8(**kw))
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it is on a device."""
+    is_cuda = True
+
+    def get_device(self):
+        return 0
+
+
+def test_a_given_workspace_is_device_memory_of_its_size():
+    gpu = lambda t: t.as_subclass(OnGpu)
+    like = gpu(torch.zeros(1))
+    ws = gpu(torch.zeros(4096, dtype=torch.uint8))
+    assert slim._given8(4000, ws, like, 0) == (ws.data_ptr(), 4096)
+    assert slim._given8(0, None, like, 0) == (None, 0)
+    wide = gpu(torch.zeros(1024))
+    assert slim._given8(4000, wide, like, 0) == (wide.data_ptr(), 4096)
+    for bad in (torch.zeros(4096, dtype=torch.uint8),                  # on the host
+                gpu(torch.zeros(1, dtype=torch.uint8)).expand(4096),   # one byte
+                gpu(torch.zeros(8192, dtype=torch.uint8))[::2]):
+        with pytest.raises(ValueError):
+            slim._given8(4000, bad, like, 0)
+
+
+class Elsewhere(OnGpu):
+    def get_device(self):
+        return 1
+
+
+def test_a_given_workspace_is_on_the_tensors_device():
+    with pytest.raises(ValueError, match="device"):
+        slim._given8(10, torch.zeros(4096, dtype=torch.uint8).as_subclass(Elsewhere), torch.zeros(1).as_subclass(OnGpu), 0)
+
+
+def test_the_compressed_layer_looks_at_its_workspace_too(monkeypatch):
+    seen = []
+
+    def record(*ts):
+        seen.extend(ts)
+        raise Reached
+
+    monkeypatch.setattr(slim, "_on_gpu", record)
+    x, ws = torch.zeros((4, 256), dtype=torch.bfloat16), torch.zeros(8)
+    for call in (lambda: slim.linear(x, {"N": 32}, ws=ws), lambda: slim.bwd_dx(x, {"K": 32}, ws=ws),
+                 lambda: slim.linear_qa(x, {"N": 32}, {"r": 32}, ws=ws)):
+        seen.clear()
+        with pytest.raises(Reached):
+            call()
+        assert any(t is ws for t in seen)
