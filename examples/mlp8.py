@@ -116,6 +116,7 @@ def main():
     # single tokens, captured once and replayed
     one = x[:1].clone()
     side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())      # for `one` and the weights
     with torch.cuda.stream(side):
         model.forward(one, keep=False)
     side.synchronize()
