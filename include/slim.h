@@ -518,8 +518,10 @@ int slim_linear_hybrid(const void* X, int64_t M, int64_t N, int64_t K, const uin
  * ----
  *
  * slim_quant8 - X [M, K] (`dtype` SLIM_F16, SLIM_BF16 or SLIM_F32, row stride ldx) in 8 bits.
- * slim_dequant8 - the values back in `dtype`, row stride ldy: exact in fp32 and bf16; in fp16
- *   rounded to nearest (exact for values that came from fp16 below 63488; past 65519 infinite).
+ * slim_dequant8 - the values back in `dtype`, row stride ldy, rounded to nearest: exact in fp32 and, from
+ *   2^-130 on, in bf16; in fp16 for values that came from fp16 below 63488. What passes the type's range is
+ *   infinite: in fp16 past 65519, in fp32 and bf16 values from 248 2^120 on (within 3 % of their largest),
+ *   whose nearest code is 256.
  */
 int slim_quant8(const void* X, int dtype, int64_t M, int64_t K, int64_t ldx, uint8_t* codes, uint8_t* exps, void* stream);
 int slim_dequant8(const uint8_t* codes, const uint8_t* exps, int64_t M, int64_t K, void* Y, int dtype, int64_t ldy,
@@ -544,8 +546,9 @@ int slim_pack8(const void* W, int dtype, int64_t N, int64_t K, int64_t ldw, uint
  *   ws          slim_linear8_workspace(xdtype, M, N, K) bytes (0 when the call needs none); its
  *               contents need not be kept or cleared.
  * Sums are fp32, but for those of each eight consecutive products, which the scaled matrix instructions
- * cut at 2^-13 of the largest of them: together 1.5e-5 of the result's norm, before Y is rounded to
- * 16 bits. For that reason fp32 is not offered for Y.
+ * cut at 2^-13 of the largest of them: together 2e-5 of the result's norm, 4.5e-5 where a hundredth of X's
+ * channels is twenty times the rest, before Y is rounded to 16 bits (2e-4 in fp16, 1.7e-3 in bf16). For
+ * that reason fp32 is not offered for Y.
  */
 int slim_linear8_workspace(int xdtype, int64_t M, int64_t N, int64_t K, size_t* bytes);
 int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t N, int64_t K, int64_t ldx,
@@ -555,7 +558,7 @@ int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int
 /*
  * slim_grad_w8 - the weight gradient dY^T X with X [M, K] an 8-bit checkpoint (xcodes, xexps).
  *   dY, dtype   [M, N], SLIM_F16 or SLIM_BF16, row stride lddy. X is widened to the same type: exact in
- *               bf16 from 2^-133 on; in fp16 values below its normal range are rounded to multiples of
+ *               bf16 from 2^-130 on; in fp16 values below its normal range are rounded to multiples of
  *               2^-24, and in a group of 128 columns with values past 448 2^7 to less than 2^-39 of its
  *               largest over the rows (no value of X is lost to fp16's range). Products are exact, sums
  *               fp32 along M.

@@ -10,8 +10,9 @@ namespace {
 // --------------------------------------------------------------------------- activations
 // One group of 128 consecutive values of a row per 8 lanes, 16 values a lane: the group's largest magnitude over the
 // eight lanes, its exponent, and 16 codes a lane in one 16-byte store. Groups are numbered row by row, so the lanes of a
-// wave read eight groups that follow each other. Bound by HBM (2 or 4 bytes in, 1 + 1/128 out per value): 8192 x 8192 in bf16
-// 31.4 us (6.4 TB/s), 8192 x 28672 124 us (5.7 TB/s), in fp32 8192 x 8192 55.6 us (6.0 TB/s); 1 x 4096 3.9 us.
+// wave read eight groups that follow each other. Bound by HBM (2 or 4 bytes in, 1 + 1/128 out per value). A launch by itself, X
+// from memory: 8192 x 8192 in bf16 36.5 us (5.5 TB/s), 8192 x 28672 127 us (5.6 TB/s), in fp32 8192 x 8192 57.8 us (5.8 TB/s);
+// 1 x 4096 5.5 us, 2.0 as one of many in a graph.
 template <int DT>
 __global__ void __launch_bounds__(256)
 k_quant8(const void* __restrict__ X, int64_t ldx, uint32_t K, uint32_t G, uint32_t total, uint8_t* __restrict__ codes,
@@ -37,8 +38,9 @@ k_quant8(const void* __restrict__ X, int64_t ldx, uint32_t K, uint32_t G, uint32
   else if (g == G - 1 && g + sub < Ge) exps[(int64_t)row * Ge + g + sub] = 0;   // the row's last word ends in zeros
 }
 
-// The values codes stand for, 16 a lane, in the order of k_quant8; every one is exact in fp32 and in bf16. 8192 x 8192 to bf16
-// 31.0 us (6.5 TB/s), to fp32 76.6 us (4.4 TB/s; 16 values a lane side by side, 64 bytes, 99.9).
+// The values codes stand for, 16 a lane, in the order of k_quant8; every one below 2^128 is exact in fp32, and in bf16 from 2^-130
+// on (multiples of 2^-135 at e = -126). A launch by itself, codes from memory: 8192 x 8192 to bf16 34.4 us (5.9 TB/s), 8192 x 28672
+// 124 us, to fp32 8192 x 8192 75.9 us (4.4 TB/s; 16 values a lane side by side, 64 bytes, 99.9).
 template <int DT>
 __global__ void __launch_bounds__(256)
 k_dequant8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ exps, uint32_t K, uint32_t G, uint32_t total,
@@ -78,8 +80,8 @@ k_dequant8(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ exps, 
 // --------------------------------------------------------------------------- weights
 // One 128 x 128 block of W per workgroup: its largest magnitude, its exponent, and its codes as tiles of 16 rows x 128
 // reduction positions (see include/slim.h). Codes go through LDS row by row; the same LDS image read by columns gives
-// the transposed pack, whose blocks have the same exponents. Once a step at most: 28672 x 8192 from fp32 235 us, with both packs
-// 261 us (5.4 TB/s).
+// the transposed pack, whose blocks have the same exponents. Once a step at most: 28672 x 8192 from fp32 240 us, with both packs
+// 271 us (5.2 TB/s).
 // Piece i of 1024: 16 codes, row i / 8, columns 16 (i % 8) ..
 template <int DT>
 __global__ void __launch_bounds__(256)

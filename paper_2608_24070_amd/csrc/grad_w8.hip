@@ -5,7 +5,7 @@
 // on the way into LDS, and the products run on v_mfma_f32_32x32x16 with fp32 accumulators. X moves at half the bytes of a
 // 16-bit activation.
 //
-// Widening is exact in bf16. fp16 holds 448 2^7 at most, so that where a block's rows have a larger exponent than 7 in a group
+// Widening is exact in bf16 (from 2^-130 on). fp16 holds 448 2^7 at most, so that where a block's rows have a larger exponent than 7 in a group
 // of 128 columns, it lowers all of that group's exponents by `down`, as much as the largest needs, and multiplies the group's
 // sums by 2^down at the end: finite gradients stay finite (fp16 activations come there from 63488 on, whose nearest code is
 // 65536). Values below fp16's normal range are rounded to its steps, 2^-24, or 2^(down - 24) in such a group: less than 2^-39
@@ -84,7 +84,9 @@ SLIM_DEV void store_rows(float* gW, bool masked, const uint32_t (&byte)[COUNT], 
 // slice, which k_wgrad8_sum adds in slice order.
 // TK 128: two blocks a CU hide each other's LDS and barriers. TK 64: for layers of so few tiles that a block stands alone
 // on its CU anyway, where reads, products and writes of a chunk follow one another: half of each, on twice the CUs. 999 x 2051 x
-// 768 14.5 us, 0.5 us a chunk of 64 rows; 64 x 28672 x 8192 225 us with TK 128, of which writing the result is 184.
+// 768 14.7 us in bf16 and 15.2 in fp16 for a launch by itself, 13.3 and 13.8 where calls follow each other, 0.5 us a chunk of 64
+// rows; 64 x 28672 x 8192 226 us with TK 128, of which writing the result is 184. TK 64 has one block a CU and no read of LDS in
+// flight under its products: of the registers that a block alone on its CU could have, it uses half.
 template <int DT, int HI>
 SLIM_DEV uint32_t widen2(uint32_t c, float s);
 
@@ -378,9 +380,9 @@ SLIM_DEV uint32_t lds_at_wide(int r, int c) {
 // barrier a chunk, between its two 16-row steps, whose operands are read while the step before is multiplied. Columns past N
 // and K read what lies there or zero; their results are not stored.
 // Bound by the matrix unit, busy for 65 % of the cycles at the 1.6 GHz that the card then keeps (LDS for 33 %), and by its waits
-// for operands: 8192 x 8192 x 8192 in bf16 874 us (1.26 PFLOP/s; a library product of bf16 operands 1.23), 8192 x 28672 x 8192
-// at kept positions 2.87 ms (1.34). Over few rows the first loads and last stores of every round of tiles show: 512 x 28672 x
-// 8192 331 us, of which writing the result is 184; at kept positions 290.
+// for operands: 8192 x 8192 x 8192 in bf16 865 to 900 us by card (1.22 to 1.27 PFLOP/s; a library product of bf16 operands 1.23), in
+// fp16 2 % more; 8192 x 28672 x 8192 at kept positions 2.9 to 3.2 ms (1.2 to 1.3). Over few rows the first loads and last stores of
+// every round of tiles show: 512 x 28672 x 8192 343 us (fp16 356), of which writing the result is 184; at kept positions 311.
 template <int DT>
 __global__ void __launch_bounds__(256, 1)
 k_wgrad8_wide(const uint16_t* __restrict__ dY, int64_t lddy, const uint8_t* __restrict__ xc, const uint8_t* __restrict__ xe,

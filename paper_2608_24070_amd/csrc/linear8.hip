@@ -7,9 +7,13 @@
 // second. The weight is the first operand, so a lane's four results are four consecutive columns of Y.
 // Precision: the accumulators are fp32, but the unit adds the products of eight consecutive reduction positions (one lane's
 // eight bytes) first, aligned to the largest of them and cut towards zero below 2^-13 of its leading bit (found with single
-// pairs of products of known sizes; the unscaled fp8 instructions do the same); across the eights it keeps 24 bits. Against
-// 64 bits that is 1.5e-5 of the result's norm, at K 512 as at 8192. Y is rounded once to 16 bits, whose steps are 30 (fp16)
-// to 250 times (bf16) as large, so it costs Y nothing that shows; an fp32 Y would promise more than the unit holds.
+// pairs of products of known sizes; the unscaled fp8 instructions do the same); across the eights it keeps 24 bits. So each eight
+// lose less than 7 2^-13 of their largest product. Against 64 bits that is 2e-5 of the result's norm for operands of one size
+// throughout, and 4.5e-5 where a hundredth of X's channels is twenty times the rest; one sign in all operands leaves no bias that
+// shows (below 1e-6). Y's rounding to 16 bits is 2.1e-4 (fp16) and 1.7e-3 (bf16) of its norm: with both, 45 x 13824 x 5120 in fp16 is
+// 2.12e-4 from 64 bits where fp32 sums would be 2.07e-4, and one element in seven is the neighbouring fp16 value. The operands'
+// own rounding to e4m3 is some hundred times as large. An fp32 Y would promise more than the unit holds, and is not offered; exact
+// sums would take 16-bit products, at half the rate.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <type_traits>
@@ -71,7 +75,8 @@ SLIM_DEV void quant16(const void* X, int64_t at, int64_t left, u32x4_t& c, uint3
 // and add their sums through LDS in wave order. Nothing is shared within the reduction, so weight tiles (2 KiB of
 // consecutive bytes) and X fragments go straight from memory to registers, U groups of a wave in flight at once. Bound by
 // the weight's bytes, and for more than a few rows by those of X, which every block reads: two tiles a block halve them.
-// 28672 x 8192: M 1 40.3 us (5.8 TB/s), M 16 47.4; 4096 x 4096, M 1 9.8 us, of which a launch is half.
+// 28672 x 8192, M 1: 42.8 us (5.5 TB/s) for a launch by itself, operands from memory; 4096 x 4096, M 1 10.0 us, of which a launch
+// is half (7.0 as one of many in a graph).
 // XT: the type of X. 3 (codes): rows are read as they are. Otherwise every block first turns the whole of X into codes in
 // LDS, while its first weight tiles are on their way: worth it for the few rows whose codes fit kFewLds.
 constexpr int kFewLds = 32768;
@@ -199,11 +204,11 @@ SLIM_DEV int swizzle8(int row) { return ((row >> 1) & 7) ^ (((row >> 2) ^ (row >
 // 32-bit word (four groups) a row; the unit picks the group's byte by itself. Fragments of X are read three ahead of their
 // four MFMAs. LDS reads are written out with counted waits (the compiler cannot tell the ring's slots apart and would wait for
 // every load in flight). Rows and weight tiles past the ends repeat the last one; their results are not stored.
-// 256 x 256 tiles are bound by the matrix unit and by the power it draws: 8192 x 28672 x 8192 1.31 ms, 2.9 PFLOP/s (a library
-// product of unscaled fp8 2.66): it is busy for 78 % of the cycles (8192 x 8192 x 8192) at the 1.6 GHz that the card then keeps,
+// 256 x 256 tiles are bound by the matrix unit and by the power it draws: 8192 x 28672 x 8192 1.31 to 1.36 ms by card, 2.8 to
+// 2.9 PFLOP/s (a library product of unscaled fp8 2.66): it is busy for 78 % of the cycles (8192 x 8192 x 8192) at the 1.6 GHz that the card then keeps,
 // LDS for 22 %. Shorter tiles and parts of the reduction are for fewer rows, where the weight's bytes come to count: 512 x
-// 28672 x 8192 94 us (2.6 PFLOP/s), 64 x 28672 x 8192 52 us (4.5 TB/s of weights), 45 x 13824 x 5120 19.9 us, 2048 x 4096 x 4096
-// 34 us (2.0).
+// 28672 x 8192 98 us (2.5 PFLOP/s), 64 x 28672 x 8192 53 us (4.4 TB/s of weights), 16 x 28672 x 8192 48 us, 45 x 13824 x 5120 22 us
+// (weights from memory; a launch of k_quant8 before it, 4 us), 2048 x 4096 x 4096 34 us (2.0).
 template <int FM, int WN, int DT>
 __global__ void __launch_bounds__(256, 1)
 k_linear8_tile(const uint8_t* __restrict__ X, const uint8_t* __restrict__ ex, const uint8_t* __restrict__ W,

@@ -8,7 +8,7 @@
 // Every row is read once and stays in registers between its sums and its result; a block takes rows block by block, so
 // that gamma, beta and the column sums of the backward stay in registers too, and loads the next row before it works on
 // the present one. All arithmetic is fp32; y and dx are rounded once. Sums have a fixed order, so results repeat bit for
-// bit. Bound by HBM.
+// bit. Bound by HBM. Figures are of a launch by itself with its operands from memory, unless they say otherwise.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 
@@ -242,10 +242,11 @@ struct NormArgs {
 // Rows of up to 8 T V elements, T threads a row, V vectors of 8 a thread. Each wave sums its part of the row about its
 // own mean, and the waves' (count, mean, squares) are joined exactly as if about the row's mean: one barrier a row, and no
 // cancellation for rows far from zero. Means are quotients, not products with 1 / K, so that a row of one value has that
-// value as its mean wherever its sum is exact, and results of beta. HOLD: gamma and beta stay in registers from row to row; AHEAD: the next row is loaded
-// before the present one is worked on (both as registers allow).
-// Bound by memory: 8192 x 8192 in bf16 41.6 us (6.5 TB/s read and written), to 8 bits 46.9 us (4.3 TB/s); 2047 x 5120 in
-// fp16 15.0 us; one row of 4096 6.4 us, which is a launch and two trips to memory.
+// value as its mean wherever its sum is exact, and results of beta. HOLD: gamma and beta stay in registers from row to row;
+// AHEAD: the next row is loaded before the present one is worked on (both as registers allow).
+// Bound by memory: 8192 x 8192 in bf16 49.1 us (5.5 TB/s read and written), to 8 bits 57.2 us (3.5 TB/s); 2047 x 5120 in
+// fp16 16.5 us, 11.7 where calls follow each other; one row of 4096 6.4 us, which is a launch and two trips to memory, 3.1 as one
+// of many in a graph.
 template <int DT, int YT, int T, int V, bool HOLD, bool AHEAD, bool RAG>
 __global__ void __launch_bounds__(T == 64 ? 256 : T)
 k_norm(NormArgs a) {
@@ -344,7 +345,7 @@ k_norm(NormArgs a) {
 
 // Longer rows: one block a row reads it three times (mean, squares, result), the later times from the caches. Also ragged
 // rows past 16384, where a vector's tests for the row's end cost the kernel above its scalar registers: 2048 x 28671 in
-// bf16 79 us (28672 in registers: 57.6 us).
+// bf16 100 us (28672 in registers: 65.5 us).
 template <int DT, int YT>
 __global__ void __launch_bounds__(1024)
 k_norm_long(NormArgs a) {
@@ -408,7 +409,9 @@ struct NormBwdArgs {
 // As k_norm: T threads a row, V vectors a thread; dgamma's and dbeta's sums over the block's rows stay in registers and
 // leave as one row of partial sums a block (k_norm_cols adds those in block order). Rows of up to 8192 take 256 threads of
 // four vectors rather than 512 of two: two blocks share a CU and do not wait at one barrier (8192 x 8192 in bf16 79.0 and
-// 96.7 us). That is 5.1 TB/s; k_norm_cols takes another 5.8 us. 8192 x 4096 33.2 + 4.5, 2047 x 5120 in fp16 20.8 + 4.0.
+// 96.7 us). That is 5.1 TB/s; k_norm_cols takes another 5.8 us. From 8 bits 66.6 us (5.1 TB/s). 8192 x 4096 37.2 + 4.6 (from 8
+// bits 35.1), 2047 x 5120 in fp16 24.4 + 4.1, 333 x 1000 from 8 bits 8.2 + 7.0 (both launches in a graph 8.0). RMS norms take
+// dbeta's sums along: a row of registers and half of k_norm_cols' reading.
 template <int DT, int XT, int T, int V, bool HOLD, bool AHEAD, bool RAG>
 __global__ void __launch_bounds__(T == 64 ? 256 : T)
 k_norm_bwd(NormBwdArgs a) {
@@ -527,8 +530,8 @@ k_norm_bwd(NormBwdArgs a) {
   }
 }
 
-// Longer rows, second kernel: dx, one block a row, which reads it twice (400 x 65536 in bf16: 38.7 us). The column sums of
-// such rows do not fit the registers beside the row itself, and have a kernel of their own.
+// Longer rows, second kernel: dx, one block a row, which reads it twice (400 x 65536 in bf16: 41.7 us). The column sums of
+// such rows have a kernel of their own (24.3 us there).
 template <int DT, int XT>
 __global__ void __launch_bounds__(1024)
 k_norm_bwd_long(NormBwdArgs a) {
@@ -566,7 +569,9 @@ k_norm_bwd_long(NormBwdArgs a) {
 }
 
 // The same for whole vectors and rows of up to 32768: the row stays in registers between its sums and its result. 2048 x 28672
-// in bf16 72 us (read twice: 80), 4.9 TB/s, after 43 for the column sums; 3221 x 20832 in fp32 165 us (196).
+// in bf16 76 us, 4.6 TB/s, after 53 for the column sums (where calls follow each other 121 for all three launches); 3221 x 20832 in
+// fp32 159 us after 116. Read twice, dx took 80 us for 72, and 196 for 165. (The column sums would fit beside 16-bit and 8-bit rows
+// of up to 28672 with seven vectors a thread, and gamma read anew; that has not been built.)
 template <int DT, int XT>
 __global__ void __launch_bounds__(1024)
 k_norm_bwd_dx(NormBwdArgs a) {
