@@ -365,13 +365,21 @@ def _on_gpu(*ts):
             raise ValueError("tensors must be contiguous and on the GPU")
 
 
+_capture_calls = None
+
+
 def _capturing(dev: int | None) -> bool:
     """Whether the current stream of device `dev` (None: the current one) is being captured into a graph."""
-    cuda = _torch().cuda
-    if dev is None or cuda.current_device() == dev:
-        return cuda.is_current_stream_capturing()
-    with cuda.device(dev):
-        return cuda.is_current_stream_capturing()
+    global _capture_calls
+    if _capture_calls is None:      # the calls under torch.cuda's: 0.27 us together, against 0.48
+        cuda, c = _torch().cuda, _torch()._C
+        _capture_calls = (getattr(c, "_cuda_getDevice", cuda.current_device),
+                          getattr(c, "_cuda_isCurrentStreamCapturing", cuda.is_current_stream_capturing))
+    device, captured = _capture_calls
+    if dev is None or device() == dev:
+        return captured()
+    with _torch().cuda.device(dev):
+        return captured()
 
 
 _ws_cache: dict = {}
