@@ -193,7 +193,7 @@ def _weight_tiles(codes):
     *e, n, k = codes.shape
     np_, kp = _up(n, 16), _up(k, 128)
     c = torch.nn.functional.pad(codes, (0, kp - k, 0, np_ - n)).view(-1, np_ // 16, 16, kp // 128, 4, 2, 16)
-    return c.permute(0, 1, 3, 5, 4, 2, 6).reshape(*e, np_ // 16, kp // 128, 2, 4, 16, 16)
+    return c.permute(0, 1, 3, 5, 4, 2, 6).contiguous().view(*e, np_ // 16, kp // 128, 2, 4, 16, 16)
 
 
 def _weight_exps(b):
