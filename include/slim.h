@@ -107,6 +107,16 @@ typedef enum { SLIM_F16 = 0, SLIM_BF16 = 1, SLIM_F32 = 2 } slim_dtype;
 /* Values kept in 8 bits (see "The 8-bit path" below), where an entry point names it among its types. */
 typedef enum { SLIM_Q8_E4M3 = 3 } slim_dtype_q8;
 
+/* Activations: x; max(x, 0); x Phi(x) (Phi the normal distribution); x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2;
+ * x / (1 + exp(-x)). */
+typedef enum {
+  SLIM_ACT_NONE = 0,
+  SLIM_ACT_RELU = 1,
+  SLIM_ACT_GELU = 2,
+  SLIM_ACT_GELU_TANH = 3,
+  SLIM_ACT_SILU = 4
+} slim_act;
+
 /* Human-readable name of a status code (static string, never NULL). */
 const char* slim_status_string(int status);
 
@@ -554,6 +564,49 @@ int slim_linear8_workspace(int xdtype, int64_t M, int64_t N, int64_t K, size_t* 
 int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t N, int64_t K, int64_t ldx,
                  const uint8_t* codes, const uint8_t* exps, void* Y, int ydtype, int64_t ldy, void* ws, size_t ws_bytes,
                  void* stream);
+
+/*
+ * slim_linear8_act - a product that ends in an activation: z = X W^T + bias, Y = act(z) mul + residual, the sums as
+ * slim_linear8's and all that follows in fp32, rounded once.
+ *   X .. exps   as slim_linear8.                    act        a slim_act.
+ *   bias        [N] of `bdtype` (SLIM_F16, SLIM_BF16, SLIM_F32), or NULL.
+ *   mul, residual  [M, N] of `dtype` with row strides ldmul, ldres, or NULL: a gate's factor, what Y is added to.
+ *   dtype, q8   SLIM_F16 or SLIM_BF16: the type of mul, residual, Y and pre; with q8 nonzero Y and pre leave as 8-bit
+ *               rows instead (codes with exponents yexps, preexps; ldy, ldpre are not looked at), rounded from fp32.
+ *   Y           out, row stride ldy; may be mul or residual.
+ *   pre         out, NULL if not wanted: z, for the backward; row stride ldpre.
+ *   ws          slim_linear8_act_workspace(xdtype, M, N, K, dtype, q8) bytes; its contents need not be kept or cleared.
+ *
+ * slim_bwd_dx8_act - the gradient through the activation in front of a product: dh = dY W, the input gradient of the
+ * product that took act(u) mul, then dU = dh mul act'(u), dmul = dh act(u) and dbias = the sum of dU over the rows.
+ *   dY .. expsT  M, N, K as in the product's forward (W [N, K], dY [M, N], dh [M, K]), dY of any type that
+ *               slim_linear8 takes, codesT and expsT its transposed pack.
+ *   U, udtype   [M, K], the kept argument: `dtype` with row stride ldu, or SLIM_Q8_E4M3 with uexps. May be NULL with
+ *               SLIM_ACT_NONE where mul is.
+ *   mul         [M, K] like U (ldmul or mulexps), the gate's factor, or NULL; then dmul is NULL too.
+ *   dtype       SLIM_F16 or SLIM_BF16, of dU, dmul (row strides lddu, lddmul) and dbias.
+ *   dU, dmul    out; may be U and mul.
+ *   dbias       out, [K] of `dtype`, or NULL. It is as near as the product's sums (2e-5 to 4.5e-5 of its norm), then
+ *               rounded; fp32 is not offered for it, as for Y above.
+ *   ws          slim_bwd_dx8_act_workspace(dydtype, M, N, K, dtype, dbias != NULL) bytes, as above.
+ *
+ * slim_act_bwd - the same from a dh at hand: dH [M, K] of `dtype`, row stride lddh. dU may be dH. dbias fp32.
+ *   ws          slim_act_bwd_workspace(M, K, dbias != NULL) bytes, as above.
+ */
+int slim_linear8_act_workspace(int xdtype, int64_t M, int64_t N, int64_t K, int dtype, int q8, size_t* bytes);
+int slim_linear8_act(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t N, int64_t K, int64_t ldx,
+                     const uint8_t* codes, const uint8_t* exps, int act, const void* bias, int bdtype, const void* mul,
+                     int64_t ldmul, const void* residual, int64_t ldres, int dtype, int q8, void* Y, int64_t ldy, uint8_t* yexps,
+                     void* pre, int64_t ldpre, uint8_t* preexps, void* ws, size_t ws_bytes, void* stream);
+int slim_bwd_dx8_act_workspace(int dydtype, int64_t M, int64_t N, int64_t K, int dtype, int sums, size_t* bytes);
+int slim_bwd_dx8_act(const void* dY, int dydtype, const uint8_t* dyexps, int64_t M, int64_t N, int64_t K, int64_t lddy,
+                     const uint8_t* codesT, const uint8_t* expsT, int act, const void* U, int udtype, const uint8_t* uexps,
+                     int64_t ldu, const void* mul, const uint8_t* mulexps, int64_t ldmul, int dtype, void* dU, int64_t lddu,
+                     void* dmul, int64_t lddmul, void* dbias, void* ws, size_t ws_bytes, void* stream);
+int slim_act_bwd_workspace(int64_t M, int64_t K, int sums, size_t* bytes);
+int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, int64_t K, int act, const void* U, int udtype,
+                 const uint8_t* uexps, int64_t ldu, const void* mul, const uint8_t* mulexps, int64_t ldmul, void* dU, int64_t lddu,
+                 void* dmul, int64_t lddmul, float* dbias, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * slim_grad_w8 - the weight gradient dY^T X with X [M, K] an 8-bit checkpoint (xcodes, xexps).

@@ -28,6 +28,8 @@ the thesis' definitions:
   deployment of PATCH").
 * The 8-bit path (``act8``): e4m3 codes with a power of two for each group of 128, their product, and
   the norms with their backward pass.
+* The operators around its products in an MLP (``mlp8``): activations, bias, gate and residual with their gradients, the
+  router and the experts.
 
 Parity status per function is stated in ``slim_oracle``'s module docstring.
 """
@@ -37,3 +39,4 @@ from . import slim_quant  # noqa: F401
 from . import slim_lora  # noqa: F401
 from . import patch_hybrid  # noqa: F401
 from . import act8  # noqa: F401
+from . import mlp8  # noqa: F401

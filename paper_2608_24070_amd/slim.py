@@ -24,6 +24,10 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "slim.h")
  SLIM_EUNSUPPORTED, SLIM_ERANGE) = range(10)
 SLIM_F16, SLIM_BF16, SLIM_F32 = 0, 1, 2
 SLIM_Q8_E4M3 = 3
+# slim_act, and the names that the helpers know them by
+SLIM_ACT_NONE, SLIM_ACT_RELU, SLIM_ACT_GELU, SLIM_ACT_GELU_TANH, SLIM_ACT_SILU = range(5)
+ACTS = {"none": SLIM_ACT_NONE, "relu": SLIM_ACT_RELU, "gelu": SLIM_ACT_GELU, "gelu_tanh": SLIM_ACT_GELU_TANH,
+        "silu": SLIM_ACT_SILU}
 
 _c_i64 = ctypes.c_int64
 _c_p = ctypes.c_void_p
@@ -68,6 +72,19 @@ _SIGS = {
     "slim_linear8_workspace": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
     "slim_linear8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
                                     ctypes.c_int, _c_i64, _c_p, ctypes.c_size_t, _c_p]),
+    "slim_linear8_act_workspace": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, ctypes.c_int, ctypes.c_int,
+                                                  ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_linear8_act": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, ctypes.c_int, _c_p,
+                                        ctypes.c_int, _c_p, _c_i64, _c_p, _c_i64, ctypes.c_int, ctypes.c_int, _c_p, _c_i64, _c_p,
+                                        _c_p, _c_i64, _c_p, _c_p, ctypes.c_size_t, _c_p]),
+    "slim_bwd_dx8_act_workspace": (ctypes.c_int, [ctypes.c_int, _c_i64, _c_i64, _c_i64, ctypes.c_int, ctypes.c_int,
+                                                  ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_bwd_dx8_act": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, ctypes.c_int, _c_p,
+                                        ctypes.c_int, _c_p, _c_i64, _c_p, _c_p, _c_i64, ctypes.c_int, _c_p, _c_i64, _c_p, _c_i64,
+                                        _c_p, _c_p, ctypes.c_size_t, _c_p]),
+    "slim_act_bwd_workspace": (ctypes.c_int, [_c_i64, _c_i64, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_act_bwd": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_i64, _c_i64, ctypes.c_int, _c_p, ctypes.c_int, _c_p, _c_i64, _c_p,
+                                    _c_p, _c_i64, _c_p, _c_i64, _c_p, _c_i64, _c_p, _c_p, ctypes.c_size_t, _c_p]),
     "slim_grad_w8_workspace": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, ctypes.c_int, ctypes.c_int,
                                               ctypes.POINTER(ctypes.c_size_t)]),
     "slim_grad_w8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
@@ -269,6 +286,42 @@ def slim_linear8_workspace(xdtype, M, N, K) -> int:
 
 def slim_linear8(X, xdtype, xexps, M, N, K, ldx, codes, exps, Y, ydtype, ldy, ws, ws_bytes, stream) -> int:
     return lib().slim_linear8(X, xdtype, xexps, M, N, K, ldx, codes, exps, Y, ydtype, ldy, ws, ws_bytes, stream)
+
+
+def slim_linear8_act_workspace(xdtype, M, N, K, dtype, q8) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().slim_linear8_act_workspace(xdtype, M, N, K, dtype, q8, ctypes.byref(out)), "slim_linear8_act_workspace")
+    return out.value
+
+
+def slim_linear8_act(X, xdtype, xexps, M, N, K, ldx, codes, exps, act, bias, bdtype, mul, ldmul, residual, ldres, dtype, q8, Y, ldy,
+                     yexps, pre, ldpre, preexps, ws, ws_bytes, stream) -> int:
+    return lib().slim_linear8_act(X, xdtype, xexps, M, N, K, ldx, codes, exps, act, bias, bdtype, mul, ldmul, residual, ldres, dtype,
+                                  q8, Y, ldy, yexps, pre, ldpre, preexps, ws, ws_bytes, stream)
+
+
+def slim_bwd_dx8_act_workspace(dydtype, M, N, K, dtype, sums) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().slim_bwd_dx8_act_workspace(dydtype, M, N, K, dtype, sums, ctypes.byref(out)), "slim_bwd_dx8_act_workspace")
+    return out.value
+
+
+def slim_bwd_dx8_act(dY, dydtype, dyexps, M, N, K, lddy, codesT, expsT, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dtype, dU, lddu,
+                     dmul, lddmul, dbias, ws, ws_bytes, stream) -> int:
+    return lib().slim_bwd_dx8_act(dY, dydtype, dyexps, M, N, K, lddy, codesT, expsT, act, U, udtype, uexps, ldu, mul, mulexps, ldmul,
+                                  dtype, dU, lddu, dmul, lddmul, dbias, ws, ws_bytes, stream)
+
+
+def slim_act_bwd_workspace(M, K, sums) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().slim_act_bwd_workspace(M, K, sums, ctypes.byref(out)), "slim_act_bwd_workspace")
+    return out.value
+
+
+def slim_act_bwd(dH, dtype, lddh, M, K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul, dbias, ws, ws_bytes,
+                 stream) -> int:
+    return lib().slim_act_bwd(dH, dtype, lddh, M, K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul, dbias, ws,
+                              ws_bytes, stream)
 
 
 def slim_grad_w8_workspace(M, N, K, masked, aligned) -> int:
@@ -956,7 +1009,8 @@ def _given8(nbytes: int, ws, like, stream: int):
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, where: str):
+def _product8_operands(X, codes, exps, N: int, K: int):
+    """Checked parts of a product's operands: x, its exponents' pointer, type, rows, row stride, device."""
     if codes.shape != ((N + 15) // 16, (K + 127) // 128, 2, 4, 16, 16) or exps.shape != ((N + 127) // 128, (K + 511) // 512 * 4):
         raise ValueError("codes and exponents do not have the shape of the 8-bit weight")
     _bytes_on_gpu(codes, exps)
@@ -970,6 +1024,11 @@ def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, where: str):
         raise ValueError("the rows' width does not match the pack")
     if codes.get_device() != dev or exps.get_device() != dev:
         raise ValueError("X and the pack must be on one device")
+    return x, xe, xdt, M, ldx, dev
+
+
+def _product8(X, codes, exps, N: int, K: int, dtype, out, ws, where: str):
+    x, xe, xdt, M, ldx, dev = _product8_operands(X, codes, exps, N, K)
     if dtype is None:
         torch = _torch()
         dtype = out.dtype if out is not None else torch.float16 if xdt == SLIM_F16 else torch.bfloat16
@@ -1003,6 +1062,149 @@ def bwd_dx8(dY, p: dict, dtype=None, out=None, ws=None, stream=None):
     if stream is not None:
         return _on_its_stream(stream, bwd_dx8, dY, p, dtype, out, ws)
     return _product8(dY, p["codesT"], p["expsT"], p["K"], p["N"], dtype, out, ws, "slim_linear8")
+
+
+def _act_code(act: str) -> int:
+    code = ACTS.get(act)
+    if code is None:
+        raise ValueError(f"act must be one of {', '.join(ACTS)}, got {act!r}")
+    return code
+
+
+def _like_rows(t, M: int, N: int, dtype, dev: int, what: str):
+    """(pointer, row stride) of an optional [M, N] operand of `dtype`."""
+    if t is None:
+        return None, 0
+    return t.data_ptr(), _matrix_out(t, M, N, dtype, dev, what)
+
+
+def _rows8_of(q, M: int, N: int, dev: int, what: str):
+    """(pointer of codes, of exponents) of 8-bit rows [M, N]."""
+    codes, exps, m, n, _ = _rows8(q, dev)
+    if (m, n) != (M, N):
+        raise ValueError(f"{what} must be ({M}, {N}), got ({m}, {n})")
+    return codes.data_ptr(), exps.data_ptr()
+
+
+def linear8_act(X, p: dict, act: str = "none", bias=None, mul=None, residual=None, pre: bool = False, q8: bool = False, dtype=None,
+                out=None, ws=None, stream=None):
+    """slim_linear8_act: Y [M, N] = act(X W^T + bias) * mul + residual with an 8-bit weight (pack8), X as in linear8. `act`: "none",
+    "relu", "gelu", "gelu_tanh" or "silu"; bias [N] of any float type; mul and residual [M, N] of `dtype` (fp16 or bf16, default as
+    linear8). Y in `dtype`, or with `q8` 8-bit rows. With `pre`: (Y, X W^T + bias), the second like Y, for the backward."""
+    if stream is not None:
+        return _on_its_stream(stream, linear8_act, X, p, act, bias, mul, residual, pre, q8, dtype, out, ws)
+    N, K, a = p["N"], p["K"], _act_code(act)
+    x, xe, xdt, M, ldx, dev = _product8_operands(X, p["codes"], p["exps"], N, K)
+    if dtype is None:
+        torch = _torch()
+        given = out if out is not None and not q8 else mul if mul is not None else residual
+        dtype = given.dtype if given is not None else torch.float16 if xdt == SLIM_F16 else torch.bfloat16
+    dt = _float_code(dtype)
+    bp, bdt = None, SLIM_F32
+    if bias is not None:
+        _vector(bias, N, dev, "bias")
+        bp, bdt = bias.data_ptr(), _float_code(bias.dtype)
+    mp, ldm = _like_rows(mul, M, N, dtype, dev, "mul")
+    rp, ldr = _like_rows(residual, M, N, dtype, dev, "residual")
+    second, zp, ze, ldz = None, None, None, 0
+    if q8:
+        if out is None:
+            out = _empty_rows8(M, N, x)
+        else:
+            _rows8_of(out, M, N, dev, "out")
+        yp, ye, ldy = out["codes"].data_ptr(), out["exps"].data_ptr(), 0
+        if pre:
+            second = _empty_rows8(M, N, x)
+            zp, ze = second["codes"].data_ptr(), second["exps"].data_ptr()
+    else:
+        if out is None:
+            out, ldy = x.new_empty((M, N), dtype=dtype), N
+        else:
+            ldy = _matrix_out(out, M, N, dtype, dev)
+        yp, ye = out.data_ptr(), None
+        if pre:
+            second = x.new_empty((M, N), dtype=dtype)
+            zp, ldz = second.data_ptr(), N
+    L, st, q = lib(), _stream_on(dev), 1 if q8 else 0
+    need = ctypes.c_size_t()
+    rc = L.slim_linear8_act_workspace(xdt, M, N, K, dt, q, need)
+    if not rc:
+        wp, wn = _given8(need.value, ws, x, st)
+        rc = L.slim_linear8_act(x.data_ptr(), xdt, xe, M, N, K, ldx, p["codes"].data_ptr(), p["exps"].data_ptr(), a, bp, bdt, mp, ldm, rp,
+                                ldr, dt, q, yp, ldy, ye, zp, ldz, ze, wp, wn, st)
+    if rc:
+        raise SlimError(rc, "slim_linear8_act")
+    return (out, second) if pre else out
+
+
+def _kept_operands(u, mul, M: int, K: int, dtype, dev: int):
+    """u's type code and (pointer, exponents, stride) of u and mul, both 8-bit rows or both of `dtype`."""
+    if type(u) is dict or type(mul) is dict:
+        if (u is not None and type(u) is not dict) or (mul is not None and type(mul) is not dict):
+            raise TypeError("u and mul must both be 8-bit rows or both be tensors")
+        up, ue = (None, None) if u is None else _rows8_of(u, M, K, dev, "u")
+        mp, me = (None, None) if mul is None else _rows8_of(mul, M, K, dev, "mul")
+        return SLIM_Q8_E4M3, (up, ue, 0), (mp, me, 0)
+    (up, ldu), (mp, ldm) = _like_rows(u, M, K, dtype, dev, "u"), _like_rows(mul, M, K, dtype, dev, "mul")
+    return _float_code(dtype), (up, None, ldu), (mp, None, ldm)
+
+
+def bwd_dx8_act(dY, p: dict, u, act: str = "none", mul=None, bias: bool = False, dtype=None, out=None, ws=None, stream=None):
+    """slim_bwd_dx8_act: (du, dmul, dbias) from dY [M, N] of a product Y = h W^T with h = act(u) * mul: with dh = dY W (pack8 with
+    bwd=True) du = dh * mul * act'(u), dmul = dh * act(u) (None without mul), dbias [K] = the sums of du's columns (None unless
+    `bias`), all of `dtype` (as linear8). u and mul [M, K]: of `dtype`, or 8-bit rows."""
+    if stream is not None:
+        return _on_its_stream(stream, bwd_dx8_act, dY, p, u, act, mul, bias, dtype, out, ws)
+    N, K, a = p["N"], p["K"], _act_code(act)
+    x, xe, xdt, M, ldx, dev = _product8_operands(dY, p["codesT"], p["expsT"], K, N)
+    if dtype is None:
+        torch = _torch()
+        given = out if out is not None else u if u is not None and type(u) is not dict else None
+        dtype = given.dtype if given is not None else torch.float16 if xdt == SLIM_F16 else torch.bfloat16
+    dt = _float_code(dtype)
+    udt, (up, ue, ldu), (mp, me, ldm) = _kept_operands(u, mul, M, K, dtype, dev)
+    if out is None:
+        out, ldo = x.new_empty((M, K), dtype=dtype), K
+    else:
+        ldo = _matrix_out(out, M, K, dtype, dev)
+    dmul = None if mul is None else x.new_empty((M, K), dtype=dtype)
+    dbias = x.new_empty((K,), dtype=dtype) if bias else None
+    L, st = lib(), _stream_on(dev)
+    need = ctypes.c_size_t()
+    rc = L.slim_bwd_dx8_act_workspace(xdt, M, N, K, dt, 1 if bias else 0, need)
+    if not rc:
+        wp, wn = _given8(need.value, ws, x, st)
+        rc = L.slim_bwd_dx8_act(x.data_ptr(), xdt, xe, M, N, K, ldx, p["codesT"].data_ptr(), p["expsT"].data_ptr(), a, up, udt, ue, ldu, mp,
+                                me, ldm, dt, out.data_ptr(), ldo, _ptr(dmul), K, _ptr(dbias), wp, wn, st)
+    if rc:
+        raise SlimError(rc, "slim_bwd_dx8_act")
+    return out, dmul, dbias
+
+
+def act_bwd(dh, u, act: str = "none", mul=None, bias: bool = False, out=None, ws=None, stream=None):
+    """slim_act_bwd: (du, dmul, dbias) as bwd_dx8_act's from a dh [M, K] at hand (fp16 or bf16), of whose type they are; dbias fp32."""
+    if stream is not None:
+        return _on_its_stream(stream, act_bwd, dh, u, act, mul, bias, out, ws)
+    M, K, ldh, dev = _matrix(dh, "dh")
+    a, dtype = _act_code(act), dh.dtype
+    dt = _float_code(dtype)
+    udt, (up, ue, ldu), (mp, me, ldm) = _kept_operands(u, mul, M, K, dtype, dev)
+    if out is None:
+        out, ldo = dh.new_empty((M, K)), K
+    else:
+        ldo = _matrix_out(out, M, K, dtype, dev)
+    dmul = None if mul is None else dh.new_empty((M, K))
+    dbias = dh.new_empty((K,), dtype=_torch().float32) if bias else None
+    L, st = lib(), _stream_on(dev)
+    need = ctypes.c_size_t()
+    rc = L.slim_act_bwd_workspace(M, K, 1 if bias else 0, need)
+    if not rc:
+        wp, wn = _given8(need.value, ws, dh, st)
+        rc = L.slim_act_bwd(dh.data_ptr(), dt, ldh, M, K, a, up, udt, ue, ldu, mp, me, ldm, out.data_ptr(), ldo, _ptr(dmul), K, _ptr(dbias), wp,
+                            wn, st)
+    if rc:
+        raise SlimError(rc, "slim_act_bwd")
+    return out, dmul, dbias
 
 
 def grad_w8(dY, q: dict, p: dict | None = None, out=None, ws=None, stream=None):

@@ -1,0 +1,315 @@
+"""Products that end in an activation, and the gradient through it, against the oracle in 64 bits.
+
+Bounds, per element. The product's: the matrix unit cuts each product of eight consecutive positions below 2^-13 of the largest's
+leading bit, S = 8 2^-13 (the sum over eights of the operands' largest) + 2^-20 (the sum of magnitudes). An activation's slope is
+below 1.13, its own error in fp32 below 2^-19 (|z| + |act|) (e^x: one place of x log2 e up to 2^7, so 2^-17 of a tail that is below
+2^-2 there), so y is within (1.13 S' + 2^-19 (|z| + 1)) |mul| + u |y|, S' with bias S + 2^-23 |z|, u the half step of the type.
+8-bit results are within 2^-4 of themselves, or 2^-10 of their group's 2^e (at most 2 amax / 448), of such a value."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import act8, mlp8
+from paper_2608_24070_amd import slim, synth
+from tests.gpu_common import dev, host, kernels_of
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16}
+U = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+TINY = {"bf16": 2.0 ** -133, "fp16": 2.0 ** -24}       # the step of the type's smallest values
+ACTS = list(mlp8.ACTS)
+
+
+def eights(a):
+    return np.abs(np.pad(a, ((0, 0), (0, -a.shape[1] % 8)))).reshape(len(a), -1, 8).max(2)
+
+
+def sums_bound(x, w):
+    return 8 * 2.0 ** -13 * (eights(x) @ eights(w).T) + 2.0 ** -20 * (np.abs(x) @ np.abs(w).T)
+
+
+def within(got, ref, lim, what=""):
+    got = got if isinstance(got, np.ndarray) else got.double().cpu().numpy()
+    bad = ~(np.abs(got - ref) <= lim)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} out of bound, first {np.argwhere(bad)[:3].tolist()}"
+
+
+def rounded8(ref, err):
+    """Bound of a value kept in 8 bits whose exact one is within err of ref."""
+    m, k = ref.shape
+    g = -(-k // 128)
+    amax = np.zeros((m, g * 128))
+    amax[:, :k] = np.abs(ref) + err
+    amax = np.repeat(amax.reshape(m, g, 128).max(2), 128, 1)[:, :k]
+    return err + 2.0 ** -4 * (np.abs(ref) + err) + 2.0 ** -10 * 2 * amax / 448
+
+
+def check_rows8(q, ref, err, what):
+    m, n = ref.shape
+    codes, exps = host(q["codes"]), host(q["exps"])
+    assert not codes[:, n:].any() and not exps[:, -(-n // 128):].any(), what
+    within(act8.values_rows(codes, exps, n), ref, rounded8(ref, err), what)
+
+
+def case(m, n, k, dtype, seed=0):
+    gen = torch.Generator("cuda").manual_seed(m + n + k + seed)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")
+    x = (rand(m, k) * 2.0 ** torch.randint(-1, 2, (m, 1), generator=gen, device="cuda")).to(DT[dtype])
+    w = rand(n, k) * (1.5 * k ** -0.5)
+    return x, w, rand(n), rand(m, n).to(DT[dtype]), (3 * rand(m, n)).to(DT[dtype])
+
+
+# few rows, then every tile kernel, whole and in slices; the last tiles of a few rows or columns
+FEW = [(1, 1, 1), (1, 4100, 512), (2, 300, 1300), (3, 100, 300), (4, 130, 640), (9, 5000, 260), (16, 257, 1000), (17, 64, 129), (33, 130, 640), (64, 513, 384)]
+TILES = [(65, 17, 129), (100, 513, 1300), (129, 1000, 129), (2047, 100, 900), (300, 2050, 2100), (1500, 2050, 1300), (400, 8200, 129),
+         (2047, 2050, 300), (2500, 4100, 900), (1500, 8200, 129)]
+SLICED = [(24, 512, 14336), (64, 1000, 28001), (300, 131, 9000), (512, 515, 28672), (2000, 200, 12345)]
+
+
+@pytest.mark.parametrize("m,n,k", FEW + TILES + SLICED)
+def test_forward(m, n, k):
+    for i, (dtype, q8) in enumerate((d, q) for d in DT for q in (False, True)):
+        act = ACTS[(m + n + i) % len(ACTS)]
+        use = [(m + i) % 2 == 0 or m == 1, (n + i) % 3 != 0, (k + i) % 3 != 1]
+        print(f"linear8_act m={m} n={n} k={k} {dtype} q8={q8} {act} bias, mul, residual {use}", flush=True)
+        x, w, bias, mul, res = case(m, n, k, dtype, i)
+        bias, mul, res = bias if use[0] else None, mul if use[1] else None, res if use[2] else None
+        p = slim.pack8(w)
+        y, z = slim.linear8_act(x, p, act=act, bias=bias, mul=mul, residual=res, pre=True, q8=q8, dtype=DT[dtype])
+        only = slim.linear8_act(x, p, act=act, bias=bias, mul=mul, residual=res, q8=q8, dtype=DT[dtype])
+        assert all(torch.equal(only[v], y[v]) for v in ("codes", "exps")) if q8 else torch.equal(only, y)
+        rows = np.unique(np.r_[0, m - 1, synth.stream(0, f"act/rows/{m}").integers(0, m, 40)])
+        at = torch.from_numpy(rows).cuda()
+        some = lambda t: {"codes": t["codes"][at], "exps": t["exps"][at]} if type(t) is dict else t[at]
+        num = lambda t: host(t[at].double())
+        xv = act8.values_rows(*act8.quant_rows(num(x)), k)
+        wv = act8.values_weight(*act8.quant_weight(host(w).astype(np.float64)))
+        zr = xv @ wv.T + (0 if bias is None else host(bias).astype(np.float64))
+        mr = 1.0 if mul is None else num(mul)
+        yr = mlp8.forward(zr, act, None if mul is None else mr, None if res is None else num(res))
+        zerr = sums_bound(xv, wv) + 2.0 ** -23 * np.abs(zr)
+        yerr = (1.13 * zerr + 2.0 ** -19 * (np.abs(zr) + 1)) * np.abs(mr) + 2.0 ** -23 * np.abs(yr)
+        if q8:
+            check_rows8(some(y), yr, yerr, "y")
+            check_rows8(some(z), zr, zerr, "z")
+        else:
+            within(some(y), yr, yerr + U[dtype] * np.abs(yr) + TINY[dtype], "y")
+            within(some(z), zr, zerr + U[dtype] * np.abs(zr) + TINY[dtype], "z")
+
+
+@pytest.mark.parametrize("m,n,k", FEW + TILES + SLICED)
+def test_nothing_added_is_the_product(m, n, k):
+    x, w, _, _, _ = case(m, n, k, "bf16")
+    p = slim.pack8(w, bwd=True)
+    want = slim.linear8(x, p)
+    assert torch.equal(slim.linear8_act(x, p), want)
+    assert torch.equal(slim.linear8_act(slim.quant8(x), p), want)
+    dy = x.new_empty((m, n)).normal_()
+    du, dmul, db = slim.bwd_dx8_act(dy, p, None)
+    assert torch.equal(du, slim.bwd_dx8(dy, p)) and dmul is None and db is None
+
+
+@pytest.mark.parametrize("m,n,k", FEW + TILES + SLICED)
+def test_backward(m, n, k):
+    # n: the reduction here, k: the columns of dh
+    n, k = k, n
+    for i, (dtype, q8) in enumerate((d, q) for d in DT for q in (False, True)):
+        act, gated, bias = ACTS[(m + k + i) % len(ACTS)], (m + i) % 2 == 0, (k + i) % 3 != 0
+        print(f"bwd_dx8_act m={m} n={n} k={k} {dtype} q8={q8} {act} gated={gated} bias={bias}", flush=True)
+        gen = torch.Generator("cuda").manual_seed(m + n + k + i)
+        rand = lambda *s: torch.randn(s, generator=gen, device="cuda")
+        dy, w = rand(m, n).to(DT[dtype]), rand(n, k) * n ** -0.5
+        u, mul = (2 * rand(m, k)).to(DT[dtype]), rand(m, k).to(DT[dtype]) if gated else None
+        ku, km = (slim.quant8(u), None if mul is None else slim.quant8(mul)) if q8 else (u, mul)
+        p = slim.pack8(w, bwd=True)
+        du, dmul, db = slim.bwd_dx8_act(dy, p, ku, act=act, mul=km, bias=bias, dtype=DT[dtype])
+        assert (dmul is None) == (mul is None) and (db is None) == (not bias)
+        dyv = act8.values_rows(*act8.quant_rows(host(dy.double())), n)
+        wv = act8.values_weight(*act8.quant_weight(host(w).astype(np.float64)))
+        dh, err = dyv @ wv, sums_bound(dyv, np.ascontiguousarray(wv.T))
+        read = (lambda t: act8.values_rows(*act8.quant_rows(host(t.double())), k)) if q8 else (lambda t: host(t.double()))
+        uv, mv = read(u), None if mul is None else read(mul)
+        r_du, r_dm, r_db = mlp8.backward(dh, uv, act, mv)
+        am = 1.0 if mv is None else np.abs(mv)
+        e_du = (1.13 * err + 2.0 ** -19 * (np.abs(dh) + err)) * am + 2.0 ** -22 * np.abs(r_du)
+        within(du, r_du, e_du + U[dtype] * np.abs(r_du) + TINY[dtype], "du")
+        if mul is not None:
+            e = np.abs(mlp8.value(act, uv)) * err + 2.0 ** -19 * np.abs(dh) * (np.abs(uv) + 1) + U[dtype] * np.abs(r_dm) + TINY[dtype]
+            within(dmul, r_dm, e, "dmul")
+        if bias:
+            # fp32 chains of at most 256 rows a lane and 16 parts after them, 2^-24 each
+            e = e_du.sum(0) + (m + 16) * 2.0 ** -24 * np.abs(r_du).sum(0) + U[dtype] * np.abs(r_db) + TINY[dtype]
+            within(db, r_db, e, "dbias")
+
+
+AB = [(1, 1), (1, 4096), (3, 100), (7, 129), (16, 128), (65, 1000), (100, 4097), (333, 257), (1000, 515), (2000, 6001), (37, 28672)]
+
+
+@pytest.mark.parametrize("m,k", AB)
+@pytest.mark.parametrize("act", ACTS)
+def test_gradient_by_itself(m, k, act):
+    for i, (dtype, q8) in enumerate((d, q) for d in DT for q in (False, True)):
+        gated, bias = (m + i) % 2 == 0, (k + i) % 3 != 0
+        print(f"act_bwd m={m} k={k} {dtype} q8={q8} {act} gated={gated} bias={bias}", flush=True)
+        gen = torch.Generator("cuda").manual_seed(m + k + i)
+        rand = lambda: torch.randn((m, k), generator=gen, device="cuda")
+        dh, u, mul = rand().to(DT[dtype]), (2 * rand()).to(DT[dtype]), rand().to(DT[dtype]) if gated else None
+        ku, km = (slim.quant8(u), None if mul is None else slim.quant8(mul)) if q8 else (u, mul)
+        du, dmul, db = slim.act_bwd(dh, ku, act=act, mul=km, bias=bias)
+        read = (lambda t: act8.values_rows(*act8.quant_rows(host(t.double())), k)) if q8 else (lambda t: host(t.double()))
+        uv, mv, hv = read(u), None if mul is None else read(mul), host(dh.double())
+        r_du, r_dm, r_db = mlp8.backward(hv, uv, act, mv)
+        e_du = 2.0 ** -19 * np.abs(hv) * (1.0 if mv is None else np.abs(mv)) + 2.0 ** -22 * np.abs(r_du)
+        within(du, r_du, e_du + U[dtype] * np.abs(r_du) + TINY[dtype], "du")
+        if mul is not None:
+            within(dmul, r_dm, 2.0 ** -19 * np.abs(hv) * (np.abs(uv) + 1) + U[dtype] * np.abs(r_dm) + TINY[dtype], "dmul")
+        if bias:
+            assert db.dtype == torch.float32
+            within(db, r_db, e_du.sum(0) + (m + 16) * 2.0 ** -24 * np.abs(r_du).sum(0) + 2.0 ** -24 * np.abs(r_db), "dbias")
+        # in place
+        same = dh.clone()
+        assert slim.act_bwd(same, ku, act=act, mul=km, out=same)[0] is same and torch.equal(same, du)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_far_values(act):
+    # every 16-bit value through the activation and its slope; infinite and NaN ones may only give what is not finite or the limit
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(256, 256).cuda()
+    ones = torch.ones_like(bits)
+    du, dv, _ = slim.act_bwd(ones, bits, act=act, mul=ones)
+    x = host(bits.double())
+    fine = np.isfinite(x)
+    with np.errstate(all="ignore"):
+        v, d = mlp8.value(act, x), mlp8.slope(act, np.clip(x, -1e15, 1e15))
+    ok = fine & (np.abs(v) < 3.3e38)
+    within(host(dv.double())[ok], v[ok], U["bf16"] * np.abs(v[ok]) + 2.0 ** -19 * np.minimum(np.abs(x[ok]), 16) + 2.0 ** -126)
+    within(host(du.double())[fine], d[fine], U["bf16"] * np.abs(d[fine]) + 2.0 ** -19)
+    nan = np.isnan(x)
+    assert np.isnan(host(dv.double())[nan]).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 200, 300), (40, 333, 600), (300, 333, 600), (64, 515, 28672)])
+def test_strides_places_and_the_bytes_around_the_results(m, n, k):
+    x, w, bias, _, _ = case(m, n, k, "bf16")
+    p = slim.pack8(w, bwd=True)
+    wide = torch.randn((m + 2, n + 19), device="cuda").bfloat16()
+    mul = wide[1:1 + m, 7:7 + n]
+    buf = torch.full((m + 2, n + 40), -7.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[1:1 + m, 9:9 + n]
+    want = slim.linear8_act(x, p, act="silu", bias=bias, mul=mul.contiguous(), residual=mul.contiguous())
+    slim.linear8_act(x, p, act="silu", bias=bias, mul=mul, residual=mul, out=out)
+    assert torch.equal(out, want)
+    out.fill_(-7.0)
+    assert bool((buf == -7).all())
+    # the residual's own place, bias in 16 bits
+    out.copy_(mul)
+    half = bias.bfloat16()
+    want = slim.linear8_act(x, p, act="gelu", bias=half.float(), residual=mul.contiguous())
+    assert torch.equal(slim.linear8_act(x, p, act="gelu", bias=half, residual=out, out=out), want)
+    out.fill_(-7.0)
+    assert bool((buf == -7).all())
+    # the gradient into u's own place
+    dy = torch.randn((m, n), device="cuda").bfloat16()
+    u = torch.randn((m, k), device="cuda").bfloat16()
+    want = slim.bwd_dx8_act(dy, p, u, act="gelu", bias=True)
+    buf = torch.full((m + 2, k + 40), -7.0, dtype=torch.bfloat16, device="cuda")
+    out = buf[1:1 + m, 11:11 + k]
+    out.copy_(u)
+    got = slim.bwd_dx8_act(dy, p, out, act="gelu", bias=True, out=out)
+    assert torch.equal(out, want[0]) and torch.equal(got[2], want[2])
+    out.fill_(-7.0)
+    assert bool((buf == -7).all())
+
+
+@pytest.mark.parametrize("m", [4, 40, 200])
+def test_nan_rows_stay_apart(m):
+    x, w, bias, mul, res = case(m, 70, 300, "bf16")
+    p = slim.pack8(w)
+    for q8 in (False, True):
+        call = lambda t: slim.linear8_act(t, p, act="gelu", bias=bias, mul=mul, residual=res, q8=q8)
+        read = (lambda y: slim.dequant8(y)) if q8 else (lambda y: y)
+        clean = read(call(x))
+        bad = x.clone()
+        bad[1, 40], bad[3, 299] = float("nan"), float("inf")
+        got = read(call(bad))
+        rows = torch.ones(m, dtype=torch.bool, device="cuda")
+        rows[[1, 3]] = False
+        assert bool(got[[1, 3]].isnan().all()) and torch.equal(got[rows], clean[rows])
+
+
+def test_no_rows():
+    _, w, bias, _, _ = case(1, 70, 300, "bf16")
+    p = slim.pack8(w, bwd=True)
+    none = lambda n: torch.empty((0, n), dtype=torch.bfloat16, device="cuda")
+    y, z = slim.linear8_act(none(300), p, act="gelu", bias=bias, pre=True)
+    assert y.shape == z.shape == (0, 70)
+    q = slim.linear8_act(none(300), p, act="gelu", q8=True)
+    assert q["codes"].shape == (0, 128)
+    du, dm, db = slim.bwd_dx8_act(none(70), p, none(300), act="gelu", mul=none(300), bias=True)
+    assert du.shape == dm.shape == (0, 300) and not bool(db.any())
+    du, dm, db = slim.act_bwd(none(300), none(300), act="gelu", mul=none(300), bias=True)
+    assert du.shape == dm.shape == (0, 300) and db.shape == (300,) and not bool(db.any())
+
+
+@pytest.mark.parametrize("m,n,k", [(2, 515, 640), (40, 515, 640), (300, 515, 640), (64, 1000, 28001)])
+def test_repeats_streams_and_graph_replays(m, n, k):
+    x, w, bias, mul, _ = case(m, n, k, "bf16")
+    p = slim.pack8(w, bwd=True)
+    dy = torch.randn((m, n), device="cuda").bfloat16()
+    u = torch.randn((m, k), device="cuda").bfloat16()
+
+    def calls(stream=None):
+        y, z = slim.linear8_act(x, p, act="silu", bias=bias, mul=mul, pre=True, stream=stream)
+        q = slim.linear8_act(x, p, act="gelu", bias=bias, q8=True, stream=stream)
+        a = slim.bwd_dx8_act(dy, p, u, act="gelu", bias=True, stream=stream)
+        b = slim.act_bwd(u, u, act="silu", mul=u, bias=True, stream=stream)
+        return [y, z, q["codes"], q["exps"], a[0], a[2], b[0], b[1], b[2]]
+
+    same = lambda a, b: all(torch.equal(s, t) for s, t in zip(a, b))
+    want = calls()
+    assert all(same(calls(), want) for _ in range(3))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = calls(side)
+    side.synchronize()
+    assert same(got, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = calls()
+    for rep in range(3):
+        x.normal_()
+        u.normal_()
+        for t in held:
+            t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert same(held, calls()), rep
+
+
+@pytest.mark.parametrize("m,n,k", [(2, 515, 640), (24, 512, 14336), (64, 513, 384), (300, 515, 640), (512, 515, 28672)])
+def test_workspaces_are_what_is_asked_for(m, n, k):
+    x, w, bias, _, _ = case(m, n, k, "bf16")
+    p, q, BF = slim.pack8(w, bwd=True), slim.quant8(x), slim.SLIM_BF16
+    u, dh = torch.randn((m, n), device="cuda").bfloat16(), torch.randn((m, n), device="cuda").bfloat16()
+    pT = slim.pack8(w.t().contiguous(), bwd=True)           # dh [m, n] = q W^T once more, as an input gradient
+    runs = [(slim.slim_linear8_act_workspace(slim.SLIM_Q8_E4M3, m, n, k, BF, 0), lambda ws: slim.linear8_act(q, p, act="gelu", ws=ws)),
+            (slim.slim_linear8_act_workspace(BF, m, n, k, BF, 1), lambda ws: slim.linear8_act(x, p, act="gelu", q8=True, ws=ws)["codes"]),
+            (slim.slim_bwd_dx8_act_workspace(BF, m, k, n, BF, 1), lambda ws: slim.bwd_dx8_act(x, pT, u, act="gelu", bias=True, ws=ws)[2]),
+            (slim.slim_act_bwd_workspace(m, n, 1), lambda ws: slim.act_bwd(dh, u, act="gelu", bias=True, ws=ws)[2])]
+    for need, run in runs:
+        ws = torch.full((need + 256,), 7, dtype=torch.uint8, device="cuda")
+        got = run(ws[:need])
+        assert bool((ws[need:] == 7).all()) and torch.equal(got, run(None))
+        if need:
+            with pytest.raises(slim.SlimError):
+                run(ws[:need - 1])
+
+
+def test_the_kernels_that_run():
+    # a size at which a tile of 256 columns is picked
+    x, w, bias, mul, _ = case(1500, 2050, 1300, "bf16")
+    p = slim.pack8(w, bwd=True)
+    assert kernels_of(lambda: slim.linear8_act(x, p, act="gelu", q8=True)) == {"quant8", "act8_tile"}
+    assert kernels_of(lambda: slim.linear8_act(x[:1], p, act="gelu", bias=bias)) == {"act8_few"}
+    assert kernels_of(lambda: slim.bwd_dx8_act(mul, p, x, act="gelu", bias=True)) == {"quant8", "act8_tile", "act8_sums"}
