@@ -609,6 +609,37 @@ int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, int64_t K, 
                  void* dmul, int64_t lddmul, float* dbias, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * slim_route - the router in front of a layer of experts: p = softmax(x Wr^T) over E experts for each row x of X, then the `top` largest.
+ *   X, xdtype   [M, K]: SLIM_F16, SLIM_BF16 or SLIM_F32 with row stride ldx, or SLIM_Q8_E4M3 with xexps.
+ *   Wr, wdtype  [E, K]: SLIM_F16, SLIM_BF16 or SLIM_F32, row stride ldw. E <= 512.
+ *   top         1 .. min(E, 16).                    renorm   nonzero: weights are divided by their row's sum.
+ *   ids         out, int32 [M, top]: experts by falling logit, the lower number first where two are equal.
+ *   weights     out, fp32 [M, top]: their p.
+ *   ws          slim_route_workspace(M, E) bytes; its contents need not be kept or cleared.
+ * Arithmetic is fp32. A row with a NaN among its logits has weights of NaN, and those experts last that gave it.
+ *
+ * slim_moe8 - a layer of experts for a few tokens: y_i = sum_j w_ij down_e(act(gate_e x_i) * (up_e x_i)) (+ residual), e = ids_ij.
+ *   X, xdtype   [M, D], M <= 64: SLIM_F16 or SLIM_BF16 with row stride ldx, or SLIM_Q8_E4M3 with xexps, whose values stand for x.
+ *   gate, up    E weights of rows F, columns D, each as slim_pack8's, one after the other (codes E [F/16 up][D/128 up] tiles, exponents
+ *               E [F/128 up] rows). up NULL: h = act(gate x).            down     E weights of rows D, columns F.
+ *   act         a slim_act.
+ *   ids, weights  [M, top] as slim_route's, E <= 512, top <= 16. A number outside 0 .. E - 1 adds nothing (a row of padding, a dropped
+ *               token); one that is twice in a row adds twice.
+ *   residual    [M, D] of `dtype`, row stride ldres, or NULL.
+ *   Y, dtype    out, SLIM_F16 or SLIM_BF16, row stride ldy; may be the residual.
+ *   ws          slim_moe8_workspace(M, D, F, E, top) bytes; its contents need not be kept or cleared.
+ * x is not rounded to 8 bits, nor is h, which is held to 16 significant bits; sums are fp32, the experts' of a row in order of number.
+ */
+int slim_route_workspace(int64_t M, int64_t E, size_t* bytes);
+int slim_route(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t K, int64_t ldx, const void* Wr, int wdtype, int64_t E,
+               int64_t ldw, int top, int renorm, int32_t* ids, float* weights, void* ws, size_t ws_bytes, void* stream);
+int slim_moe8_workspace(int64_t M, int64_t D, int64_t F, int64_t E, int top, size_t* bytes);
+int slim_moe8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t D, int64_t ldx, int64_t F, int64_t E, const uint8_t* gate,
+              const uint8_t* gate_exps, const uint8_t* up, const uint8_t* up_exps, const uint8_t* down, const uint8_t* down_exps, int act,
+              const int32_t* ids, const float* weights, int top, const void* residual, int64_t ldres, void* Y, int dtype, int64_t ldy,
+              void* ws, size_t ws_bytes, void* stream);
+
+/*
  * slim_grad_w8 - the weight gradient dY^T X with X [M, K] an 8-bit checkpoint (xcodes, xexps).
  *   dY, dtype   [M, N], SLIM_F16 or SLIM_BF16, row stride lddy. X is widened to the same type: exact in
  *               bf16 from 2^-130 on; in fp16 values below its normal range are rounded to multiples of

@@ -14,7 +14,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslim.so")
 SOURCES = ["api.cpp", "pack.hip", "adapter_gemm.hip", "sparse_gemm.hip", "mid_gemm.hip", "train.hip", "quant.hip", "lora.hip", "hybrid.hip", "act8.hip",
-           "linear8.hip", "linear8_act.hip", "norm.hip", "grad_w8.hip", "timing.hip"]
+           "linear8.hip", "linear8_act.hip", "moe8.hip", "norm.hip", "grad_w8.hip", "timing.hip"]
 ARCH = "gfx950"
 
 

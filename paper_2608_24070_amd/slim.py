@@ -85,6 +85,13 @@ _SIGS = {
     "slim_act_bwd_workspace": (ctypes.c_int, [_c_i64, _c_i64, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
     "slim_act_bwd": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_i64, _c_i64, ctypes.c_int, _c_p, ctypes.c_int, _c_p, _c_i64, _c_p,
                                     _c_p, _c_i64, _c_p, _c_i64, _c_p, _c_i64, _c_p, _c_p, ctypes.c_size_t, _c_p]),
+    "slim_route_workspace": (ctypes.c_int, [_c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_route": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_i64, _c_i64, ctypes.c_int,
+                                  ctypes.c_int, _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]),
+    "slim_moe8_workspace": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_i64, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_moe8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p,
+                                 ctypes.c_int, _c_p, _c_p, ctypes.c_int, _c_p, _c_i64, _c_p, ctypes.c_int, _c_i64, _c_p, ctypes.c_size_t,
+                                 _c_p]),
     "slim_grad_w8_workspace": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, ctypes.c_int, ctypes.c_int,
                                               ctypes.POINTER(ctypes.c_size_t)]),
     "slim_grad_w8": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_p, _c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_p, _c_p,
@@ -322,6 +329,28 @@ def slim_act_bwd(dH, dtype, lddh, M, K, act, U, udtype, uexps, ldu, mul, mulexps
                  stream) -> int:
     return lib().slim_act_bwd(dH, dtype, lddh, M, K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul, dbias, ws,
                               ws_bytes, stream)
+
+
+def slim_route_workspace(M, E) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().slim_route_workspace(M, E, ctypes.byref(out)), "slim_route_workspace")
+    return out.value
+
+
+def slim_route(X, xdtype, xexps, M, K, ldx, Wr, wdtype, E, ldw, top, renorm, ids, weights, ws, ws_bytes, stream) -> int:
+    return lib().slim_route(X, xdtype, xexps, M, K, ldx, Wr, wdtype, E, ldw, top, renorm, ids, weights, ws, ws_bytes, stream)
+
+
+def slim_moe8_workspace(M, D, F, E, top) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().slim_moe8_workspace(M, D, F, E, top, ctypes.byref(out)), "slim_moe8_workspace")
+    return out.value
+
+
+def slim_moe8(X, xdtype, xexps, M, D, ldx, F, E, gate, gate_exps, up, up_exps, down, down_exps, act, ids, weights, top, residual, ldres, Y,
+              dtype, ldy, ws, ws_bytes, stream) -> int:
+    return lib().slim_moe8(X, xdtype, xexps, M, D, ldx, F, E, gate, gate_exps, up, up_exps, down, down_exps, act, ids, weights, top,
+                           residual, ldres, Y, dtype, ldy, ws, ws_bytes, stream)
 
 
 def slim_grad_w8_workspace(M, N, K, masked, aligned) -> int:
@@ -1205,6 +1234,116 @@ def act_bwd(dh, u, act: str = "none", mul=None, bias: bool = False, out=None, ws
     if rc:
         raise SlimError(rc, "slim_act_bwd")
     return out, dmul, dbias
+
+
+def pack8_experts(W, stream=None) -> dict:
+    """slim_pack8 of each of the weights W [E, N, K] (fp16, bf16 or fp32): {"codes", "exps", "E", "N", "K"}, one weight after the
+    other, as moe8 takes them."""
+    if stream is not None:
+        return _on_its_stream(stream, pack8_experts, W)
+    torch = _torch()
+    if W.dim() != 3 or not W.is_cuda:
+        raise ValueError("W must be a 3-D tensor on the GPU")
+    E, N, K = W.shape
+    up = lambda a, b: -(-a // b)
+    codes = torch.empty((E, up(N, 16), up(K, 128), 2, 4, 16, 16), dtype=torch.uint8, device=W.device)
+    exps = torch.empty((E, up(N, 128), up(K, 512) * 4), dtype=torch.uint8, device=W.device)
+    one = torch.empty_like(exps[0])      # a weight's exponents in a place of their own: slim_pack8's are 16-byte aligned
+    for e in range(E):
+        n, k, ldw, dev = _matrix(W[e], "W[e]")
+        _check(slim_pack8(W[e].data_ptr(), _float_code(W.dtype), n, k, ldw, codes[e].data_ptr(), one.data_ptr(), None, None,
+                          _stream_on(dev)), "slim_pack8")
+        exps[e].copy_(one)
+    return {"codes": codes, "exps": exps, "E": E, "N": N, "K": K}
+
+
+def _rows_in(X, what: str):
+    """(pointer, type, exponents, rows, columns, stride, device, tensor) of rows in 8 bits or of a float type."""
+    if type(X) is dict:
+        x, xe, M, K, dev = _rows8(X)
+        return x.data_ptr(), SLIM_Q8_E4M3, xe.data_ptr(), M, K, 0, dev, x
+    M, K, ldx, dev = _matrix(X, what)
+    return X.data_ptr(), _float_code(X.dtype), None, M, K, ldx, dev, X
+
+
+def route(X, router, top: int, renorm: bool = True, ws=None, stream=None):
+    """slim_route: (ids int32 [M, top], weights fp32 [M, top]), the `top` largest of softmax(X router^T) in each row of X [M, K] (fp16,
+    bf16 or fp32, or 8-bit rows), router [E, K] of any float type; with `renorm` a row's weights sum to one."""
+    if stream is not None:
+        return _on_its_stream(stream, route, X, router, top, renorm, ws)
+    torch = _torch()
+    xp, xdt, xe, M, K, ldx, dev, x = _rows_in(X, "X")
+    E, k, ldw, d = _matrix(router, "router")
+    if k != K or d != dev:
+        raise ValueError("the router must have X's width and be on its device")
+    wdt = _float_code(router.dtype)
+    if not 1 <= top <= E:
+        raise ValueError(f"top must be 1 .. {E}, got {top}")
+    ids = x.new_empty((M, top), dtype=torch.int32)
+    weights = x.new_empty((M, top), dtype=torch.float32)
+    L, st = lib(), _stream_on(dev)
+    need = ctypes.c_size_t()
+    rc = L.slim_route_workspace(M, E, need)
+    if not rc:
+        wp, wn = _given8(need.value, ws, x, st)
+        rc = L.slim_route(xp, xdt, xe, M, K, ldx, router.data_ptr(), wdt, E, ldw, top, 1 if renorm else 0, ids.data_ptr(),
+                          weights.data_ptr(), wp, wn, st)
+    if rc:
+        raise SlimError(rc, "slim_route")
+    return ids, weights
+
+
+def _experts8(p: dict, E: int, N: int, K: int, dev: int, what: str):
+    codes, exps = p["codes"], p["exps"]
+    if (p["E"], p["N"], p["K"]) != (E, N, K):
+        raise ValueError(f"{what} must be {E} weights of ({N}, {K}), got {p['E']} of ({p['N']}, {p['K']})")
+    if codes.shape != (E, (N + 15) // 16, (K + 127) // 128, 2, 4, 16, 16) or exps.shape != (E, (N + 127) // 128, (K + 511) // 512 * 4):
+        raise ValueError(f"{what}: codes and exponents do not have the shape of 8-bit weights")
+    _bytes_on_gpu(codes, exps)
+    if codes.get_device() != dev or exps.get_device() != dev:
+        raise ValueError(f"X and {what} must be on one device")
+    return codes.data_ptr(), exps.data_ptr()
+
+
+def moe8(X, gate: dict, up: dict | None, down: dict, ids, weights, act: str = "silu", residual=None, dtype=None, out=None, ws=None,
+         stream=None):
+    """slim_moe8: Y [M, D] = sum over a row's experts e of weight * down_e(act(gate_e x) * (up_e x)) (+ residual) for up to 64 rows X
+    [M, D] (fp16, bf16 or 8-bit rows). gate, up (or None) and down: pack8_experts of [E, F, D], [E, F, D], [E, D, F]; ids int32 and
+    weights fp32 [M, top] as route's. Y in `dtype`, fp16 or bf16 (default X's type; bf16 for 8-bit rows)."""
+    if stream is not None:
+        return _on_its_stream(stream, moe8, X, gate, up, down, ids, weights, act, residual, dtype, out, ws)
+    torch = _torch()
+    xp, xdt, xe, M, D, ldx, dev, x = _rows_in(X, "X")
+    a, E, F = _act_code(act), gate["E"], gate["N"]
+    gp, ge = _experts8(gate, E, F, D, dev, "gate")
+    up_p, up_e = (None, None) if up is None else _experts8(up, E, F, D, dev, "up")
+    dp, de = _experts8(down, E, D, F, dev, "down")
+    if ids.dim() != 2 or ids.shape != weights.shape or ids.shape[0] != M:
+        raise ValueError(f"ids and weights must be ({M}, top)")
+    if ids.dtype is not torch.int32 or weights.dtype is not torch.float32:
+        raise TypeError("ids must be int32 and weights fp32")
+    _on_gpu(ids, weights)
+    if ids.get_device() != dev or weights.get_device() != dev:
+        raise ValueError("X, ids and weights must be on one device")
+    top = ids.shape[1]
+    if dtype is None:
+        dtype = out.dtype if out is not None else torch.bfloat16 if xdt == SLIM_Q8_E4M3 else X.dtype
+    dt = _float_code(dtype)
+    rp, ldr = _like_rows(residual, M, D, dtype, dev, "residual")
+    if out is None:
+        out, ldy = x.new_empty((M, D), dtype=dtype), D
+    else:
+        ldy = _matrix_out(out, M, D, dtype, dev)
+    L, st = lib(), _stream_on(dev)
+    need = ctypes.c_size_t()
+    rc = L.slim_moe8_workspace(M, D, F, E, top, need)
+    if not rc:
+        wp, wn = _given8(need.value, ws, x, st)
+        rc = L.slim_moe8(xp, xdt, xe, M, D, ldx, F, E, gp, ge, up_p, up_e, dp, de, a, ids.data_ptr(), weights.data_ptr(), top, rp, ldr,
+                         out.data_ptr(), dt, ldy, wp, wn, st)
+    if rc:
+        raise SlimError(rc, "slim_moe8")
+    return out
 
 
 def grad_w8(dY, q: dict, p: dict | None = None, out=None, ws=None, stream=None):
