@@ -59,10 +59,10 @@ k_act8_tile(TileCall<Fin> c) {
 }
 
 // Ends rows whose sums (`slices` of them, fp32 [M][N up to 4] each, added in slice order) or whose dh (16 bits) lie in memory: `lpr`
-// lanes take a row of 8 lpr columns, a block the rows r0 .. r0 + per, four of each lane's in flight while the last four are ended.
+// lanes take a row of 8 lpr columns, a block the rows r0 .. r0 + per, four of a lane's at a time; other waves fill the time between.
 // Bound by HBM.
 template <bool BWD, int DT, bool SUMS>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
 k_act8_rows(const void* __restrict__ src, int64_t ld, int slices, int64_t stride, int64_t M, int64_t N, int per, int lpr, uint32_t strips,
             ActRows<BWD, DT> fin) {
   __shared__ float red[4 * 512];
@@ -71,54 +71,54 @@ k_act8_rows(const void* __restrict__ src, int64_t ld, int slices, int64_t stride
   const int64_t col = 8 * (strip * lpr + lane % lpr);
   const int rows = (int)(M - r0 < per ? M - r0 : per), step = 4 * (64 / lpr), at0 = wave * (64 / lpr) + lane / lpr;
   typename ActRows<BWD, DT>::Lane l;
-  fin.begin(l, r0, col);
-  struct Row {
-    typename ActRows<BWD, DT>::In in;
-    u32x4_t d;
-  };
-  const auto load = [&](Row& r, int row) {
-    const bool ok = row < rows;
-    fin.load(r.in, l, row, ok);
-    r.d = u32x4_t{0, 0, 0, 0};
-    if constexpr (!SUMS)
-      if (ok && l.n) r.d = ActRows<BWD, DT>::load16(reinterpret_cast<const char*>(src) + 2 * ((r0 + row) * ld + col), l.n);
-  };
-  const auto sum8 = [&](int row, float* f) {
-    if constexpr (SUMS) {
+  fin.begin(l, r0 + at0, step, col);
+  const int todo = fin.todo();
+  typedef typename ActRows<BWD, DT>::In In;
+  const auto turns = [&](auto whole) SLIM_INLINE {
+    constexpr bool W = decltype(whole)::value;
+    const auto there = [&](int row) { return W || (row < rows && l.n); };
+    const auto load = [&](u32x4_t* d, In* in, int row) SLIM_INLINE {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = 0.f;
-      if (row >= rows) return;
-      const float* s = reinterpret_cast<const float*>(src) + (r0 + row) * ld + col;
-      for (int i = 0; i < slices; ++i, s += stride) {
-        const f4_t z = {0.f, 0.f, 0.f, 0.f};
-        const f4_t lo = l.n > 0 ? *reinterpret_cast<const f4_t*>(s) : z, hi = l.n > 4 ? *reinterpret_cast<const f4_t*>(s + 4) : z;
+      for (int b = 0; b < 4; ++b) {
+        d[b] = u32x4_t{0, 0, 0, 0};
+        if constexpr (!SUMS)
+          if (there(row + step * b))
+            d[b] = ActRows<BWD, DT>::load16(reinterpret_cast<const char*>(src) + 2 * ((r0 + row + step * b) * ld + col), W ? 8 : l.n);
+      }
+      fin.template load4<W>(in, l, todo, step, rows - row);
+    };
+#pragma unroll 1
+    for (int t = 0; t < rows; t += 4 * step) {      // the same number of turns for every lane
+      u32x4_t d[4];
+      In in[4];
+      load(d, in, t + at0);
+      float f[4][8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          f[e] += lo[e];
-          f[4 + e] += hi[e];
+      for (int b = 0; b < 4; ++b) {
+        if constexpr (SUMS) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[b][e] = 0.f;
+          if (!there(t + at0 + step * b)) continue;
+          const float* s = reinterpret_cast<const float*>(src) + (r0 + t + at0 + step * b) * ld + col;
+          for (int i = 0; i < slices; ++i, s += stride) {
+            const f4_t lo = *reinterpret_cast<const f4_t*>(s);
+            const f4_t hi = W || l.n > 4 ? *reinterpret_cast<const f4_t*>(s + 4) : f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              f[b][e] += lo[e];
+              f[b][4 + e] += hi[e];
+            }
+          }
+        } else {
+          act8_to_f(d[b], DT == 1, f[b]);
         }
       }
+      fin.template end4<W>(l, in, todo, step, rows - t - at0, f);
     }
   };
-  Row cur[4];
-#pragma unroll
-  for (int b = 0; b < 4; ++b) load(cur[b], at0 + step * b);
-#pragma unroll 1
-  for (int t = 0; t < rows; t += 4 * step) {      // the same number of turns for every lane
-    Row next[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) load(next[b], t + at0 + step * (4 + b));
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int row = t + at0 + step * b;
-      float f[8];
-      if constexpr (SUMS) sum8(row, f);
-      else act8_to_f(cur[b].d, DT == 1, f);
-      fin.eight(l, cur[b].in, row, row < rows, f);
-    }
-#pragma unroll
-    for (int b = 0; b < 4; ++b) cur[b] = next[b];
-  }
+  // whole turns of whole columns need no bounds
+  if (rows % (4 * step) == 0 && 8 * (strip + 1) * lpr <= N) turns(std::true_type{});
+  else turns(std::false_type{});
   if (fin.sums_wanted()) {
     // over the row places of a wave, then over the waves in order
 #pragma unroll

@@ -399,23 +399,52 @@ SLIM_DEV void tile_body(const uint8_t* __restrict__ X, const uint8_t* __restrict
   if constexpr (Fin::kRows) {
     // The sums leave through LDS as fp32, fragment by fragment (16 columns of 16 rows; a row's place among its 16 is XORed by
     // the column's, so that reads along a row spread over the banks), 16 FC rows at a time; then 16 lanes take a row of 128 columns,
-    // eight each, and end it. A lane keeps its columns, so that sums over rows stay in it. What a row's end has to read is
-    // loaded four rows ahead, the first four before the sums are written.
+    // eight each, and end it, four such rows at a time. A lane keeps its columns, so that sums over rows stay in it. What the rows'
+    // ends have to read is loaded four rows ahead.
     constexpr int FC = WK == 1 ? FM / 2 : FM, kWaves = 512 / TN, kStep = 4 * kWaves, kTurns = 16 * FC / kStep;
     static_assert(TN % 128 == 0 && kTurns % 4 == 0 && 4 * FC * 4096 <= (int)sizeof(lds));
     f4_t* const all = reinterpret_cast<f4_t*>(lds);
     const int cg = wave / kWaves, at0 = (wave % kWaves) * 4 + eq;
     const int64_t col = n0 + 128 * cg + 8 * er;
     typename Fin::Lane lane8;
-    fin.begin(lane8, m0, col);
-    // a lane's two fours of a row: wave column and fragment column of its eight columns
+    fin.begin(lane8, m0 + at0, kStep, col);
+    const int todo = fin.todo();
+    // a lane's two fours of a row: wave column and fragment column of its eight columns; rows kStep apart stand in one fragment, or
+    // at the same place of the next
     const int pn = (er & 7) >> 1, pq = (er & 1) * 2, pw = 2 * cg + (er >> 3);
+    const f4_t* from[16 / kStep][2];
+#pragma unroll
+    for (int v = 0; v < 16 / kStep; ++v)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        from[v][k] = all + (pw * FC * 4 + pn) * 64 + (pq + k) * 16 + ((at0 + kStep * v) ^ ((pn * 4 + pq + k) ^ (pw & 1)));
+    const auto rows_end = [&](auto whole, int left) __attribute__((always_inline)) {      // `left` rows from this lane's next one on
+      constexpr bool W = decltype(whole)::value;
+      typename Fin::In in[4];
+      fin.template load4<W>(in, lane8, todo, kStep, left);
+#pragma unroll 1
+      for (int t = 0; t < kTurns; t += 4, left -= 4 * kStep) {
+        float f[4][8];
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const f4_t v = from[b % (16 / kStep)][k][(kStep * t / 16 + kStep * b / 16) * 256];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[b][4 * k + e] = v[e];
+          }
+        typename Fin::In next[4];
+        if (t + 4 < kTurns) fin.template load4<W>(next, lane8, todo, kStep, left - 4 * kStep);
+        __builtin_amdgcn_sched_barrier(0);
+        fin.template end4<W>(lane8, in, todo, kStep, left, f);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) in[b] = next[b];
+      }
+    };
+    const bool whole = rows == TM && n0 + TN <= N;
     each<FM / FC>([&](auto hc) {
       constexpr int h = decltype(hc)::value;
-      const int left = rows - 16 * FC * h;
-      typename Fin::In in[4];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) fin.load(in[b], lane8, 16 * FC * h + at0 + kStep * b, at0 + kStep * b < left);
       if constexpr (h > 0) __syncthreads();
 #pragma unroll
       for (int f = 0; f < FC; ++f) {
@@ -435,26 +464,9 @@ SLIM_DEV void tile_body(const uint8_t* __restrict__ X, const uint8_t* __restrict
         }
         __syncthreads();
       }
-#pragma unroll 1
-      for (int t = 0; t < kTurns; t += 4) {
-        typename Fin::In next[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int row = at0 + kStep * (t + 4 + b);
-          fin.load(next[b], lane8, 16 * FC * h + row, t + 4 < kTurns && row < left);
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int row = at0 + kStep * (t + b);
-          const f4_t* const p = all + ((pw * FC + (row >> 4)) * 4 + pn) * 64;
-          const int sw0 = (row & 15) ^ ((pn * 4 + pq) ^ (pw & 1)), sw1 = (row & 15) ^ ((pn * 4 + pq + 1) ^ (pw & 1));
-          const f4_t lo = p[pq * 16 + sw0], hi = p[pq * 16 + 16 + sw1];
-          float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-          fin.eight(lane8, in[b], 16 * FC * h + row, row < left, f);
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) in[b] = next[b];
-      }
+      const int left = rows - 16 * FC * h - at0;
+      if (whole) rows_end(std::true_type{}, left);
+      else rows_end(std::false_type{}, left);
     });
     // sums over the tile's rows: the four row places of a wave, then the waves of a column group in wave order
     if (fin.sums_wanted()) {

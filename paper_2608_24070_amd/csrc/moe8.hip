@@ -146,62 +146,62 @@ k_route_top(const float* __restrict__ logits, int64_t M, int E, int top, int ren
 }
 
 // ------------------------------------------------------------------------------------- who goes where
-// The picked experts in order of number, and the rows that picked each with their weights, in order of row. A row that names an expert
-// twice is there once, with both weights; a number outside 0 .. E - 1 is nowhere.
+// The picked experts in order of number, each with a run of places: the rows that picked it with their weights, in order of row. A
+// row that names an expert twice is there once, with both weights; a number outside 0 .. E - 1 is nowhere. Slots behind the last
+// expert have n = 0.
+struct Slot {
+  int expert, start, n, pad;
+};
 struct Table {
-  int experts;                       // that were picked
-  int expert[kExperts], start[kExperts + 1];
+  int experts, pad[3];
+  Slot slot[kExperts];
   int row[kTokens * kTop];
   float weight[kTokens * kTop];
 };
 
+// One block: a thread a pair of row and expert (two at most), then a thread an expert.
 __global__ void __launch_bounds__(512)
 k_moe_table(const int32_t* __restrict__ ids, const float* __restrict__ weights, int M, int top, int E, Table* __restrict__ t) {
   constexpr int P = kTokens * kTop;
   typedef int i32x4_t __attribute__((ext_vector_type(4)));
   __shared__ __attribute__((aligned(16))) int id[P];
   __shared__ float weight[P];
+  __shared__ int count[kExperts], first[kExperts];
   __shared__ int sums[2][8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pairs = M * top;
-  for (int i = tid; i < P; i += 512) {
-    const int e = i < pairs ? ids[i] : -1;
+  count[tid] = 0;
+#pragma unroll
+  for (int k = 0; k < P / 512; ++k) {
+    const int i = tid + 512 * k, e = i < pairs ? ids[i] : -1;
     id[i] = e >= 0 && e < E ? e : -1;
     weight[i] = i < pairs ? weights[i] : 0.f;
   }
   __syncthreads();
-  // a pair whose expert is in its row once more before it goes; the first one takes the weights
-  int keep[P / 512];
+  // of an expert's pairs in one row the first takes all weights
+  int mine[P / 512];
   float total[P / 512];
 #pragma unroll
   for (int k = 0; k < P / 512; ++k) {
     const int i = tid + 512 * k;
-    keep[k] = id[i];
+    mine[k] = id[i];
     total[k] = weight[i];
     if (i < pairs) {
       const int j = i % top, end = i - j + top;
       for (int o = i - j; o < i; ++o)
-        if (id[o] == keep[k]) keep[k] = -1;
+        if (id[o] == mine[k]) mine[k] = -1;
       for (int o = i + 1; o < end; ++o)
-        if (id[o] == keep[k]) total[k] += weight[o];
+        if (id[o] == mine[k]) total[k] += weight[o];
     }
   }
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < P / 512; ++k) {
-    id[tid + 512 * k] = keep[k];
-    weight[tid + 512 * k] = total[k];
+    id[tid + 512 * k] = mine[k];
+    if (mine[k] >= 0) atomicAdd(&count[mine[k]], 1);
   }
   __syncthreads();
-  // a thread an expert: how many pairs name it
-  const int fours = (pairs + 3) / 4, me = tid < E ? tid : -2;
-  const i32x4_t* const id4 = reinterpret_cast<const i32x4_t*>(id);
-  int n = 0;
-#pragma unroll 8
-  for (int i = 0; i < fours; ++i) {
-    const i32x4_t v = id4[i];
-    n += (v[0] == me) + (v[1] == me) + (v[2] == me) + (v[3] == me);
-  }
-  // places of experts and of their rows: sums over the threads up to this one
+  // places of experts and of their runs: sums over the experts up to this one
+  const int n = count[tid];
   int a = n > 0, b = n;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
@@ -216,28 +216,63 @@ k_moe_table(const int32_t* __restrict__ ids, const float* __restrict__ weights, 
     sums[1][wave] = b;
   }
   __syncthreads();
-  for (int w = 0; w < wave; ++w) {
-    a += sums[0][w];
-    b += sums[1][w];
-  }
-  if (n > 0) {
-    t->expert[a - 1] = tid;
-    t->start[a] = b;
-    int p = b - n;
-#pragma unroll 4
-    for (int i = 0; i < fours; ++i) {
-      const i32x4_t v = id4[i];
+  int experts = 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (v[k] == me) {
-          t->row[p] = (4 * i + k) / top;
-          t->weight[p++] = weight[4 * i + k];
-        }
+  for (int w = 0; w < 8; ++w) {
+    if (w < wave) {
+      a += sums[0][w];
+      b += sums[1][w];
+    }
+    experts += sums[0][w];
+  }
+  first[tid] = b - n;
+  if (n > 0) t->slot[a - 1] = Slot{tid, b - n, n, 0};
+  if (tid >= experts) t->slot[tid] = Slot{0, 0, 0, 0};
+  if (tid == 0) t->experts = experts;
+  __syncthreads();
+  // a pair's place in its run: how many before it name the same expert
+  const i32x4_t* const id4 = reinterpret_cast<const i32x4_t*>(id);
+#pragma unroll
+  for (int k = 0; k < P / 512; ++k) {
+    const int i = tid + 512 * k;
+    if (512 * k >= pairs) break;
+    int before = 0;
+#pragma unroll 8
+    for (int o = 0; o < (pairs + 3) / 4; ++o) {
+      const i32x4_t v = id4[o];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) before += v[c] == mine[k] && 4 * o + c < i;
+    }
+    if (mine[k] >= 0) {
+      t->row[first[mine[k]] + before] = i / top;
+      t->weight[first[mine[k]] + before] = total[k];
     }
   }
-  if (tid == 511) t->experts = a;
-  if (tid == 0) t->start[0] = 0;
 }
+
+// What a kernel knows of it: the table, or for one row the numbers themselves (a slot for each, its place the slot's own).
+struct Picks {
+  const Table* t;          // null: one row
+  const int32_t* ids;
+  const float* weights;
+  int top, E;
+
+  SLIM_DEV Slot slot(int s) const {
+    if (t) return t->slot[s];
+    const int e = ids[s];
+    bool good = e >= 0 && e < E;
+    for (int o = 0; o < s; ++o) good &= ids[o] != e;
+    return Slot{good ? e : 0, s, good ? 1 : 0, 0};
+  }
+  SLIM_DEV int row(int place) const { return t ? t->row[place] : 0; }
+  SLIM_DEV float weight(int place) const {
+    if (t) return t->weight[place];
+    float w = weights[place];
+    for (int o = place + 1; o < top; ++o)
+      if (ids[o] == ids[place]) w += weights[o];
+    return w;
+  }
+};
 
 // ------------------------------------------------------------------------------------- experts
 // 32 codes of a lane as four operands of eight 16-bit values, times 2^(b - 127) (weights: b = 127, exact).
@@ -275,7 +310,6 @@ struct Experts {
 };
 
 // 8 values of a row from column c on, zeros past K; p is null for a row that is not there.
-template <int XT>
 SLIM_DEV b8_t x_eight(const uint8_t* p, int c, int K) {
   u32x4_t v = {0, 0, 0, 0};
   if (p && c < K) {
@@ -291,206 +325,273 @@ SLIM_DEV b8_t x_eight(const uint8_t* p, int c, int K) {
   return __builtin_bit_cast(b8_t, v);
 }
 
-// h = act(gate x) * (up x) of the rows that picked expert `slot`: a block takes 16 columns of h, its eight waves the reduction's groups of
-// 128 in turn. Weight tiles go straight from memory to registers, two groups of a wave in flight; the rows' values come from L2.
-// h leaves as the sum of two bf16 values, 16 significant bits in fp32's range: hi [pairs][F up to 128], then lo.
-// GATED: whether there is an up. (A template's parameter: with a branch on w.up between the gate's products and the reads of their
-// results the compiler leaves out the wait states that the way past the up's products needs.)
-template <int XT, bool GATED>
-__global__ void __launch_bounds__(512)
-k_moe_up(const uint8_t* __restrict__ X, const uint8_t* __restrict__ xe, int64_t ldx, Experts w, const Table* __restrict__ t,
-         uint16_t* __restrict__ hi, uint16_t* __restrict__ lo, int tiles) {
-  constexpr int AT = XT == SLIM_Q8_E4M3 ? 1 : XT, FM = kTokens / 16, U = 2, T = GATED ? 2 : 1;
-  __shared__ f4_t part[8][T * FM][64];
-  const int slot = blockIdx.x / tiles;
-  if (slot >= t->experts) return;
-  const int e = t->expert[slot], p0 = t->start[slot], n = t->start[slot + 1] - p0;
-  const int64_t tile = blockIdx.x - (int64_t)slot * tiles, Ft = (w.F + 15) / 16, Fp = q8_row(w.F);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
-  const int K = (int)w.D, G = (int)(q8_row(K) / 128), Ge = (G + 3) & ~3, fm = (n + 15) / 16;
-  f4_t acc[T][FM];
+// act(gate x) and up x of one tile of 16 columns for the FM sixteens of a slot's rows, summed over this wave's groups of 128: its weight
+// tiles go straight from memory to registers, U groups of a wave in flight with the rows' values for them (from L2).
+template <int XT, int T, int FM, int U, int W>
+SLIM_DEV void up_groups(const uint8_t* X, const uint8_t* xe, int64_t ldx, const Picks& picks, const Slot& slot, int K,
+                        const uint8_t* const* wp, const uint8_t* const* we, int wave, int lane, f4_t (*acc)[T]) {
+  constexpr int AT = XT == SLIM_Q8_E4M3 ? 1 : XT;
+  const int r = lane & 15, q = lane >> 4, G = (int)(q8_row(K) / 128), Ge = (G + 3) & ~3;
+  const uint8_t* xp[FM];
+  const uint8_t* xs[FM];
 #pragma unroll
-  for (int k = 0; k < T; ++k)
+  for (int f = 0; f < FM; ++f) {
+    const bool in = 16 * f + r < slot.n;
+    const int64_t m = in ? picks.row(slot.start + 16 * f + r) : 0;
+    xp[f] = !in ? nullptr : XT == SLIM_Q8_E4M3 ? X + m * G * 128 + 32 * q : X + 2 * m * ldx;
+    xs[f] = XT == SLIM_Q8_E4M3 ? xe + m * Ge : nullptr;
 #pragma unroll
-    for (int f = 0; f < FM; ++f) acc[k][f] = f4_t{0.f, 0.f, 0.f, 0.f};
-  if (tile < Ft) {
-    const int64_t at = ((int64_t)e * Ft + tile) * G * 2048 + lane * 16, ea = ((int64_t)e * ((w.F + 127) / 128) + tile / 8) * Ge;
-    const uint8_t* const wp[2] = {w.gate + at, GATED ? w.up + at : nullptr};
-    const uint8_t* const we[2] = {w.gate_e + ea, GATED ? w.up_e + ea : nullptr};
-    const uint8_t* xp[FM];
-    const uint8_t* xs[FM];
+    for (int k = 0; k < T; ++k) acc[f][k] = f4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  for (int g0 = wave; g0 < G; g0 += W * U) {
+    u32x4_t c[U][T][2];
+    float s[U][T];
+    b8_t x[U][FM][4];
 #pragma unroll
-    for (int f = 0; f < FM; ++f) {
-      const bool in = 16 * f + r < n;
-      const int64_t m = in ? t->row[p0 + 16 * f + r] : 0;
-      xp[f] = !in ? nullptr : XT == SLIM_Q8_E4M3 ? X + m * G * 128 + 32 * q : X + 2 * m * ldx;
-      xs[f] = XT == SLIM_Q8_E4M3 ? xe + m * Ge : nullptr;
+    for (int u = 0; u < U; ++u) {
+      const int g = g0 + W * u;
+      if (g < G) {
+#pragma unroll
+        for (int k = 0; k < T; ++k) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) c[u][k][h] = *reinterpret_cast<const u32x4_t*>(wp[k] + (int64_t)g * 2048 + 1024 * h);
+          s[u][k] = q8_pow2(we[k][g]);
+        }
+      }
     }
-    for (int g = wave; g < G; g += 8 * U) {
-      u32x4_t c[U][T][2];
-      float s[U][T];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (g + 8 * u < G)
+    for (int u = 0; u < U; ++u) {
+      const int g = g0 + W * u;
+      if (g < G)
 #pragma unroll
-          for (int k = 0; k < T; ++k) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) c[u][k][h] = *reinterpret_cast<const u32x4_t*>(wp[k] + (int64_t)(g + 8 * u) * 2048 + 1024 * h);
-            s[u][k] = q8_pow2(we[k][g + 8 * u]);
-          }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (g + 8 * u < G) {
-          b8_t wv[T][4];
-#pragma unroll
-          for (int k = 0; k < T; ++k) widen<AT>(c[u][k], 1.f, wv[k]);
-#pragma unroll
-          for (int f = 0; f < FM; ++f)
-            if (f < fm) {
-              b8_t x[4];
-              if constexpr (XT == SLIM_Q8_E4M3) {
-                u32x4_t xc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-                float xsc = 1.f;
-                if (xp[f]) {
-                  xc[0] = *reinterpret_cast<const u32x4_t*>(xp[f] + (g + 8 * u) * 128);
-                  xc[1] = *reinterpret_cast<const u32x4_t*>(xp[f] + (g + 8 * u) * 128 + 16);
-                  xsc = q8_pow2(xs[f][g + 8 * u]);
-                }
-                widen<1>(xc, xsc, x);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = x_eight<XT>(xp[f], (g + 8 * u) * 128 + 32 * q + 8 * i, K);
-              }
-#pragma unroll
-              for (int k = 0; k < T; ++k) {
-                f4_t d = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) d = mfma_of<AT>(wv[k][i], x[i], d);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[k][f][i] = __builtin_fmaf(d[i], s[u][k], acc[k][f][i]);
-              }
+        for (int f = 0; f < FM; ++f) {
+          if constexpr (XT == SLIM_Q8_E4M3) {
+            // codes and exponent for now, widened where they are used
+            u32x4_t v[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+            u32x4_t e = {127, 0, 0, 0};
+            if (xp[f]) {
+              v[0] = *reinterpret_cast<const u32x4_t*>(xp[f] + g * 128);
+              v[1] = *reinterpret_cast<const u32x4_t*>(xp[f] + g * 128 + 16);
+              e[0] = xs[f][g];
             }
+            x[u][f][0] = __builtin_bit_cast(b8_t, v[0]);
+            x[u][f][1] = __builtin_bit_cast(b8_t, v[1]);
+            x[u][f][2] = __builtin_bit_cast(b8_t, e);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[u][f][i] = x_eight(xp[f], g * 128 + 32 * q + 8 * i, K);
+          }
         }
     }
-  }
 #pragma unroll
-  for (int f = 0; f < FM; ++f)
-    if (f < fm)
+    for (int u = 0; u < U; ++u)
+      if (g0 + W * u < G) {
+        b8_t wv[T][4];
 #pragma unroll
-      for (int k = 0; k < T; ++k) part[wave][T * f + k][lane] = acc[k][f];
-  __syncthreads();
-  if (wave < fm) {
-    f4_t a = part[0][T * wave][lane], b = part[0][T * wave + T - 1][lane];
+        for (int k = 0; k < T; ++k) widen<AT>(c[u][k], 1.f, wv[k]);
 #pragma unroll
-    for (int k = 1; k < 8; ++k) {
-      a += part[k][T * wave][lane];
-      if constexpr (GATED) b += part[k][T * wave + 1][lane];
-    }
-    if (16 * wave + r < n) {
-      float h[4];
-      with_act(w.act, [&](auto A) {
+        for (int f = 0; f < FM; ++f) {
+          b8_t xv[4];
+          if constexpr (XT == SLIM_Q8_E4M3) {
+            const u32x4_t v[2] = {__builtin_bit_cast(u32x4_t, x[u][f][0]), __builtin_bit_cast(u32x4_t, x[u][f][1])};
+            widen<1>(v, q8_pow2(__builtin_bit_cast(u32x4_t, x[u][f][2])[0]), xv);
+          } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = act_value<decltype(A)::value>(a[i]);
-      });
-      u32x2_t vh, vl;
-      uint32_t bh[4], bl[4];
+            for (int i = 0; i < 4; ++i) xv[i] = x[u][f][i];
+          }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float v = 16 * tile + 4 * q + i < w.F ? (GATED ? h[i] * b[i] : h[i]) : 0.f;
-        bh[i] = to_bf16(v);
-        const float left = v - __builtin_bit_cast(float, bh[i] << 16);
-        bl[i] = __builtin_fabsf(left) < __builtin_inff() ? to_bf16(left) : 0u;      // of an infinite or NaN value nothing is left
+          for (int k = 0; k < T; ++k) {
+            f4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d = mfma_of<AT>(wv[k][i], xv[i], d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[f][k][i] = __builtin_fmaf(d[i], s[u][k], acc[f][k][i]);
+          }
+        }
       }
-      vh = u32x2_t{bh[0] | bh[1] << 16, bh[2] | bh[3] << 16};
-      vl = u32x2_t{bl[0] | bl[1] << 16, bl[2] | bl[3] << 16};
-      const int64_t to = (int64_t)(p0 + 16 * wave + r) * Fp + 16 * tile + 4 * q;
-      *reinterpret_cast<u32x2_t*>(hi + to) = vh;
-      *reinterpret_cast<u32x2_t*>(lo + to) = vl;
-    }
   }
 }
 
-// y = sum over the picked experts of weight * (down h): a block takes 16 columns of y and one of `parts` parts of all experts'
-// groups of 128; its waves take consecutive ones, and add each expert's results to sums of their own in LDS, which are added in wave
-// order. With one part y leaves (with the residual), else its fp32 sums.
-template <int DT>
-__global__ void __launch_bounds__(512)
-k_moe_down(const uint16_t* __restrict__ hi, const uint16_t* __restrict__ lo, Experts w, const Table* __restrict__ t, int M, int parts,
-           float* __restrict__ sums, const uint16_t* __restrict__ res, int64_t ldres, uint16_t* __restrict__ Y, int64_t ldy) {
-  constexpr int FM = kTokens / 16, U = 4;
-  __shared__ __attribute__((aligned(16))) float all[8 * kTokens * 16];          // [8 waves][M][16]
+// h = act(gate x) * (up x) of the rows that picked the expert of a slot, 16 columns of h a block, the reduction's groups over its four
+// waves, whose sums are added through LDS in wave order. h leaves as the sum of two bf16 values, 16 significant bits in fp32's range:
+// hi [pairs][F up to 128], then lo. GATED: whether there is an up. (A template's parameter: with a branch on w.up between the gate's
+// products and the reads of their results the compiler leaves out the wait states that the way past the up's products needs.)
+template <int XT, bool GATED>
+__global__ void __launch_bounds__(256, 2)
+k_moe_up(const uint8_t* __restrict__ X, const uint8_t* __restrict__ xe, int64_t ldx, Experts w, Picks picks, uint16_t* __restrict__ hi,
+         uint16_t* __restrict__ lo, int tiles) {
+  constexpr int FM = kTokens / 16, T = GATED ? 2 : 1, W = 4;
+  __shared__ f4_t part[W][T * FM][64];
+  const int at = blockIdx.x / tiles;
+  const Slot slot = picks.slot(at);
+  if (slot.n == 0) return;
+  const int64_t tile = blockIdx.x - (int64_t)at * tiles, Ft = (w.F + 15) / 16, Fp = q8_row(w.F);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
-  const int tile = blockIdx.x / parts, part = blockIdx.x - tile * parts;
-  const int G = (int)(q8_row(w.F) / 128), Ge = (G + 3) & ~3;
-  const int64_t Dt = (w.D + 15) / 16, Db = (w.D + 127) / 128, Fp = (int64_t)G * 128;
-  float* const mine = all + wave * M * 16;
-  for (int i = lane; i < M * 4; i += 64) *reinterpret_cast<f4_t*>(mine + 4 * i) = f4_t{0.f, 0.f, 0.f, 0.f};
-  const int units = t->experts * G, w8 = part * 8 + wave;              // fewer than 2^25
-  const int from = (int)((int64_t)units * w8 / (8 * parts)), to = (int)((int64_t)units * (w8 + 1) / (8 * parts));
-  for (int u0 = __builtin_amdgcn_readfirstlane(from), end = __builtin_amdgcn_readfirstlane(to); u0 < end;) {
-    const int slot = __builtin_amdgcn_readfirstlane(u0 / G);
-    const int g0 = u0 - slot * G, g1 = end - slot * G < G ? end - slot * G : G;
-    u0 = slot * G + g1;
-    const int e = t->expert[slot], p0 = t->start[slot], n = t->start[slot + 1] - p0, fm = (n + 15) / 16;
-    const uint8_t* const wp = w.down + ((int64_t)e * Dt + tile) * G * 2048 + lane * 16;
-    const uint8_t* const we = w.down_e + ((int64_t)e * Db + tile / 8) * Ge;
-    int ha[FM];                                    // at most 64 top rows of F up to 2^22, in eights: below 2^30
+  const int K = (int)w.D, G = (int)(q8_row(K) / 128), Ge = (G + 3) & ~3, fm = (slot.n + 15) / 16;
+  if (tile < Ft) {
+    const int64_t to = ((int64_t)slot.expert * Ft + tile) * G * 2048 + lane * 16, te = ((int64_t)slot.expert * ((w.F + 127) / 128) + tile / 8) * Ge;
+    const uint8_t* const wp[2] = {w.gate + to, GATED ? w.up + to : nullptr};
+    const uint8_t* const we[2] = {w.gate_e + te, GATED ? w.up_e + te : nullptr};
+    const auto run = [&](auto fc, auto uc) SLIM_INLINE {
+      constexpr int F = decltype(fc)::value;
+      f4_t acc[F][T];
+      up_groups<XT, T, F, decltype(uc)::value, W>(X, xe, ldx, picks, slot, K, wp, we, wave, lane, acc);
 #pragma unroll
-    for (int f = 0; f < FM; ++f) ha[f] = 16 * f + r < n ? (int)((int64_t)(p0 + 16 * f + r) * Fp / 8) + 4 * q : -1;
-    f4_t acc[FM];
+      for (int f = 0; f < F; ++f)
 #pragma unroll
-    for (int f = 0; f < FM; ++f) acc[f] = f4_t{0.f, 0.f, 0.f, 0.f};
-    for (int g = g0; g < g1; g += U) {
-      u32x4_t c[U][2];
-      float s[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (g + u < g1) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) c[u][h] = *reinterpret_cast<const u32x4_t*>(wp + (int64_t)(g + u) * 2048 + 1024 * h);
-          s[u] = q8_pow2(we[g + u]);
-        }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (g + u < g1) {
-          b8_t wv[4];
-          widen<1>(c[u], 1.f, wv);
-#pragma unroll
-          for (int f = 0; f < FM; ++f)
-            if (f < fm) {
-              f4_t d = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                u32x4_t a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-                if (ha[f] >= 0) {
-                  a = reinterpret_cast<const u32x4_t*>(hi)[(int64_t)(ha[f] + (g + u) * 16 + i)];
-                  b = reinterpret_cast<const u32x4_t*>(lo)[(int64_t)(ha[f] + (g + u) * 16 + i)];
-                }
-                d = mfma_of<1>(wv[i], __builtin_bit_cast(b8_t, a), d);
-                d = mfma_of<1>(wv[i], __builtin_bit_cast(b8_t, b), d);
-              }
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[f][i] = __builtin_fmaf(d[i], s[u], acc[f][i]);
-            }
-        }
-    }
-#pragma unroll
-    for (int f = 0; f < FM; ++f)
-      if (16 * f + r < n) {                        // an expert's rows are distinct
-        f4_t* const a = reinterpret_cast<f4_t*>(mine + t->row[p0 + 16 * f + r] * 16 + 4 * q);
-        const float k = t->weight[p0 + 16 * f + r];
-        *a += acc[f] * k;
-      }
+        for (int k = 0; k < T; ++k) part[wave][T * f + k][lane] = acc[f][k];
+    };
+    using std::integral_constant;
+    if (fm == 1) run(integral_constant<int, 1>{}, integral_constant<int, 4>{});
+    else if (fm == 2) run(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+    else run(integral_constant<int, 4>{}, integral_constant<int, 1>{});
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < M * 16; i += 512) {
+  if (wave < fm && 16 * wave + r < slot.n) {
+    float h[4] = {0.f, 0.f, 0.f, 0.f};
+    if (tile < Ft) {
+      f4_t a = part[0][T * wave][lane], b = part[0][T * wave + T - 1][lane];
+#pragma unroll
+      for (int k = 1; k < W; ++k) {
+        a += part[k][T * wave][lane];
+        if constexpr (GATED) b += part[k][T * wave + 1][lane];
+      }
+      with_act(w.act, [&](auto A) SLIM_INLINE {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = act_value<decltype(A)::value>(a[i]);
+      });
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = 16 * tile + 4 * q + i < w.F ? (GATED ? h[i] * b[i] : h[i]) : 0.f;      // zeros up to the group's end
+    }
+    uint32_t bh[4], bl[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bh[i] = to_bf16(h[i]);
+      const float left = h[i] - __builtin_bit_cast(float, bh[i] << 16);
+      bl[i] = __builtin_fabsf(left) < __builtin_inff() ? to_bf16(left) : 0u;      // of an infinite or NaN value nothing is left
+    }
+    const int64_t to = (int64_t)(slot.start + 16 * wave + r) * Fp + 16 * tile + 4 * q;
+    *reinterpret_cast<u32x2_t*>(hi + to) = u32x2_t{bh[0] | bh[1] << 16, bh[2] | bh[3] << 16};
+    *reinterpret_cast<u32x2_t*>(lo + to) = u32x2_t{bl[0] | bl[1] << 16, bl[2] | bl[3] << 16};
+  }
+}
+
+// Groups g0 .. g1 of a slot's h times NT tiles of 16 of its expert's down, added with the rows' weights to this wave's sums
+// mine [M][16 NT] in LDS. U groups in flight.
+template <int NT, int FM, int U>
+SLIM_DEV void down_groups(const u32x4_t* hi, const u32x4_t* lo, const Picks& picks, const Slot& slot, int G, int g0, int g1,
+                          const uint8_t* wp, const int* next, const uint8_t* we, int lane, float* mine) {
+  const int r = lane & 15, q = lane >> 4;
+  int ha[FM];                                      // in eights: at most 64 top rows of F up to 2^22, below 2^30
+#pragma unroll
+  for (int f = 0; f < FM; ++f) ha[f] = 16 * f + r < slot.n ? (slot.start + 16 * f + r) * G * 16 + 4 * q : -1;
+  f4_t acc[FM][NT];
+#pragma unroll
+  for (int f = 0; f < FM; ++f)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[f][n] = f4_t{0.f, 0.f, 0.f, 0.f};
+  for (int g = g0; g < g1; g += U) {
+    u32x4_t c[U][NT][2], a[U][FM][4], b[U][FM][4];
+    float s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (g + u < g1) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) c[u][n][h] = *reinterpret_cast<const u32x4_t*>(wp + (int64_t)(g + u) * 2048 + next[n] + 1024 * h);
+        s[u] = q8_pow2(we[g + u]);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (g + u < g1)
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            a[u][f][i] = b[u][f][i] = u32x4_t{0, 0, 0, 0};
+            if (ha[f] >= 0) {
+              a[u][f][i] = hi[(int64_t)(ha[f] + (g + u) * 16 + i)];
+              b[u][f][i] = lo[(int64_t)(ha[f] + (g + u) * 16 + i)];
+            }
+          }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (g + u < g1)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          b8_t wv[4];
+          widen<1>(c[u][n], 1.f, wv);
+#pragma unroll
+          for (int f = 0; f < FM; ++f) {
+            f4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              d = mfma_of<1>(wv[i], __builtin_bit_cast(b8_t, a[u][f][i]), d);
+              d = mfma_of<1>(wv[i], __builtin_bit_cast(b8_t, b[u][f][i]), d);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[f][n][i] = __builtin_fmaf(d[i], s[u], acc[f][n][i]);
+          }
+        }
+  }
+#pragma unroll
+  for (int f = 0; f < FM; ++f)
+    if (16 * f + r < slot.n) {                     // an expert's rows are distinct
+      const int place = slot.start + 16 * f + r;
+      float* const row = mine + picks.row(place) * 16 * NT + 4 * q;
+      const float k = picks.weight(place);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) *reinterpret_cast<f4_t*>(row + 16 * n) += acc[f][n] * k;
+    }
+}
+
+// y = sum over the slots of weight * (down h): a block takes 16 NT columns of y and one of `parts` parts of all slots' groups of 128; its
+// W waves take consecutive ones, and add each expert's results to sums of their own in LDS, which are added in wave order. With one
+// part y leaves (with the residual), else its fp32 sums. (Eight tiles of a weight share one row of exponents, and NT divides eight.)
+template <int DT, int NT, int W>
+__global__ void __launch_bounds__(64 * W, W == 4 ? 2 : 1)
+k_moe_down(const u32x4_t* __restrict__ hi, const u32x4_t* __restrict__ lo, Experts w, Picks picks, int slots, int M, int parts,
+           float* __restrict__ sums, const uint16_t* __restrict__ res, int64_t ldres, uint16_t* __restrict__ Y, int64_t ldy) {
+  __shared__ __attribute__((aligned(16))) float all[W * kTokens * 16 * NT];          // [W][M][16 NT]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int strip = blockIdx.x / parts, part = blockIdx.x - strip * parts;
+  const int G = (int)(q8_row(w.F) / 128), Ge = (G + 3) & ~3;
+  const int D = (int)w.D, Dt = (D + 15) / 16, Db = (D + 127) / 128, tile = strip * NT;
+  float* const mine = all + wave * M * 16 * NT;
+  for (int i = lane; i < M * 4 * NT; i += 64) *reinterpret_cast<f4_t*>(mine + 4 * i) = f4_t{0.f, 0.f, 0.f, 0.f};
+  const int used = picks.t ? picks.t->experts : slots;
+  int next[NT];                                               // the strip's tiles from its first on; past the last: not stored
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    next[n] = (tile + n < Dt ? n : Dt - 1 - tile) * G * 2048;
+    asm volatile("" : "+v"(next[n]));                         // scalar registers are short here
+  }
+  const int units = used * G, w8 = part * W + wave;           // fewer than 2^25
+  const int from = __builtin_amdgcn_readfirstlane((int)((int64_t)units * w8 / (W * parts)));
+  const int end = __builtin_amdgcn_readfirstlane((int)((int64_t)units * (w8 + 1) / (W * parts)));
+  for (int u0 = from; u0 < end;) {
+    const int s = __builtin_amdgcn_readfirstlane(u0 / G);
+    const int g0 = u0 - s * G, g1 = end - s * G < G ? end - s * G : G;
+    u0 = s * G + g1;
+    const Slot slot = picks.slot(s);
+    if (slot.n == 0) continue;
+    const uint8_t* const wp = w.down + ((int64_t)slot.expert * Dt + tile) * G * 2048 + lane * 16;
+    const uint8_t* const we = w.down_e + ((int64_t)slot.expert * Db + tile / 8) * Ge;
+    if (slot.n <= 16) down_groups<NT, 1, NT == 1 ? 4 : 2>(hi, lo, picks, slot, G, g0, g1, wp, next, we, lane, mine);
+    else      // 32 rows at a time: what an expert has past them reads its weights again, from L2
+      for (int done = 0; done < slot.n; done += 32)
+        down_groups<NT, 2, NT == 1 ? 2 : 1>(hi, lo, picks, Slot{slot.expert, slot.start + done, slot.n - done, 0}, G, g0, g1, wp, next, we, lane, mine);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < M * 16 * NT; i += 64 * W) {
     float v = all[i];
 #pragma unroll
-    for (int k = 1; k < 8; ++k) v += all[k * M * 16 + i];
-    const int64_t m = i >> 4, col = (int64_t)tile * 16 + (i & 15);
-    if (col >= w.D) continue;
+    for (int k = 1; k < W; ++k) v += all[k * M * 16 * NT + i];
+    const int64_t m = i / (16 * NT), col = tile * 16 + i % (16 * NT);
+    if (col >= D) continue;
     if (parts > 1) {
-      sums[((int64_t)part * M + m) * w.D + col] = v;
+      sums[((int64_t)part * M + m) * D + col] = v;
     } else {
       if (res) v += load_elem<DT>(res, m * ldres + col);
       store_elem<DT>(Y, m * ldy + col, v);
@@ -516,15 +617,22 @@ bool is_16(int t) { return t == SLIM_F16 || t == SLIM_BF16; }
 bool is_float(int t) { return is_16(t) || t == SLIM_F32; }
 size_t elem(int t) { return t == SLIM_F32 ? 4 : 2; }
 
+// Four tiles of y a block where h, which every strip reads, would cost more than its weights do; parts of the reduction as long as they
+// fill the chip, each wave with eight groups at least.
 struct MoePlan {
-  int parts;
+  int tiles, waves, slots, parts;
+  int64_t strips;
   size_t table, h, sums;
 };
-MoePlan moe_plan(int64_t M, int64_t D, int64_t F, int64_t top) {
+MoePlan moe_plan(int64_t M, int64_t D, int64_t F, int64_t E, int64_t top) {
   MoePlan p;
-  const int64_t tiles = cdiv(D, 16);
-  p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(8, 256 / tiles));
-  p.table = round256(sizeof(Table));
+  p.slots = (int)(M == 1 ? top : std::min<int64_t>(E, M * top));
+  p.tiles = M <= 2 ? 1 : 4;
+  p.waves = p.tiles == 1 ? 8 : 4;
+  p.strips = cdiv(cdiv(D, 16), p.tiles);
+  const int64_t units = p.slots * (q8_row(F) / 128), fill = p.tiles == 1 ? 256 : 512;
+  p.parts = (int)std::max<int64_t>(1, std::min({fill / p.strips, units / (8 * p.waves), int64_t(16)}));
+  p.table = M == 1 ? 0 : round256(sizeof(Table));
   p.h = round256((size_t)(M * top * q8_row(F) * 2));
   p.sums = p.parts > 1 ? round256((size_t)(p.parts * M * D * 4)) : 0;
   return p;
@@ -590,10 +698,10 @@ extern "C" int slim_moe8_workspace(int64_t M, int64_t D, int64_t F, int64_t E, i
   if (!bytes) return SLIM_EINVAL;
   if (M < 0 || D < 1 || F < 1 || E < 1 || top < 1 || D > kMaxRow8 || F > kMaxRow8) return SLIM_ESHAPE;
   if (M > kTokens || E > kExperts || top > kTop) return SLIM_EUNSUPPORTED;
-  if (!one_launch(std::min<int64_t>(E, M * top) * (q8_row(F) / 16), 512)) return SLIM_EUNSUPPORTED;
+  if (!one_launch(std::max<int64_t>(top, std::min<int64_t>(E, M * top)) * (q8_row(F) / 16), 256)) return SLIM_EUNSUPPORTED;
   *bytes = 0;
   if (M == 0) return SLIM_OK;
-  const MoePlan p = moe_plan(M, D, F, top);
+  const MoePlan p = moe_plan(M, D, F, E, top);
   *bytes = p.table + 2 * p.h + p.sums;
   return SLIM_OK;
 }
@@ -618,25 +726,26 @@ extern "C" int slim_moe8(const void* X, int xdtype, const uint8_t* xexps, int64_
   if (!ws || ws_bytes < need) return SLIM_EWORKSPACE;
   if (!slim_aligned16(ws)) return SLIM_EALIGN;
   hipStream_t s = (hipStream_t)stream;
-  const MoePlan p = moe_plan(M, D, F, top);
+  const MoePlan p = moe_plan(M, D, F, E, top);
   char* at = reinterpret_cast<char*>(ws);
   Table* t = reinterpret_cast<Table*>(at);
   uint16_t* hi = reinterpret_cast<uint16_t*>(at + p.table);
   uint16_t* lo = reinterpret_cast<uint16_t*>(at + p.table + p.h);
   float* sums = reinterpret_cast<float*>(at + p.table + 2 * p.h);
   const Experts w{gate, gate_exps, up, up_exps, down, down_exps, D, F, (int)E, act};
-  {
+  const Picks picks{M == 1 ? nullptr : t, ids, weights, top, (int)E};
+  if (M > 1) {
     SlimKernelTimer timer("moe_table", s);
     SLIM_LAUNCH(timer, k_moe_table, dim3(1), dim3(512), s, ids, weights, (int)M, top, (int)E, t);
   }
   {
     const int tiles = (int)(q8_row(F) / 16);
-    const dim3 grid((unsigned)(std::min<int64_t>(E, M * top) * tiles));
+    const dim3 grid((unsigned)((int64_t)p.slots * tiles));
     const uint8_t* x = reinterpret_cast<const uint8_t*>(X);
     SlimKernelTimer timer("moe_up", s);
     const auto call = [&](auto xt) {
       constexpr int XT = decltype(xt)::value;
-      SLIM_LAUNCH(timer, (up ? k_moe_up<XT, true> : k_moe_up<XT, false>), grid, dim3(512), s, x, xexps, ldx, w, (const Table*)t, hi, lo, tiles);
+      SLIM_LAUNCH(timer, (up ? k_moe_up<XT, true> : k_moe_up<XT, false>), grid, dim3(256), s, x, xexps, ldx, w, picks, hi, lo, tiles);
     };
     if (packed) call(std::integral_constant<int, SLIM_Q8_E4M3>{});
     else if (xdtype == SLIM_F16) call(std::integral_constant<int, SLIM_F16>{});
@@ -645,10 +754,14 @@ extern "C" int slim_moe8(const void* X, int xdtype, const uint8_t* xexps, int64_
   const uint16_t* res = reinterpret_cast<const uint16_t*>(residual);
   uint16_t* y = reinterpret_cast<uint16_t*>(Y);
   {
-    const dim3 grid((unsigned)(cdiv(D, 16) * p.parts));
+    const dim3 grid((unsigned)(p.strips * p.parts));
     SlimKernelTimer timer("moe_down", s);
-    SLIM_LAUNCH(timer, (dtype == SLIM_F16 ? k_moe_down<0> : k_moe_down<1>), grid, dim3(512), s, hi, lo, w, (const Table*)t, (int)M, p.parts, sums,
-                res, ldres, y, ldy);
+    const auto call = [&](auto kernel, int waves) {
+      SLIM_LAUNCH(timer, kernel, grid, dim3(64 * waves), s, reinterpret_cast<const u32x4_t*>(hi), reinterpret_cast<const u32x4_t*>(lo), w, picks,
+                  p.slots, (int)M, p.parts, sums, res, ldres, y, ldy);
+    };
+    if (p.tiles == 1) call(dtype == SLIM_F16 ? k_moe_down<0, 1, 8> : k_moe_down<1, 1, 8>, 8);
+    else call(dtype == SLIM_F16 ? k_moe_down<0, 4, 4> : k_moe_down<1, 4, 4>, 4);
   }
   if (p.parts > 1) {
     const dim3 grid((unsigned)cdiv(M * D, 256));

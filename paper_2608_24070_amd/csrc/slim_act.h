@@ -6,6 +6,9 @@
 #include "slim.h"
 #include "slim_q8.h"
 
+// A lambda that is always inlined: one that is not keeps what it refers to in memory.
+#define SLIM_INLINE __attribute__((always_inline))
+
 // f(integral_constant A) for the activation `act` (uniform)
 template <class F>
 SLIM_DEV void with_act(int act, F&& f) {
@@ -50,12 +53,12 @@ SLIM_DEV void act_both(float x, float& v, float& d) {
     v = x * phi;
     d = __builtin_fmaf(x * 0.398942280f, e, phi);
   } else if constexpr (A == SLIM_ACT_GELU_TANH) {
-    // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y)), y = sqrt(2 / pi) (x + 0.044715 x^3)
-    const float y2 = x * __builtin_fmaf(0.0713548163f, x * x, 1.59576912f), p = act_rcp(1.f + act_exp(-y2));
+    // (1 + tanh y) / 2 = 1 / (1 + 2^(-2 y log2 e)), y = sqrt(2 / pi) (x + 0.044715 x^3); past 12 that is 0 or 1 to fp32, and the slope's
+    // second term nothing, so x^2 may stop there and stays in range
+    const float c = __builtin_amdgcn_fmed3f(x, -12.f, 12.f), c2 = c * c;
+    const float p = act_rcp(1.f + __builtin_amdgcn_exp2f(x * __builtin_fmaf(-0.102943240f, c2, -2.30220819f)));
     v = x * p;
-    // past 12 the second term is below 2^-126 and its factors may pass fp32's range
-    const float c = x > 12.f ? 12.f : x < -12.f ? -12.f : x;
-    d = __builtin_fmaf(c * p * (1.f - p), __builtin_fmaf(0.214064449f, c * c, 1.59576912f), p);
+    d = __builtin_fmaf(c * __builtin_fmaf(-p, p, p), __builtin_fmaf(0.214064449f, c2, 1.59576912f), p);
   } else if constexpr (A == SLIM_ACT_SILU) {
     const float p = act_rcp(1.f + act_exp(-x));
     v = x * p;
@@ -95,59 +98,73 @@ struct ActArgs {
   float* part;                                                  // backward: sums of y over each block's rows [blocks][N], or null
 };
 
-// Ends rows eight columns a lane, 16 lanes for 128 columns of a row (all 16 take part in every call). DT: the type of 16-bit
-// rows. Everything is fp32 until the one rounding of a result; a column's sum over rows takes du before it.
-// A lane keeps the places of its columns in the first row; what is uniform is little then, for the tiles' scalar registers.
+// Ends rows eight columns a lane, 16 lanes for 128 columns of a row (all 16 take part in every call), and four rows at a time, `step`
+// apart: their reads, an activation's chains of dependent steps and the choices that are the launch's go side by side. DT: the type of
+// 16-bit rows. Everything is fp32 until the one rounding of a result; a column's sum over rows takes du before it.
+// A lane keeps its places in what is read and in what is written, and the ways to the next row, in vector registers: the tiles' scalar
+// ones are few.
 template <bool BWD, int DT>
 struct ActRows {
   static constexpr bool kRows = true;
   static constexpr int kType = DT;
   ActArgs a;
   struct Lane {
-    int n;               // columns that exist, 0 .. 8
-    int place;           // of the eight in their group of 128 (0 .. 15), or -1 past the last group
-    int tail;            // whether this lane writes one of the zeros behind the row's exponents: how far from its group's
-    const char *p, *q;                 // u, mul or mul, res
+    int n;                             // columns that exist, 0 .. 8
+    int place;                         // of the eight in their group of 128 (0 .. 15), or -1 past the last group
+    int tail;                          // whether this lane writes one of the zeros behind the row's exponents: how far from its group's
+    const char *p, *q;                 // u, mul or mul, res: the next row to read
     const uint8_t *pe, *qe;
-    char *y, *w;
+    char *y, *w;                       // the next row to write
     uint8_t *ye, *we;
+    int64_t p_by, q_by, y_by, w_by;
+    int e_by;
     float bias[8], s[8];
   };
   struct In {
     u32x4_t p, q;
     uint32_t pe, qe;
   };
+  // what there is to do (one scalar)
+  enum { kQ8 = 1, kP = 2, kQ = 4, kW = 8, kBias = 16 };
+  SLIM_DEV int todo() const {
+    return (a.q8 ? kQ8 : 0) | ((BWD ? a.u : a.mul) ? kP : 0) | ((BWD ? a.mul != nullptr : a.res != nullptr) ? kQ : 0) | (a.w ? kW : 0) |
+           (a.bias ? kBias : 0);
+  }
 
   SLIM_DEV bool sums_wanted() const { return BWD && a.part; }
   SLIM_DEV void put_sum(int64_t block, int64_t col, int64_t N, float v) const { a.part[block * N + col] = v; }
-  SLIM_DEV int code_row() const { return (int)q8_row(a.N); }
-  SLIM_DEV int exp_row() const { return (int)q8_exp_row(a.N); }
 
-  // Columns col .. col + 7 of rows from m0 on.
-  SLIM_DEV void begin(Lane& l, int64_t m0, int64_t col) const {
-    const int64_t left = a.N - col, g = col >> 7;
+  template <class T>
+  static SLIM_DEV T in_vector(T v) {
+    asm volatile("" : "+v"(v));
+    return v;
+  }
+
+  // Columns col .. col + 7 of rows m, m + step, ...
+  SLIM_DEV void begin(Lane& l, int64_t m, int step, int64_t col) const {
+    const int64_t left = a.N - col, g = col >> 7, codes = q8_row(a.N), exps = q8_exp_row(a.N);
     l.n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
-    const bool in = col < code_row();
+    const bool in = col < codes;
     l.place = in ? (int)(col >> 3) & 15 : -1;
-    l.tail = in && g == (a.N - 1) >> 7 && l.place > 0 && l.place < 4 && g + l.place < exp_row() ? l.place : 0;
-    const auto at = [&](const void* p, int64_t ld, bool q8) {
-      return reinterpret_cast<const char*>(p) + (q8 ? m0 * code_row() + col : 2 * (m0 * ld + col));
-    };
-    const auto exp_at = [&](const uint8_t* e) { return e + m0 * exp_row() + g; };
-    if constexpr (BWD) {
-      l.p = at(a.u, a.ldu, a.q8);
-      l.q = at(a.mul, a.ldmul, a.q8);
-      l.pe = exp_at(a.ue);
-      l.qe = exp_at(a.me);
-    } else {
-      l.p = at(a.mul, a.ldmul, false);
-      l.q = at(a.res, a.ldres, false);
-    }
-    const bool y8 = !BWD && a.q8;
-    l.y = const_cast<char*>(at(a.y, a.ldy, y8));
-    l.w = const_cast<char*>(at(a.w, a.ldw, y8));
-    l.ye = const_cast<uint8_t*>(exp_at(a.ye));
-    l.we = const_cast<uint8_t*>(exp_at(a.we));
+    l.tail = in && g == (a.N - 1) >> 7 && l.place > 0 && l.place < 4 && g + l.place < exps ? l.place : 0;
+    const bool in8 = BWD && a.q8, out8 = !BWD && a.q8;
+    const auto at = [&](const void* p, int64_t ld, bool q8) { return reinterpret_cast<const char*>(p) + (q8 ? m * codes + col : 2 * (m * ld + col)); };
+    const auto by = [&](int64_t ld, bool q8) { return in_vector((q8 ? codes : 2 * ld) * step); };
+    const auto exp_at = [&](const uint8_t* e) { return e + m * exps + g; };
+    const int64_t ldp = BWD ? a.ldu : a.ldmul, ldq = BWD ? a.ldmul : a.ldres;
+    l.p = at(BWD ? a.u : a.mul, ldp, in8);
+    l.q = at(BWD ? a.mul : a.res, ldq, in8);
+    l.pe = exp_at(a.ue);
+    l.qe = exp_at(a.me);
+    l.y = const_cast<char*>(at(a.y, a.ldy, out8));
+    l.w = const_cast<char*>(at(a.w, a.ldw, out8));
+    l.ye = const_cast<uint8_t*>(exp_at(a.ye)) + l.tail;
+    l.we = const_cast<uint8_t*>(exp_at(a.we)) + l.tail;
+    l.p_by = by(ldp, in8);
+    l.q_by = by(ldq, in8);
+    l.y_by = by(a.ldy, out8);
+    l.w_by = by(a.ldw, out8);
+    l.e_by = in_vector((int)exps * step);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       l.s[e] = 0.f;
@@ -158,10 +175,7 @@ struct ActRows {
   }
 
   // n, compared where it stands: the compiler keeps eight masks in scalar registers over the rows' loop otherwise
-  static SLIM_DEV int here(int n) {
-    asm volatile("" : "+v"(n));
-    return n;
-  }
+  static SLIM_DEV int here(int n) { return in_vector(n); }
   static SLIM_DEV u32x4_t load16(const char* p, int n) {
     u32x4_t v = {0, 0, 0, 0};
     if (n == 8) {
@@ -182,107 +196,152 @@ struct ActRows {
   }
   static SLIM_DEV void values(u32x4_t v, uint32_t b, bool q8, float* f) {
     if (q8) {
-      q8_values4(v[0], q8_pow2(b), f);
-      q8_values4(v[1], q8_pow2(b), f + 4);
+      // (the instruction scales: a multiplication a value less than q8_values4, whose values these are down to 2^-126)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f2_t t = i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v[i >> 1], q8_pow2(b), true)
+                             : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v[i >> 1], q8_pow2(b), false);
+        f[2 * i] = t[0];
+        f[2 * i + 1] = t[1];
+      }
     } else {
       act8_to_f(v, DT == 1, f);
     }
   }
 
-  // What row m0 + row reads, if `ok`.
-  SLIM_DEV void load(In& in, const Lane& l, int row, bool ok) const {
-    in.p = in.q = u32x4_t{0, 0, 0, 0};
-    in.pe = in.qe = 1;
-    if (!ok || l.n == 0) return;
-    if constexpr (BWD) {
-      if (a.q8) {
-        const int64_t c = (int64_t)row * code_row(), e = (int64_t)row * exp_row();
-        if (a.u) {
-          in.p = load_codes(l.p + c);
-          in.pe = l.pe[e];
+  // The next four rows of this lane, of which those `step` b < more are there (WHOLE: all of them and all columns): what they read.
+  template <bool WHOLE>
+  SLIM_DEV void load4(In* in, Lane& l, int todo, int step, int more) const {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      in[b].p = in[b].q = u32x4_t{0, 0, 0, 0};
+      in[b].pe = in[b].qe = 1;
+    }
+    const auto there = [&](int b) { return WHOLE || (step * b < more && l.n > 0); };
+    if (todo & kP) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b, l.p += l.p_by) {
+        if (BWD && (todo & kQ8)) {
+          if (there(b)) {
+            in[b].p = load_codes(l.p);
+            in[b].pe = *l.pe;
+          }
+          l.pe += l.e_by;
+        } else if (there(b)) {
+          in[b].p = load16(l.p, WHOLE ? 8 : l.n);
         }
-        if (a.mul) {
-          in.q = load_codes(l.q + c);
-          in.qe = l.qe[e];
-        }
-      } else {
-        if (a.u) in.p = load16(l.p + 2 * row * a.ldu, l.n);
-        if (a.mul) in.q = load16(l.q + 2 * row * a.ldmul, l.n);
       }
-    } else {
-      if (a.mul) in.p = load16(l.p + 2 * row * a.ldmul, l.n);
-      if (a.res) in.q = load16(l.q + 2 * row * a.ldres, l.n);
     }
-  }
-
-  SLIM_DEV void store_codes(char* p, uint8_t* ep, int row, const Lane& l, bool ok, const float* f) const {
-    float v[8];
-    uint32_t big = 0;
+    if (todo & kQ) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = e < l.n ? f[e] : 0.f;
-      big = max(big, q8_abs(v[e]));
-    }
-    const uint32_t b = q8_exponent(row16_max_u32(big));
-    if (!ok || l.place < 0) return;
-    const float s = q8_inverse(b);
-    *reinterpret_cast<u32x2_t*>(p + (int64_t)row * code_row()) =
-        u32x2_t{q8_codes4(v[0], v[1], v[2], v[3], s), q8_codes4(v[4], v[5], v[6], v[7], s)};
-    uint8_t* const e = ep + (int64_t)row * exp_row();
-    if (l.place == 0 || l.tail) e[l.tail] = l.tail ? 0 : (uint8_t)b;      // the row's last word ends in zeros
-  }
-
-  // Ends row m0 + row, whose sums are f.
-  SLIM_DEV void eight(Lane& l, const In& in, int row, bool ok, float* f) const {
-    float y[8], w[8];
-    if constexpr (BWD) {
-      float u[8];
-      values(in.p, in.pe, a.q8, u);
-      with_act(a.act, [&](auto A) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float v, d;
-          act_both<decltype(A)::value>(u[e], v, d);
-          y[e] = f[e] * d;
-          w[e] = f[e] * v;
+      for (int b = 0; b < 4; ++b, l.q += l.q_by) {
+        if (BWD && (todo & kQ8)) {
+          if (there(b)) {
+            in[b].q = load_codes(l.q);
+            in[b].qe = *l.qe;
+          }
+          l.qe += l.e_by;
+        } else if (there(b)) {
+          in[b].q = load16(l.q, WHOLE ? 8 : l.n);
         }
+      }
+    }
+  }
+
+  template <bool WHOLE>
+  static SLIM_DEV void store_codes4(char*& p, uint8_t*& ep, int64_t by, const Lane& l, int step, int more, const float (*f)[8]) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b, p += by, ep += l.e_by) {
+      float v[8];
+      uint32_t big = 0;
+      const int n = WHOLE ? 8 : here(l.n);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = WHOLE || e < n ? f[b][e] : 0.f;
+        big = max(big, q8_abs(v[e]));
+      }
+      const uint32_t x = q8_exponent(row16_max_u32(big));
+      if (!WHOLE && (step * b >= more || l.place < 0)) continue;
+      const float s = q8_inverse(x);
+      *reinterpret_cast<u32x2_t*>(p) = u32x2_t{q8_codes4(v[0], v[1], v[2], v[3], s), q8_codes4(v[4], v[5], v[6], v[7], s)};
+      if (l.place == 0 || l.tail) *ep = l.tail ? 0 : (uint8_t)x;      // the row's last word ends in zeros
+    }
+  }
+  template <bool WHOLE>
+  static SLIM_DEV void store_row(char* at, const Lane& l, bool there, const float* f) {
+    if constexpr (WHOLE) store8<DT>(at, 0, 8, f);
+    else if (there && l.n) store8<DT>(at, 0, l.n == 8 ? 8 : here(l.n), f);
+  }
+  template <bool WHOLE>
+  static SLIM_DEV void store4(char*& p, int64_t by, const Lane& l, int step, int more, const float (*f)[8]) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b, p += by) store_row<WHOLE>(p, l, step * b < more, f[b]);
+  }
+
+  // Ends the next four rows, whose sums are f.
+  template <bool WHOLE>
+  SLIM_DEV void end4(Lane& l, const In* in, int todo, int step, int more, float (*f)[8]) const {
+    if constexpr (BWD) {
+      with_act(a.act, [&](auto A) SLIM_INLINE {
+        const auto rows = [&](auto gated) SLIM_INLINE {
+#pragma unroll
+          for (int b = 0; b < 4; ++b, l.y += l.y_by) {
+            const bool there = WHOLE || step * b < more;
+            float u[8], m[8], o[8];
+            values(in[b].p, in[b].pe, todo & kQ8, u);
+            if constexpr (decltype(gated)::value) values(in[b].q, in[b].qe, todo & kQ8, m);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float v, d;
+              act_both<decltype(A)::value>(u[e], v, d);
+              o[e] = f[b][e] * v;
+              f[b][e] *= d;
+              if constexpr (decltype(gated)::value) f[b][e] *= m[e];
+              l.s[e] += there ? f[b][e] : 0.f;      // of columns past the last: not asked for
+            }
+            store_row<WHOLE>(l.y, l, there, f[b]);
+            if constexpr (decltype(gated)::value) {
+              store_row<WHOLE>(l.w, l, there, o);
+              l.w += l.w_by;
+            }
+          }
+        };
+        if (todo & kQ) rows(std::true_type{});
+        else rows(std::false_type{});
       });
-      if (a.mul) {
-        values(in.q, in.qe, a.q8, u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= u[e];
-      }
-      if (a.part)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) l.s[e] += ok ? y[e] : 0.f;      // of columns past the last: not asked for
     } else {
+      if (todo & kBias)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = f[e] + l.bias[e];
-      with_act(a.act, [&](auto A) {
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = act_value<decltype(A)::value>(w[e]);
+          for (int e = 0; e < 8; ++e) f[b][e] += l.bias[e];
+      if (todo & kW) {
+        if (todo & kQ8) store_codes4<WHOLE>(l.w, l.we, l.w_by, l, step, more, f);
+        else store4<WHOLE>(l.w, l.w_by, l, step, more, f);
+      }
+      with_act(a.act, [&](auto A) SLIM_INLINE {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[b][e] = act_value<decltype(A)::value>(f[b][e]);
       });
       float o[8];
-      if (a.mul) {
-        act8_to_f(in.p, DT == 1, o);
+      if (todo & kP)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= o[e];
-      }
-      if (a.res) {
-        act8_to_f(in.q, DT == 1, o);
+        for (int b = 0; b < 4; ++b) {
+          act8_to_f(in[b].p, DT == 1, o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] += o[e];
-      }
-      if (a.q8) {
-        store_codes(l.y, l.ye, row, l, ok, y);
-        if (a.w) store_codes(l.w, l.we, row, l, ok, w);
-        return;
-      }
-    }
-    if (ok && l.n) {
-      const int n = l.n == 8 ? 8 : here(l.n);
-      store8<DT>(l.y + 2 * row * a.ldy, 0, n, y);
-      if (a.w) store8<DT>(l.w + 2 * row * a.ldw, 0, n, w);
+          for (int e = 0; e < 8; ++e) f[b][e] *= o[e];
+        }
+      if (todo & kQ)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          act8_to_f(in[b].q, DT == 1, o);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[b][e] += o[e];
+        }
+      if (todo & kQ8) store_codes4<WHOLE>(l.y, l.ye, l.y_by, l, step, more, f);
+      else store4<WHOLE>(l.y, l.y_by, l, step, more, f);
     }
   }
 
@@ -292,7 +351,7 @@ struct ActRows {
     float z[4], y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e] = v[e] + (a.bias && e < left ? load_elem_rt(a.bias, n + e, a.bdt) : 0.f);
-    with_act(a.act, [&](auto A) {
+    with_act(a.act, [&](auto A) SLIM_INLINE {
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = act_value<decltype(A)::value>(z[e]);
     });
