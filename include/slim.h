@@ -615,7 +615,7 @@ int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, int64_t K, 
  *   top         1 .. min(E, 16).                    renorm   nonzero: weights are divided by their row's sum.
  *   ids         out, int32 [M, top]: experts by falling logit, the lower number first where two are equal.
  *   weights     out, fp32 [M, top]: their p.
- *   ws          slim_route_workspace(M, E) bytes; its contents need not be kept or cleared.
+ *   ws          slim_route_workspace(M, E, K) bytes; its contents need not be kept or cleared.
  * Arithmetic is fp32. A row with a NaN among its logits has weights of NaN, and those experts last that gave it.
  *
  * slim_moe8 - a layer of experts for a few tokens: y_i = sum_j w_ij down_e(act(gate_e x_i) * (up_e x_i)) (+ residual), e = ids_ij.
@@ -630,7 +630,7 @@ int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, int64_t K, 
  *   ws          slim_moe8_workspace(M, D, F, E, top) bytes; its contents need not be kept or cleared.
  * x is not rounded to 8 bits, nor is h, which is held to 16 significant bits; sums are fp32, the experts' of a row in order of number.
  */
-int slim_route_workspace(int64_t M, int64_t E, size_t* bytes);
+int slim_route_workspace(int64_t M, int64_t E, int64_t K, size_t* bytes);
 int slim_route(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t K, int64_t ldx, const void* Wr, int wdtype, int64_t E,
                int64_t ldw, int top, int renorm, int32_t* ids, float* weights, void* ws, size_t ws_bytes, void* stream);
 int slim_moe8_workspace(int64_t M, int64_t D, int64_t F, int64_t E, int top, size_t* bytes);

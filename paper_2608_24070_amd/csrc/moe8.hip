@@ -26,30 +26,60 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // ------------------------------------------------------------------------------------- router
-// Logits of RT rows and ET experts a block: a lane takes eight consecutive columns of each 512, its four waves the 512s in turn; sums
-// over lanes, then over waves in order. fp32 throughout: products of two 16-bit values are exact. X: 3 for 8-bit rows.
+// Sums over the lanes of N values each (N a power of two up to 64): lane l ends with value l / (64 / N) of the sum over all lanes. Each step
+// gives half of the values to the other half of the lanes, so that N - 1 exchanges do for all, and the last ones for sums.
+template <int N, int D = 32>
+SLIM_DEV float lanes_sum(float* v, int lane) {
+  if constexpr (D == 0) {
+    return v[0];
+  } else if constexpr (N == 1) {
+    v[0] += __shfl_xor(v[0], D, 64);
+    return lanes_sum<1, D / 2>(v, lane);
+  } else {
+    const bool high = lane & D;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const float other = __shfl_xor(high ? v[i] : v[N / 2 + i], D, 64);
+      v[i] = (high ? v[N / 2 + i] : v[i]) + other;
+    }
+    return lanes_sum<N / 2, D / 2>(v, lane);
+  }
+}
+
+// Parts of the logits: ET experts, up to 2 RT rows and 2048 columns a block. A wave takes 512 columns, a lane eight of them, whose router
+// values stay in registers while RT rows at a time go by; sums over lanes, then over the block's four waves in order, and
+// k_route_top adds the parts. So the router is read once and x comes from L2. fp32 throughout: products of two 16-bit values are exact.
+// X: 3 for 8-bit rows.
+constexpr int kRouteCols = 2048;
+constexpr int route_rows(int rt) { return 2 * rt; }
 template <int XT, int WT, int RT, int ET>
 __global__ void __launch_bounds__(256)
 k_route_logits(const void* __restrict__ X, const uint8_t* __restrict__ xe, int64_t ldx, const void* __restrict__ Wr, int64_t ldw, int64_t M,
-               int K, int E, float* __restrict__ logits) {
-  __shared__ float part[4][RT * ET];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int eb = (E + ET - 1) / ET;
-  const int64_t rb = blockIdx.x / eb, m0 = rb * RT;
-  const int e0 = (int)(blockIdx.x - rb * eb) * ET;
-  float acc[RT][ET] = {};
-  for (int c = 8 * (wave * 64 + lane); c < K; c += 8 * 256) {
-    float w[ET][8], x[RT][8];
+               int K, int E, int parts, float* __restrict__ logits) {
+  constexpr int N = RT * ET, kRows = route_rows(RT);
+  __shared__ float sums[4][kRows * ET];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, eb = (E + ET - 1) / ET;
+  const int64_t rb = blockIdx.x / (eb * parts), m0 = rb * kRows;
+  const int left = (int)(blockIdx.x - rb * eb * parts), part = left / eb, e0 = (left - part * eb) * ET;
+  const int rows = (int)(M - m0 < kRows ? M - m0 : kRows), c = part * kRouteCols + 512 * wave + 8 * lane;
+  float w[ET][8];
 #pragma unroll
-    for (int e = 0; e < ET; ++e) load8<WT>(Wr, (int64_t)(e0 + e < E ? e0 + e : E - 1) * ldw + c, K - c, w[e]);
+  for (int e = 0; e < ET; ++e) load8<WT>(Wr, (int64_t)(e0 + e < E ? e0 + e : E - 1) * ldw + c, K - c, w[e]);      // zeros past K
+  for (int r0 = 0; r0 < rows; r0 += RT) {
+    float x[RT][8], acc[N];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const int64_t m = m0 + r < M ? m0 + r : M - 1;
+      const int64_t m = m0 + (r0 + r < rows ? r0 + r : rows - 1);
       if constexpr (XT == SLIM_Q8_E4M3) {
-        const u32x2_t v = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint8_t*>(X) + m * q8_row(K) + c);
-        const float s = q8_pow2(xe[m * q8_exp_row(K) + (c >> 7)]);
-        q8_values4(v[0], s, x[r]);
-        q8_values4(v[1], s, x[r] + 4);
+        if (c < K) {
+          const u32x2_t v = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint8_t*>(X) + m * q8_row(K) + c);
+          const float s = q8_pow2(xe[m * q8_exp_row(K) + (c >> 7)]);
+          q8_values4(v[0], s, x[r]);
+          q8_values4(v[1], s, x[r] + 4);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[r][i] = 0.f;
+        }
       } else {
         load8<XT>(X, m * ldx + c, K - c, x[r]);
       }
@@ -57,23 +87,21 @@ k_route_logits(const void* __restrict__ X, const uint8_t* __restrict__ xe, int64
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int e = 0; e < ET; ++e)
+      for (int e = 0; e < ET; ++e) {
+        float a = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[r][e] = __builtin_fmaf(x[r][i], w[e][i], acc[r][e]);
+        for (int i = 0; i < 8; ++i) a = __builtin_fmaf(x[r][i], w[e][i], a);
+        acc[r * ET + e] = a;
+      }
+    const float v = lanes_sum<N>(acc, lane);
+    const int i = r0 * ET + lane / (64 / N);
+    if (lane % (64 / N) == 0 && i < rows * ET) sums[wave][i] = v;
   }
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int e = 0; e < ET; ++e) {
-      float v = acc[r][e];
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
-      if (lane == 0) part[wave][r * ET + e] = v;
-    }
   __syncthreads();
-  const int t = threadIdx.x;
-  if (t < RT * ET && m0 + t / ET < M && e0 + t % ET < E)
-    logits[(m0 + t / ET) * E + e0 + t % ET] = part[0][t] + part[1][t] + part[2][t] + part[3][t];
+  for (int i = threadIdx.x; i < rows * ET; i += 256) {
+    const int e = e0 + i % ET;
+    if (e < E) logits[((int64_t)part * M + m0 + i / ET) * E + e] = sums[0][i] + sums[1][i] + sums[2][i] + sums[3][i];
+  }
 }
 
 // fp32 as integers in the same order (-0 below +0: made one before).
@@ -84,21 +112,22 @@ SLIM_DEV uint32_t ordered(float x) {
 
 // A wave per row, experts lane + 64 i: the largest logit that is left, the lowest expert that has it, `top` times. A NaN counts as the
 // least there and leaves all the row's weights NaN.
+template <int N>      // 64 N experts at most
 __global__ void __launch_bounds__(256)
-k_route_top(const float* __restrict__ logits, int64_t M, int E, int top, int renorm, int32_t* __restrict__ ids, float* __restrict__ weights) {
-  constexpr int N = kExperts / 64;
+k_route_top(const float* __restrict__ logits, int parts, int64_t M, int E, int top, int renorm, int32_t* __restrict__ ids,
+            float* __restrict__ weights) {
   const int lane = threadIdx.x & 63;
   const int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (m >= M) return;                                           // whole waves
   float v[N];
   uint32_t key[N];                                              // 0: taken, or no expert
-  uint32_t big = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int e = lane + 64 * i;
-    v[i] = e < E ? logits[m * E + e] : 0.f;
+    v[i] = 0.f;
+    if (e < E)
+      for (int p = 0; p < parts; ++p) v[i] += logits[((int64_t)p * M + m) * E + e];
     key[i] = e < E ? (v[i] == v[i] ? ordered(v[i]) : 1u) : 0u;
-    big = max(big, key[i]);
   }
   float most = 0.f, sum = 0.f, mine = 0.f;
   int at = 0;
@@ -642,12 +671,15 @@ template <int XT, int WT>
 void launch_logits(const void* X, const uint8_t* xe, int64_t ldx, const void* Wr, int64_t ldw, int64_t M, int64_t K, int E, float* logits,
                    hipStream_t s) {
   SlimKernelTimer timer("route_logits", s);
-  if (M >= 8) {
-    SLIM_LAUNCH(timer, (k_route_logits<XT, WT, 8, 4>), dim3((unsigned)(cdiv(M, 8) * cdiv(E, 4))), dim3(256), s, X, xe, ldx, Wr, ldw, M, (int)K, E,
-                logits);
-  } else {
-    SLIM_LAUNCH(timer, (k_route_logits<XT, WT, 1, 1>), dim3((unsigned)(M * E)), dim3(256), s, X, xe, ldx, Wr, ldw, M, (int)K, E, logits);
-  }
+  const int parts = (int)cdiv(K, kRouteCols);
+  // few rows: a block for every expert and two of them, which is all latency (7 x 8 x 4096 3.9 us against 7.7); more: the router's values
+  // are kept over 16 rows (61 x 250 x 8192, fp32 router: 16 us; over all 61 rows, in a quarter of the blocks, 37)
+  if (M >= 8)
+    SLIM_LAUNCH(timer, (k_route_logits<XT, WT, 8, 4>), dim3((unsigned)(cdiv(M, route_rows(8)) * parts * cdiv(E, 4))), dim3(256), s, X, xe, ldx, Wr,
+                ldw, M, (int)K, E, parts, logits);
+  else
+    SLIM_LAUNCH(timer, (k_route_logits<XT, WT, 1, 1>), dim3((unsigned)(cdiv(M, route_rows(1)) * parts * E)), dim3(256), s, X, xe, ldx, Wr, ldw, M,
+                (int)K, E, parts, logits);
 }
 template <int XT>
 void launch_logits(int wdtype, const void* X, const uint8_t* xe, int64_t ldx, const void* Wr, int64_t ldw, int64_t M, int64_t K, int E,
@@ -659,22 +691,23 @@ void launch_logits(int wdtype, const void* X, const uint8_t* xe, int64_t ldx, co
 
 }  // namespace
 
-extern "C" int slim_route_workspace(int64_t M, int64_t E, size_t* bytes) {
+extern "C" int slim_route_workspace(int64_t M, int64_t E, int64_t K, size_t* bytes) {
   if (!bytes) return SLIM_EINVAL;
-  if (M < 0 || E < 1) return SLIM_ESHAPE;
-  if (E > kExperts || M > (int64_t(1) << 23) / E) return SLIM_EUNSUPPORTED;      // blocks of 256 threads in one launch
-  *bytes = (size_t)M * (size_t)E * 4;
+  if (M < 0 || E < 1 || K < 1 || K > kMaxRow8) return SLIM_ESHAPE;
+  if (E > kExperts || M > int64_t(1) << 32 || !one_launch(cdiv(M, route_rows(8)) * cdiv(K, kRouteCols) * E, 256)) return SLIM_EUNSUPPORTED;
+  if (!one_launch(cdiv(M, 4), 256)) return SLIM_EUNSUPPORTED;
+  *bytes = (size_t)cdiv(K, kRouteCols) * (size_t)M * (size_t)E * 4;
   return SLIM_OK;
 }
 
 extern "C" int slim_route(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t K, int64_t ldx, const void* Wr, int wdtype,
                           int64_t E, int64_t ldw, int top, int renorm, int32_t* ids, float* weights, void* ws, size_t ws_bytes, void* stream) {
   size_t need = 0;
-  const int rc = slim_route_workspace(M, E, &need);
+  const int rc = slim_route_workspace(M, E, K, &need);
   if (rc != SLIM_OK) return rc;
   const bool packed = xdtype == SLIM_Q8_E4M3;
   if ((!packed && !is_float(xdtype)) || !is_float(wdtype)) return SLIM_EDTYPE;
-  if (K < 1 || K > kMaxRow8 || ldw < K || (!packed && ldx < K) || top < 1 || top > E) return SLIM_ESHAPE;
+  if (ldw < K || (!packed && ldx < K) || top < 1 || top > E) return SLIM_ESHAPE;
   if (top > kTop) return SLIM_EUNSUPPORTED;
   if (M == 0) return SLIM_OK;
   if (!X || (packed && !xexps) || !Wr || !ids || !weights) return SLIM_EINVAL;
@@ -690,7 +723,8 @@ extern "C" int slim_route(const void* X, int xdtype, const uint8_t* xexps, int64
   else if (xdtype == SLIM_BF16) launch_logits<SLIM_BF16>(wdtype, X, xexps, ldx, Wr, ldw, M, K, (int)E, logits, s);
   else launch_logits<SLIM_F32>(wdtype, X, xexps, ldx, Wr, ldw, M, K, (int)E, logits, s);
   SlimKernelTimer timer("route_top", s);
-  SLIM_LAUNCH(timer, k_route_top, dim3((unsigned)cdiv(M, 4)), dim3(256), s, (const float*)logits, M, (int)E, top, renorm, ids, weights);
+  SLIM_LAUNCH(timer, (E <= 64 ? k_route_top<1> : E <= 128 ? k_route_top<2> : E <= 256 ? k_route_top<4> : k_route_top<8>),
+              dim3((unsigned)cdiv(M, 4)), dim3(256), s, (const float*)logits, (int)cdiv(K, kRouteCols), M, (int)E, top, renorm, ids, weights);
   return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
 }
 

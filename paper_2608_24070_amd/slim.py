@@ -85,7 +85,7 @@ _SIGS = {
     "slim_act_bwd_workspace": (ctypes.c_int, [_c_i64, _c_i64, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
     "slim_act_bwd": (ctypes.c_int, [_c_p, ctypes.c_int, _c_i64, _c_i64, _c_i64, ctypes.c_int, _c_p, ctypes.c_int, _c_p, _c_i64, _c_p,
                                     _c_p, _c_i64, _c_p, _c_i64, _c_p, _c_i64, _c_p, _c_p, ctypes.c_size_t, _c_p]),
-    "slim_route_workspace": (ctypes.c_int, [_c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
+    "slim_route_workspace": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, ctypes.POINTER(ctypes.c_size_t)]),
     "slim_route": (ctypes.c_int, [_c_p, ctypes.c_int, _c_p, _c_i64, _c_i64, _c_i64, _c_p, ctypes.c_int, _c_i64, _c_i64, ctypes.c_int,
                                   ctypes.c_int, _c_p, _c_p, _c_p, ctypes.c_size_t, _c_p]),
     "slim_moe8_workspace": (ctypes.c_int, [_c_i64, _c_i64, _c_i64, _c_i64, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
@@ -331,9 +331,9 @@ def slim_act_bwd(dH, dtype, lddh, M, K, act, U, udtype, uexps, ldu, mul, mulexps
                               ws_bytes, stream)
 
 
-def slim_route_workspace(M, E) -> int:
+def slim_route_workspace(M, E, K) -> int:
     out = ctypes.c_size_t(0)
-    _check(lib().slim_route_workspace(M, E, ctypes.byref(out)), "slim_route_workspace")
+    _check(lib().slim_route_workspace(M, E, K, ctypes.byref(out)), "slim_route_workspace")
     return out.value
 
 
@@ -1118,8 +1118,8 @@ def _rows8_of(q, M: int, N: int, dev: int, what: str):
 def linear8_act(X, p: dict, act: str = "none", bias=None, mul=None, residual=None, pre: bool = False, q8: bool = False, dtype=None,
                 out=None, ws=None, stream=None):
     """slim_linear8_act: Y [M, N] = act(X W^T + bias) * mul + residual with an 8-bit weight (pack8), X as in linear8. `act`: "none",
-    "relu", "gelu", "gelu_tanh" or "silu"; bias [N] of any float type; mul and residual [M, N] of `dtype` (fp16 or bf16, default as
-    linear8). Y in `dtype`, or with `q8` 8-bit rows. With `pre`: (Y, X W^T + bias), the second like Y, for the backward."""
+    "relu", "gelu", "gelu_tanh" or "silu"; bias [N] of any float type; mul and residual [M, N] of `dtype` (fp16 or bf16; default
+    theirs, else as linear8). Y in `dtype`, or with `q8` 8-bit rows. With `pre`: (Y, X W^T + bias), the second like Y, for the backward."""
     if stream is not None:
         return _on_its_stream(stream, linear8_act, X, p, act, bias, mul, residual, pre, q8, dtype, out, ws)
     N, K, a = p["N"], p["K"], _act_code(act)
@@ -1181,7 +1181,7 @@ def _kept_operands(u, mul, M: int, K: int, dtype, dev: int):
 def bwd_dx8_act(dY, p: dict, u, act: str = "none", mul=None, bias: bool = False, dtype=None, out=None, ws=None, stream=None):
     """slim_bwd_dx8_act: (du, dmul, dbias) from dY [M, N] of a product Y = h W^T with h = act(u) * mul: with dh = dY W (pack8 with
     bwd=True) du = dh * mul * act'(u), dmul = dh * act(u) (None without mul), dbias [K] = the sums of du's columns (None unless
-    `bias`), all of `dtype` (as linear8). u and mul [M, K]: of `dtype`, or 8-bit rows."""
+    `bias`), all of `dtype` (default out's or u's, else as linear8). u and mul [M, K]: of `dtype`, or 8-bit rows."""
     if stream is not None:
         return _on_its_stream(stream, bwd_dx8_act, dY, p, u, act, mul, bias, dtype, out, ws)
     N, K, a = p["N"], p["K"], _act_code(act)
@@ -1283,7 +1283,7 @@ def route(X, router, top: int, renorm: bool = True, ws=None, stream=None):
     weights = x.new_empty((M, top), dtype=torch.float32)
     L, st = lib(), _stream_on(dev)
     need = ctypes.c_size_t()
-    rc = L.slim_route_workspace(M, E, need)
+    rc = L.slim_route_workspace(M, E, K, need)
     if not rc:
         wp, wn = _given8(need.value, ws, x, st)
         rc = L.slim_route(xp, xdt, xe, M, K, ldx, router.data_ptr(), wdt, E, ldw, top, 1 if renorm else 0, ids.data_ptr(),

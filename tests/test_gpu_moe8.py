@@ -1,7 +1,7 @@
 """The router and the layer of experts against the oracle in 64 bits.
 
-Bounds. Logits: fp32 products summed in chains of at most K / 2048 + 8 eights a lane and ten additions over lanes and waves, so within
-L = (K / 256 + 80) 2^-24 (the sum of magnitudes) of their value; a weight is off by twice that relatively, and by 2^-20 for e^x and the
+Bounds. Logits: fp32 products summed in chains of eight a lane, ten additions over lanes and waves and one for each 2048 columns, so
+within L = (K / 256 + 80) 2^-24 (the sum of magnitudes) of their value; a weight is off by twice that relatively, and by 2^-20 for e^x and the
 quotient. Experts: each product within 2^-17 of its magnitudes (at most 128 additions in a chain of the matrix unit's group and
 fewer after it); an activation's slope below 1.13, its error below 2^-19 (|g| + 1); h is held to 2^-16; y is rounded by u |y|."""
 import numpy as np
@@ -232,7 +232,7 @@ def test_streams_graph_replays_and_workspaces(m, e, d, f, top):
     # exactly the workspace that is asked for
     ids, weights = slim.route(x, router, top)
     for need, run in ((slim.slim_moe8_workspace(m, d, f, e, top), lambda ws: slim.moe8(x, *packs, ids, weights, ws=ws)),
-                      (slim.slim_route_workspace(m, e), lambda ws: slim.route(x, router, top, ws=ws)[1])):
+                      (slim.slim_route_workspace(m, e, d), lambda ws: slim.route(x, router, top, ws=ws)[1])):
         ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda")
         got = run(ws[:need])
         assert bool((ws[need:] == 0xFF).all()) and torch.equal(got, run(None))
