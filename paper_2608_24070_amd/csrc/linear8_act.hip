@@ -434,7 +434,7 @@ extern "C" int slim_act_bwd_workspace(int64_t M, int64_t K, int sums, size_t* by
   if (M == 0) return SLIM_OK;
   const RowPlan p = row_plan(M, K);
   if (!one_launch(p.strips * p.blocks, 256)) return SLIM_EUNSUPPORTED;
-  if (sums) *bytes = (size_t)p.blocks * (size_t)K * 4;
+  if (sums && p.blocks > 1) *bytes = (size_t)p.blocks * (size_t)K * 4;      // one block's sums are dbias
   return SLIM_OK;
 }
 
@@ -458,9 +458,10 @@ extern "C" int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, 
   if (need && (!ws || ws_bytes < need)) return SLIM_EWORKSPACE;
   if (need && !slim_aligned16(ws)) return SLIM_EALIGN;
   ActArgs a = bwd_args(K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul);
-  a.part = dbias ? reinterpret_cast<float*>(ws) : nullptr;
+  const int64_t blocks = row_plan(M, K).blocks;
+  a.part = !dbias ? nullptr : blocks > 1 ? reinterpret_cast<float*>(ws) : dbias;
   if (dtype == SLIM_F16) launch_rows<true, 0, false>(dH, lddh, 1, 0, M, a, s);
   else launch_rows<true, 1, false>(dH, lddh, 1, 0, M, a, s);
-  if (dbias) launch_sums(a.part, row_plan(M, K).blocks, K, dbias, SLIM_F32, s);
+  if (dbias && blocks > 1) launch_sums(a.part, blocks, K, dbias, SLIM_F32, s);
   return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
 }

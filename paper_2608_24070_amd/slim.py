@@ -1245,6 +1245,8 @@ def pack8_experts(W, stream=None) -> dict:
     if W.dim() != 3 or not W.is_cuda:
         raise ValueError("W must be a 3-D tensor on the GPU")
     E, N, K = W.shape
+    if not E:
+        raise ValueError("W must hold an expert at least")
     up = lambda a, b: -(-a // b)
     codes = torch.empty((E, up(N, 16), up(K, 128), 2, 4, 16, 16), dtype=torch.uint8, device=W.device)
     exps = torch.empty((E, up(N, 128), up(K, 512) * 4), dtype=torch.uint8, device=W.device)

@@ -116,6 +116,8 @@ def test_the_largest_that_are_taken():
     assert slim.slim_moe8_workspace(0, 8192, 28672, 512, 16) == slim.slim_linear8_act_workspace(F16, 0, 10, 10, F16, 1) == 0
     # a row's codes are turned up in the product's own launch
     assert slim.slim_linear8_act_workspace(BF16, 1, 4096, 4096, BF16, 0) == 0
+    # one block's sums over rows are the result
+    assert slim.slim_act_bwd_workspace(16, 4096, 1) == 0 and slim.slim_act_bwd_workspace(17, 4096, 1) > 0
 
 
 gpu = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt).as_subclass(OnGpu)
@@ -176,7 +178,7 @@ def test_binding_refuses_experts_that_do_not_fit(monkeypatch):
                  lambda: slim.moe8(x, g, g, d, ids[:3], w), lambda: slim.moe8(x, g, g, d, ids, w[:, :1]), lambda: slim.moe8(x, g, g, d, ids[:3], w[:3]),
                  lambda: slim.moe8(x, g, g, d, ids.t().contiguous().t(), w), lambda: slim.moe8(x, g, g, d, ids, w, act="swish"),
                  lambda: slim.moe8(x, g, g, d, ids, w, residual=gpu(4, 255)), lambda: slim.moe8(x, g, g, d, ids, w, out=gpu(3, 256)),
-                 lambda: slim.moe8(x, g, g, d, torch.zeros((4, 2), dtype=torch.int32), w), lambda: slim.pack8_experts(gpu(4, 4))):
+                 lambda: slim.moe8(x, g, g, d, torch.zeros((4, 2), dtype=torch.int32), w), lambda: slim.pack8_experts(gpu(4, 4)), lambda: slim.pack8_experts(gpu(0, 4, 4))):
         with pytest.raises(ValueError):
             call()
     for call in (lambda: slim.moe8(x, g, g, d, ids.long(), w), lambda: slim.moe8(x, g, g, d, ids, w.bfloat16()),
