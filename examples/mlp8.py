@@ -1,13 +1,14 @@
 """One pre-norm MLP block, y = x + W2 gelu(W1 norm(x)), trained and served on the 8-bit path.
 
-    python examples/mlp8.py [--d 512] [--ffn 2048] [--tokens 2048] [--steps 200] [--sparse] [--rms]
+    python examples/mlp8.py [--d 512] [--ffn 2048] [--tokens 2048] [--steps 200] [--sparse] [--rms] [--fused]
 
 Forward: the norm writes its result in 8 bits, which is at once the product's operand and all of it that is kept for the
 backward; so are gelu's input and output, and the block's input for the norm's gradient: 2 d + 2 ffn bytes a token instead
 of 4 d + 4 ffn in bf16. Backward: the input gradients are the same product on the transposed packs, the weight gradients
 take the kept 8-bit rows as they are, and the norm's gradient its 8-bit input. With --sparse W2 stays at its 2:4 positions:
 its gradient is computed in compressed form, weight decay is the sparse add, and only kept values change. Master weights
-are fp32; a step packs them anew.
+are fp32; a step packs them anew. With --fused the products end in what follows them: gelu, its result and its argument in 8 bits
+leave the first product's launch, the residual is added in the second's, and the gradient passes gelu in that of its own product.
 """
 import argparse
 import os
@@ -22,13 +23,14 @@ from paper_2608_24070_amd import slim  # noqa: E402
 
 
 class MLP8:
-    def __init__(self, d: int, ffn: int, sparse: bool = False, rms: bool = False, seed: int = 0, device="cuda"):
+    def __init__(self, d: int, ffn: int, sparse: bool = False, rms: bool = False, seed: int = 0, device="cuda",
+                 fused: bool = False):
         g = torch.Generator(device).manual_seed(seed)
         rand = lambda n, k: torch.randn((n, k), generator=g, device=device) * k ** -0.5
         self.w1, self.w2 = rand(ffn, d), rand(d, ffn)
         self.gamma = torch.ones(d, device=device)
         self.beta = None if rms else torch.zeros(d, device=device)
-        self.rms, self.values = rms, None
+        self.rms, self.values, self.fused = rms, None, fused
         if sparse:
             self.values = slim.pack16(self.w2, with_mask=True)
             self.kept = self.values["mask"].bool()
@@ -41,6 +43,8 @@ class MLP8:
     def forward(self, x, keep: bool = True):
         """y for x [tokens, d] in bf16, and with `keep` what the backward needs."""
         n, mean, rstd = slim.norm(x, self.gamma, self.beta, rms=self.rms, q8=True)
+        if self.fused:
+            return self._forward_fused(x, n, mean, rstd, keep)
         u = slim.linear8(n, self.p1)
         h = F.gelu(u)
         if not keep:
@@ -48,9 +52,19 @@ class MLP8:
         h = slim.quant8(h)
         return x + slim.linear8(h, self.p2), {"x": slim.quant8(x), "mean": mean, "rstd": rstd, "n": n, "u": slim.quant8(u), "h": h}
 
+    def _forward_fused(self, x, n, mean, rstd, keep):
+        if not keep:
+            return slim.linear8_act(slim.linear8_act(n, self.p1, act="gelu"), self.p2, residual=x)
+        h, u = slim.linear8_act(n, self.p1, act="gelu", pre=True, q8=True)
+        y = slim.linear8_act(h, self.p2, residual=x)
+        return y, {"x": slim.quant8(x), "mean": mean, "rstd": rstd, "n": n, "u": u, "h": h}
+
     def backward(self, dy, kept):
         """dx and the gradients of the weights (W2's at its kept positions, if it is sparse), gamma and beta."""
-        du = torch.ops.aten.gelu_backward(slim.bwd_dx8(dy, self.p2), slim.dequant8(kept["u"], dy.dtype))
+        if self.fused:
+            du, _, _ = slim.bwd_dx8_act(dy, self.p2, kept["u"], act="gelu", dtype=dy.dtype)
+        else:
+            du = torch.ops.aten.gelu_backward(slim.bwd_dx8(dy, self.p2), slim.dequant8(kept["u"], dy.dtype))
         g = {"w2": slim.grad_w8(dy, kept["h"], self.values), "w1": slim.grad_w8(du, kept["n"])}
         dx, g["gamma"], g["beta"] = slim.norm_bwd(slim.bwd_dx8(du, self.p1), kept["x"], self.gamma, kept["mean"], kept["rstd"])
         return dx + dy, g
@@ -101,9 +115,10 @@ def main():
     a.add_argument("--decay", type=float, default=0.0)
     a.add_argument("--sparse", action="store_true", help="W2 at 2:4 positions (d and ffn in whole 128s)")
     a.add_argument("--rms", action="store_true", help="RMS norm instead of layer norm")
+    a.add_argument("--fused", action="store_true", help="products that end in the activation and the residual")
     a = a.parse_args()
-    model = MLP8(a.d, a.ffn, a.sparse, a.rms)
-    train(MLP8(a.d, a.ffn, a.sparse, a.rms), a.tokens, 2, a.lr, a.decay)
+    model = MLP8(a.d, a.ffn, a.sparse, a.rms, fused=a.fused)
+    train(MLP8(a.d, a.ffn, a.sparse, a.rms, fused=a.fused), a.tokens, 2, a.lr, a.decay)
     torch.cuda.synchronize()
     t = time.time()
     losses = train(model, a.tokens, a.steps, a.lr, a.decay)
