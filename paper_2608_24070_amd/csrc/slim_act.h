@@ -125,10 +125,10 @@ struct ActRows {
     uint32_t pe, qe;
   };
   // what there is to do (one scalar)
-  enum { kQ8 = 1, kP = 2, kQ = 4, kW = 8, kBias = 16 };
+  enum { kQ8 = 1, kP = 2, kQ = 4, kW = 8, kBias = 16, kSums = 32 };
   SLIM_DEV int todo() const {
     return (a.q8 ? kQ8 : 0) | ((BWD ? a.u : a.mul) ? kP : 0) | ((BWD ? a.mul != nullptr : a.res != nullptr) ? kQ : 0) | (a.w ? kW : 0) |
-           (a.bias ? kBias : 0);
+           (a.bias ? kBias : 0) | (a.part ? kSums : 0);
   }
 
   SLIM_DEV bool sums_wanted() const { return BWD && a.part; }
@@ -248,19 +248,31 @@ struct ActRows {
     }
   }
 
+  // The largest finite magnitude's bits of eight values. A NaN loses every comparison of v_max3_f32, whose operands' signs cost
+  // nothing: half an instruction a value, where q8_abs and a maximum take four. An infinity wins; then they are gone through again.
+  static SLIM_DEV uint32_t largest(const float* v) {
+    float m = 0.f;
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(m) : "v"(v[e]), "v"(v[e + 1]));
+#endif
+    uint32_t big = abs_bits(m);
+    if (__ballot(big >= 0x7F800000u)) {
+      big = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) big = max(big, q8_abs(v[e]));
+    }
+    return big;
+  }
   template <bool WHOLE>
   static SLIM_DEV void store_codes4(char*& p, uint8_t*& ep, int64_t by, const Lane& l, int step, int more, const float (*f)[8]) {
 #pragma unroll
     for (int b = 0; b < 4; ++b, p += by, ep += l.e_by) {
       float v[8];
-      uint32_t big = 0;
       const int n = WHOLE ? 8 : here(l.n);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[e] = WHOLE || e < n ? f[b][e] : 0.f;
-        big = max(big, q8_abs(v[e]));
-      }
-      const uint32_t x = q8_exponent(row16_max_u32(big));
+      for (int e = 0; e < 8; ++e) v[e] = WHOLE || e < n ? f[b][e] : 0.f;
+      const uint32_t x = q8_exponent(row16_max_u32(largest(v)));
       if (!WHOLE && (step * b >= more || l.place < 0)) continue;
       const float s = q8_inverse(x);
       *reinterpret_cast<u32x2_t*>(p) = u32x2_t{q8_codes4(v[0], v[1], v[2], v[3], s), q8_codes4(v[4], v[5], v[6], v[7], s)};
@@ -297,8 +309,10 @@ struct ActRows {
               o[e] = f[b][e] * v;
               f[b][e] *= d;
               if constexpr (decltype(gated)::value) f[b][e] *= m[e];
-              l.s[e] += there ? f[b][e] : 0.f;      // of columns past the last: not asked for
             }
+            if (todo & kSums)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) l.s[e] += there ? f[b][e] : 0.f;      // of columns past the last: not asked for
             store_row<WHOLE>(l.y, l, there, f[b]);
             if constexpr (decltype(gated)::value) {
               store_row<WHOLE>(l.w, l, there, o);

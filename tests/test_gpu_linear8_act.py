@@ -238,6 +238,27 @@ def test_nan_rows_stay_apart(m):
         assert bool(got[[1, 3]].isnan().all()) and torch.equal(got[rows], clean[rows])
 
 
+@pytest.mark.parametrize("m", [4, 40, 1500])
+def test_values_that_are_not_finite_stay_alone_in_their_group(m):
+    n, k = 2050, 1300
+    x, w, bias, _, res = case(m, n, k, "bf16")
+    p = slim.pack8(w)
+    bad = res.clone()
+    bad[1, 5], bad[2, 200], bad[3, 2049] = float("nan"), float("inf"), -float("inf")
+    for both in (False, True):
+        if both:
+            bad[2, 201] = float("nan")
+        q = slim.linear8_act(x, p, act="gelu", bias=bias, residual=bad, q8=True)
+        y = slim.linear8_act(x, p, act="gelu", bias=bias, residual=bad, dtype=torch.bfloat16)
+        v = slim.dequant8(q, torch.float32)
+        assert torch.equal(v.isnan(), ~y.isfinite())
+        fine = y.isfinite()
+        # the others as near as 8 bits are, by the largest finite one of their group
+        a = torch.nn.functional.pad(torch.where(fine, y.float().abs(), torch.zeros((), device="cuda")), (0, -n % 128)).view(m, -1, 128).amax(2)
+        lim = 2.0 ** -4 * y.float().abs() * 1.01 + (2.0 ** -10 * 2 / 448 * 1.01) * a.repeat_interleave(128, 1)[:, :n] + 2.0 ** -8 * y.float().abs()
+        assert bool(((v - y.float()).abs() <= lim)[fine].all())
+
+
 def test_no_rows():
     _, w, bias, _, _ = case(1, 70, 300, "bf16")
     p = slim.pack8(w, bwd=True)
