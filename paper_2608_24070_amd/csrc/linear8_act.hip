@@ -59,7 +59,7 @@ k_act8_tile(TileCall<Fin> c) {
 }
 
 // Ends rows whose sums (`slices` of them, fp32 [M][N up to 4] each, added in slice order) or whose dh (16 bits) lie in memory: `lpr`
-// lanes take a row of 8 lpr columns, a block the rows r0 .. r0 + per, four of a lane's at a time; other waves fill the time between.
+// lanes take a row of 8 lpr columns, a block the rows r0 .. r0 + per, two of a lane's in flight while two are ended.
 // Bound by HBM.
 template <bool BWD, int DT, bool SUMS>
 __global__ void __launch_bounds__(256, 2)
@@ -74,27 +74,28 @@ k_act8_rows(const void* __restrict__ src, int64_t ld, int slices, int64_t stride
   fin.begin(l, r0 + at0, step, col);
   const int todo = fin.todo();
   typedef typename ActRows<BWD, DT>::In In;
+  constexpr int NB = 2;
   const auto turns = [&](auto whole) SLIM_INLINE {
     constexpr bool W = decltype(whole)::value;
     const auto there = [&](int row) { return W || (row < rows && l.n); };
     const auto load = [&](u32x4_t* d, In* in, int row) SLIM_INLINE {
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < NB; ++b) {
         d[b] = u32x4_t{0, 0, 0, 0};
         if constexpr (!SUMS)
           if (there(row + step * b))
             d[b] = ActRows<BWD, DT>::load16(reinterpret_cast<const char*>(src) + 2 * ((r0 + row + step * b) * ld + col), W ? 8 : l.n);
       }
-      fin.template load4<W>(in, l, todo, step, rows - row);
+      fin.template load_rows<W, NB>(in, l, todo, step, rows - row);
     };
+    u32x4_t d[NB];
+    In in[NB];
+    load(d, in, at0);
 #pragma unroll 1
-    for (int t = 0; t < rows; t += 4 * step) {      // the same number of turns for every lane
-      u32x4_t d[4];
-      In in[4];
-      load(d, in, t + at0);
-      float f[4][8];
+    for (int t = 0; t < rows; t += NB * step) {      // the same number of turns for every lane
+      float f[NB][8];
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < NB; ++b) {
         if constexpr (SUMS) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[b][e] = 0.f;
@@ -113,11 +114,20 @@ k_act8_rows(const void* __restrict__ src, int64_t ld, int slices, int64_t stride
           act8_to_f(d[b], DT == 1, f[b]);
         }
       }
-      fin.template end4<W>(l, in, todo, step, rows - t - at0, f);
+      u32x4_t dn[NB];
+      In next[NB];
+      if (t + NB * step < rows) load(dn, next, t + at0 + NB * step);
+      __builtin_amdgcn_sched_barrier(0);
+      fin.template end_rows<W, NB>(l, in, todo, step, rows - t - at0, f);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        d[b] = dn[b];
+        in[b] = next[b];
+      }
     }
   };
   // whole turns of whole columns need no bounds
-  if (rows % (4 * step) == 0 && 8 * (strip + 1) * lpr <= N) turns(std::true_type{});
+  if (rows % (NB * step) == 0 && 8 * (strip + 1) * lpr <= N) turns(std::true_type{});
   else turns(std::false_type{});
   if (fin.sums_wanted()) {
     // over the row places of a wave, then over the waves in order

@@ -421,7 +421,7 @@ SLIM_DEV void tile_body(const uint8_t* __restrict__ X, const uint8_t* __restrict
     const auto rows_end = [&](auto whole, int left) __attribute__((always_inline)) {      // `left` rows from this lane's next one on
       constexpr bool W = decltype(whole)::value;
       typename Fin::In in[4];
-      fin.template load4<W>(in, lane8, todo, kStep, left);
+      fin.template load_rows<W>(in, lane8, todo, kStep, left);
 #pragma unroll 1
       for (int t = 0; t < kTurns; t += 4, left -= 4 * kStep) {
         float f[4][8];
@@ -434,9 +434,9 @@ SLIM_DEV void tile_body(const uint8_t* __restrict__ X, const uint8_t* __restrict
             for (int e = 0; e < 4; ++e) f[b][4 * k + e] = v[e];
           }
         typename Fin::In next[4];
-        if (t + 4 < kTurns) fin.template load4<W>(next, lane8, todo, kStep, left - 4 * kStep);
+        if (t + 4 < kTurns) fin.template load_rows<W>(next, lane8, todo, kStep, left - 4 * kStep);
         __builtin_amdgcn_sched_barrier(0);
-        fin.template end4<W>(lane8, in, todo, kStep, left, f);
+        fin.template end_rows<W>(lane8, in, todo, kStep, left, f);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int b = 0; b < 4; ++b) in[b] = next[b];

@@ -98,7 +98,7 @@ struct ActArgs {
   float* part;                                                  // backward: sums of y over each block's rows [blocks][N], or null
 };
 
-// Ends rows eight columns a lane, 16 lanes for 128 columns of a row (all 16 take part in every call), and four rows at a time, `step`
+// Ends rows eight columns a lane, 16 lanes for 128 columns of a row (all 16 take part in every call), and some rows at a time, `step`
 // apart: their reads, an activation's chains of dependent steps and the choices that are the launch's go side by side. DT: the type of
 // 16-bit rows. Everything is fp32 until the one rounding of a result; a column's sum over rows takes du before it.
 // A lane keeps its places in what is read and in what is written, and the ways to the next row, in vector registers: the tiles' scalar
@@ -209,18 +209,18 @@ struct ActRows {
     }
   }
 
-  // The next four rows of this lane, of which those `step` b < more are there (WHOLE: all of them and all columns): what they read.
-  template <bool WHOLE>
-  SLIM_DEV void load4(In* in, Lane& l, int todo, int step, int more) const {
+  // The next NB rows of this lane, of which those `step` b < more are there (WHOLE: all of them and all columns): what they read.
+  template <bool WHOLE, int NB = 4>
+  SLIM_DEV void load_rows(In* in, Lane& l, int todo, int step, int more) const {
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < NB; ++b) {
       in[b].p = in[b].q = u32x4_t{0, 0, 0, 0};
       in[b].pe = in[b].qe = 1;
     }
     const auto there = [&](int b) { return WHOLE || (step * b < more && l.n > 0); };
     if (todo & kP) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b, l.p += l.p_by) {
+      for (int b = 0; b < NB; ++b, l.p += l.p_by) {
         if (BWD && (todo & kQ8)) {
           if (there(b)) {
             in[b].p = load_codes(l.p);
@@ -234,7 +234,7 @@ struct ActRows {
     }
     if (todo & kQ) {
 #pragma unroll
-      for (int b = 0; b < 4; ++b, l.q += l.q_by) {
+      for (int b = 0; b < NB; ++b, l.q += l.q_by) {
         if (BWD && (todo & kQ8)) {
           if (there(b)) {
             in[b].q = load_codes(l.q);
@@ -264,10 +264,10 @@ struct ActRows {
     }
     return big;
   }
-  template <bool WHOLE>
-  static SLIM_DEV void store_codes4(char*& p, uint8_t*& ep, int64_t by, const Lane& l, int step, int more, const float (*f)[8]) {
+  template <bool WHOLE, int NB>
+  static SLIM_DEV void store_codes(char*& p, uint8_t*& ep, int64_t by, const Lane& l, int step, int more, const float (*f)[8]) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b, p += by, ep += l.e_by) {
+    for (int b = 0; b < NB; ++b, p += by, ep += l.e_by) {
       float v[8];
       const int n = WHOLE ? 8 : here(l.n);
 #pragma unroll
@@ -284,20 +284,20 @@ struct ActRows {
     if constexpr (WHOLE) store8<DT>(at, 0, 8, f);
     else if (there && l.n) store8<DT>(at, 0, l.n == 8 ? 8 : here(l.n), f);
   }
-  template <bool WHOLE>
-  static SLIM_DEV void store4(char*& p, int64_t by, const Lane& l, int step, int more, const float (*f)[8]) {
+  template <bool WHOLE, int NB>
+  static SLIM_DEV void store_rows(char*& p, int64_t by, const Lane& l, int step, int more, const float (*f)[8]) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b, p += by) store_row<WHOLE>(p, l, step * b < more, f[b]);
+    for (int b = 0; b < NB; ++b, p += by) store_row<WHOLE>(p, l, step * b < more, f[b]);
   }
 
-  // Ends the next four rows, whose sums are f.
-  template <bool WHOLE>
-  SLIM_DEV void end4(Lane& l, const In* in, int todo, int step, int more, float (*f)[8]) const {
+  // Ends the next NB rows, whose sums are f.
+  template <bool WHOLE, int NB = 4>
+  SLIM_DEV void end_rows(Lane& l, const In* in, int todo, int step, int more, float (*f)[8]) const {
     if constexpr (BWD) {
       with_act(a.act, [&](auto A) SLIM_INLINE {
         const auto rows = [&](auto gated) SLIM_INLINE {
 #pragma unroll
-          for (int b = 0; b < 4; ++b, l.y += l.y_by) {
+          for (int b = 0; b < NB; ++b, l.y += l.y_by) {
             const bool there = WHOLE || step * b < more;
             float u[8], m[8], o[8];
             values(in[b].p, in[b].pe, todo & kQ8, u);
@@ -326,36 +326,36 @@ struct ActRows {
     } else {
       if (todo & kBias)
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[b][e] += l.bias[e];
       if (todo & kW) {
-        if (todo & kQ8) store_codes4<WHOLE>(l.w, l.we, l.w_by, l, step, more, f);
-        else store4<WHOLE>(l.w, l.w_by, l, step, more, f);
+        if (todo & kQ8) store_codes<WHOLE, NB>(l.w, l.we, l.w_by, l, step, more, f);
+        else store_rows<WHOLE, NB>(l.w, l.w_by, l, step, more, f);
       }
       with_act(a.act, [&](auto A) SLIM_INLINE {
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[b][e] = act_value<decltype(A)::value>(f[b][e]);
       });
       float o[8];
       if (todo & kP)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
+        for (int b = 0; b < NB; ++b) {
           act8_to_f(in[b].p, DT == 1, o);
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[b][e] *= o[e];
         }
       if (todo & kQ)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
+        for (int b = 0; b < NB; ++b) {
           act8_to_f(in[b].q, DT == 1, o);
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[b][e] += o[e];
         }
-      if (todo & kQ8) store_codes4<WHOLE>(l.y, l.ye, l.y_by, l, step, more, f);
-      else store4<WHOLE>(l.y, l.y_by, l, step, more, f);
+      if (todo & kQ8) store_codes<WHOLE, NB>(l.y, l.ye, l.y_by, l, step, more, f);
+      else store_rows<WHOLE, NB>(l.y, l.y_by, l, step, more, f);
     }
   }
 
