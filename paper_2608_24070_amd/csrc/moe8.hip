@@ -646,8 +646,10 @@ bool is_16(int t) { return t == SLIM_F16 || t == SLIM_BF16; }
 bool is_float(int t) { return is_16(t) || t == SLIM_F32; }
 size_t elem(int t) { return t == SLIM_F32 ? 4 : 2; }
 
-// Four tiles of y a block where h, which every strip reads, would cost more than its weights do; parts of the reduction as long as they
-// fill the chip, each wave with eight groups at least.
+// Four tiles of y a block from three rows on, where h, which every strip reads, would cost as much as the weights do (down and its sum: 4
+// rows, 2 of 8 experts, 4096 x 11008: 47 us against 61; 16 rows, 4 of 32, 4096 x 2048: 44 against 65; one row, 8 of 64, 4096 x 1024: 14
+// against 12.6). Parts of the reduction until 256 blocks of eight waves or 512 of four are there, each wave with eight groups at
+// least; for many rows, whose parts' sums count, 256 (64 rows, 4 of 32, 2048 x 2048: 42 us, 53 with 512; 2 of 8, 8192 x 2048: 46, 55).
 struct MoePlan {
   int tiles, waves, slots, parts;
   int64_t strips;
@@ -659,7 +661,7 @@ MoePlan moe_plan(int64_t M, int64_t D, int64_t F, int64_t E, int64_t top) {
   p.tiles = M <= 2 ? 1 : 4;
   p.waves = p.tiles == 1 ? 8 : 4;
   p.strips = cdiv(cdiv(D, 16), p.tiles);
-  const int64_t units = p.slots * (q8_row(F) / 128), fill = p.tiles == 1 ? 256 : 512;
+  const int64_t units = p.slots * (q8_row(F) / 128), fill = p.tiles == 4 && M <= 32 ? 512 : 256;
   p.parts = (int)std::max<int64_t>(1, std::min({fill / p.strips, units / (8 * p.waves), int64_t(16)}));
   p.table = M == 1 ? 0 : round256(sizeof(Table));
   p.h = round256((size_t)(M * top * q8_row(F) * 2));
