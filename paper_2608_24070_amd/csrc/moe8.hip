@@ -188,17 +188,19 @@ struct Table {
   float weight[kTokens * kTop];
 };
 
-// One block: a thread a pair of row and expert (two at most), then a thread an expert.
+// One block: a thread a pair of row and expert (two at most), then a thread an expert, which has its rows as 64 bits: how many they are
+// and how many lie before one of them is a count of bits.
+static_assert(kTokens <= 64 && kExperts <= 512 && kTokens * kTop == 2 * 512);
 __global__ void __launch_bounds__(512)
 k_moe_table(const int32_t* __restrict__ ids, const float* __restrict__ weights, int M, int top, int E, Table* __restrict__ t) {
   constexpr int P = kTokens * kTop;
-  typedef int i32x4_t __attribute__((ext_vector_type(4)));
-  __shared__ __attribute__((aligned(16))) int id[P];
+  __shared__ int id[P];
   __shared__ float weight[P];
-  __shared__ int count[kExperts], first[kExperts];
+  __shared__ uint32_t rows[2][kExperts];
+  __shared__ int first[kExperts];
   __shared__ int sums[2][8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pairs = M * top;
-  count[tid] = 0;
+  rows[0][tid] = rows[1][tid] = 0;
 #pragma unroll
   for (int k = 0; k < P / 512; ++k) {
     const int i = tid + 512 * k, e = i < pairs ? ids[i] : -1;
@@ -214,23 +216,18 @@ k_moe_table(const int32_t* __restrict__ ids, const float* __restrict__ weights, 
     const int i = tid + 512 * k;
     mine[k] = id[i];
     total[k] = weight[i];
-    if (i < pairs) {
-      const int j = i % top, end = i - j + top;
+    if (i < pairs && mine[k] >= 0) {
+      const int row = i / top, j = i - row * top, end = i - j + top, e = mine[k];
       for (int o = i - j; o < i; ++o)
-        if (id[o] == mine[k]) mine[k] = -1;
+        if (id[o] == e) mine[k] = -1;
       for (int o = i + 1; o < end; ++o)
-        if (id[o] == mine[k]) total[k] += weight[o];
+        if (id[o] == e) total[k] += weight[o];
+      atomicOr(&rows[row >> 5][e], 1u << (row & 31));
     }
   }
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < P / 512; ++k) {
-    id[tid + 512 * k] = mine[k];
-    if (mine[k] >= 0) atomicAdd(&count[mine[k]], 1);
-  }
-  __syncthreads();
   // places of experts and of their runs: sums over the experts up to this one
-  const int n = count[tid];
+  const int n = __builtin_popcount(rows[0][tid]) + __builtin_popcount(rows[1][tid]);
   int a = n > 0, b = n;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
@@ -259,22 +256,15 @@ k_moe_table(const int32_t* __restrict__ ids, const float* __restrict__ weights, 
   if (tid >= experts) t->slot[tid] = Slot{0, 0, 0, 0};
   if (tid == 0) t->experts = experts;
   __syncthreads();
-  // a pair's place in its run: how many before it name the same expert
-  const i32x4_t* const id4 = reinterpret_cast<const i32x4_t*>(id);
 #pragma unroll
   for (int k = 0; k < P / 512; ++k) {
     const int i = tid + 512 * k;
-    if (512 * k >= pairs) break;
-    int before = 0;
-#pragma unroll 8
-    for (int o = 0; o < (pairs + 3) / 4; ++o) {
-      const i32x4_t v = id4[o];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) before += v[c] == mine[k] && 4 * o + c < i;
-    }
-    if (mine[k] >= 0) {
-      t->row[first[mine[k]] + before] = i / top;
-      t->weight[first[mine[k]] + before] = total[k];
+    if (i < pairs && mine[k] >= 0) {
+      const int row = i / top, e = mine[k];
+      const uint32_t low = row < 32 ? (1u << row) - 1 : ~0u, high = row < 32 ? 0u : (1u << (row - 32)) - 1;
+      const int place = first[e] + __builtin_popcount(rows[0][e] & low) + __builtin_popcount(rows[1][e] & high);
+      t->row[place] = row;
+      t->weight[place] = total[k];
     }
   }
 }
