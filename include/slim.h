@@ -574,7 +574,8 @@ int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int
  *   mul, residual  [M, N] of `dtype` with row strides ldmul, ldres, or NULL: a gate's factor, what Y is added to.
  *   dtype, q8   SLIM_F16 or SLIM_BF16: the type of mul, residual, Y and pre; with q8 nonzero Y and pre leave as 8-bit
  *               rows instead (codes with exponents yexps, preexps; ldy, ldpre are not looked at), rounded from fp32.
- *   Y           out, row stride ldy; may be mul or residual.
+ *   Y           out, row stride ldy; may be mul or residual, but share nothing with X or pre (SLIM_EINVAL where it starts as
+ *               they do).
  *   pre         out, NULL if not wanted: z, for the backward; row stride ldpre.
  *   ws          slim_linear8_act_workspace(xdtype, M, N, K, dtype, q8) bytes; its contents need not be kept or cleared.
  *
@@ -627,7 +628,7 @@ int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, int64_t K, 
  *   ids, weights  [M, top] as slim_route's, E <= 512, top <= 16. A number outside 0 .. E - 1 adds nothing (a row of padding, a dropped
  *               token); one that is twice in a row adds twice.
  *   residual    [M, D] of `dtype`, row stride ldres, or NULL.
- *   Y, dtype    out, SLIM_F16 or SLIM_BF16, row stride ldy; may be the residual.
+ *   Y, dtype    out, SLIM_F16 or SLIM_BF16, row stride ldy; may be the residual, and X.
  *   ws          slim_moe8_workspace(M, D, F, E, top) bytes; its contents need not be kept or cleared.
  * x is not rounded to 8 bits, nor is h, which is held to 16 significant bits; sums are fp32, the experts' of a row in order of number.
  */

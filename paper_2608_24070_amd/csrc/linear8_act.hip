@@ -399,6 +399,7 @@ extern "C" int slim_linear8_act(const void* X, int xdtype, const uint8_t* xexps,
     return SLIM_ESHAPE;
   if (M == 0) return SLIM_OK;
   if (!Y || (q8 && (!yexps || (pre && !preexps)))) return SLIM_EINVAL;
+  if (Y == X || pre == X || Y == pre) return SLIM_EINVAL;      // blocks read X while others write
   const size_t to = q8 ? 16 : 2;
   if (!slim_aligned_to(Y, to) || (pre && !slim_aligned_to(pre, to)) || (mul && !slim_aligned_to(mul, 2)) ||
       (residual && !slim_aligned_to(residual, 2)) || (bias && !slim_aligned_to(bias, elem(bdtype))))

@@ -41,10 +41,11 @@ def needed(query, *args, status):
     (dict(ldx=255), SHAPE), (dict(ldy=19), SHAPE), (dict(ldm=19), SHAPE), (dict(ldr=19), SHAPE), (dict(ldp=19), SHAPE),
     (dict(N=WIDE, ldy=WIDE), SHAPE), (dict(X=ODD), ALIGN), (dict(X=MIS, xdt=Q8), ALIGN), (dict(codes=MIS), ALIGN), (dict(Y=ODD), ALIGN),
     (dict(Y=MIS, q8=1), ALIGN), (dict(pre=MIS, q8=1), ALIGN), (dict(mul=ODD), ALIGN), (dict(res=ODD), ALIGN), (dict(bias=A + 2), ALIGN),
-    (dict(ws=None), WS), (dict(short=1), WS), (dict(ws=MIS), ALIGN), (dict(M=1 << 32), UNSUP), (dict(M=0, X=None, Y=None), OK)])
+    (dict(ws=None), WS), (dict(short=1), WS), (dict(ws=MIS), ALIGN), (dict(M=1 << 32), UNSUP), (dict(M=0, X=None, Y=None), OK),
+    (dict(Y=2 * A), INV), (dict(pre=2 * A), INV), (dict(pre=3 * A), INV)])
 def test_linear8_act(kw, status):
-    a = dict(dict(X=A, xdt=BF16, xexps=A, M=70, N=20, K=256, ldx=256, codes=A, exps=A, act=2, bias=A, bdt=F32, mul=A, ldm=20, res=A, ldr=20,
-                  dt=BF16, q8=0, Y=A, ldy=20, yexps=A, pre=A, ldp=20, preexps=A, ws=A, short=0), **kw)
+    a = dict(dict(X=2 * A, xdt=BF16, xexps=A, M=70, N=20, K=256, ldx=256, codes=A, exps=A, act=2, bias=A, bdt=F32, mul=A, ldm=20, res=A, ldr=20,
+                  dt=BF16, q8=0, Y=3 * A, ldy=20, yexps=A, pre=A, ldp=20, preexps=A, ws=A, short=0), **kw)
     need = needed(slim.slim_linear8_act_workspace, a["xdt"], a["M"], a["N"], a["K"], a["dt"], a["q8"], status=status)
     assert slim.slim_linear8_act(a["X"], a["xdt"], a["xexps"], a["M"], a["N"], a["K"], a["ldx"], a["codes"], a["exps"], a["act"], a["bias"],
                                  a["bdt"], a["mul"], a["ldm"], a["res"], a["ldr"], a["dt"], a["q8"], a["Y"], a["ldy"], a["yexps"], a["pre"],

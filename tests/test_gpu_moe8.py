@@ -197,6 +197,9 @@ def test_strides_places_and_the_bytes_around():
     assert torch.equal(out, want)
     out.copy_(x)
     assert torch.equal(slim.moe8(x, *packs, ids, weights, residual=out, out=out), want)
+    # in the rows' own place
+    out.copy_(x)
+    assert torch.equal(slim.moe8(out, *packs, ids, weights, residual=out, out=out), want)
     out.fill_(-7.0)
     assert bool((buf == -7).all())
 
@@ -238,6 +241,31 @@ def test_streams_graph_replays_and_workspaces(m, e, d, f, top):
         assert bool((ws[need:] == 0xFF).all()) and torch.equal(got, run(None))
         with pytest.raises(slim.SlimError):
             run(ws[:need - 1])
+
+
+def test_two_streams_at_once():
+    g = gen(13)
+    packs, _ = experts(8, 512, 640, g)
+    router = torch.randn((8, 512), generator=g, device="cuda") * 512 ** -0.5
+    w1 = slim.pack8(torch.randn((1024, 512), generator=g, device="cuda") / 22)
+    xs = [rows(m, 512, "bf16", g)[0] for m in (48, 61)]
+
+    def work(x):
+        ids, weights = slim.route(x, router, 3)
+        y = slim.moe8(x, *packs, ids, weights, residual=x)
+        q = slim.linear8_act(y, w1, act="gelu", q8=True)
+        return [ids, weights, y, q["codes"], q["exps"]]
+
+    want = [work(x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = []
+    for _ in range(20):
+        for x, s in zip(xs, streams):
+            with torch.cuda.stream(s):
+                got.append(work(x))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i, r in enumerate(got) for a, b in zip(r, want[i % 2]))
 
 
 def test_no_rows():
