@@ -19,7 +19,7 @@ struct SumRows {
   static constexpr int kType = 0;
   float* sums;
   int64_t ld;
-  SLIM_DEV void four(int64_t m, int64_t n, int64_t, f4_t v) const { *reinterpret_cast<f4_t*>(sums + m * ld + n) = v; }
+  SLIM_DEV void four(int64_t m, int64_t n, int64_t, f4_t v) const { *(SLIM_GLOBAL f4_t*)(sums + m * ld + n) = v; }
 };
 
 // Few rows. 1 x 11008 x 4096, silu and a gate's factor: 8 us (5.6 TB/s), as the bare product.
@@ -31,7 +31,8 @@ k_act8_few(const uint8_t* __restrict__ X, const uint8_t* __restrict__ ex, int64_
 }
 
 // 4096 x 28672 x 8192: 695 us with nothing added (the bare product 695), silu 703, gelu_tanh 707, gelu 742, gelu to 8 bits 762, its
-// argument too 794; backward with a gate, from 8 bits, 820: 0.7 GB in the ends of seven rounds of tiles, each of which moves together.
+// argument too 794; backward with a gate, from 8 bits, 818: bound in its end by the instructions of
+// one wave a SIMD (tiles that start apart, so that their memory traffic does not meet, took as long).
 // What ends the rows is some thirty scalars, which the loop has no registers for: they are read from the launch's arguments anew
 // after it (a copy behind an opaque address, which the compiler cannot move up; held over the loop they were spilled).
 template <class Fin>

@@ -83,6 +83,10 @@ SLIM_DEV uint32_t row16_max_u32(uint32_t v) {
   return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, false));
 }
 
+// Global memory by name: a pointer whose origin the compiler does not see would be a flat one, which takes the LDS's counter too.
+#define SLIM_GLOBAL __attribute__((address_space(1)))
+typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));
+
 // What a row's end reads and writes. Forward: z = sums + bias, y = act(z) mul + res, w = z. Backward: y = du = dh mul act'(u),
 // w = dmul = dh act(u). N columns; rows in 8 bits have q8_row(N) codes and q8_exp_row(N) exponents.
 struct ActArgs {
@@ -132,7 +136,7 @@ struct ActRows {
   }
 
   SLIM_DEV bool sums_wanted() const { return BWD && a.part; }
-  SLIM_DEV void put_sum(int64_t block, int64_t col, int64_t N, float v) const { a.part[block * N + col] = v; }
+  SLIM_DEV void put_sum(int64_t block, int64_t col, int64_t N, float v) const { ((SLIM_GLOBAL float*)a.part)[block * N + col] = v; }
 
   template <class T>
   static SLIM_DEV T in_vector(T v) {
@@ -179,9 +183,9 @@ struct ActRows {
   static SLIM_DEV u32x4_t load16(const char* p, int n) {
     u32x4_t v = {0, 0, 0, 0};
     if (n == 8) {
-      __builtin_memcpy(&v, p, 16);
+      v = *(const SLIM_GLOBAL u32x4_any_t*)p;
     } else {
-      const uint16_t* t = reinterpret_cast<const uint16_t*>(p);
+      const SLIM_GLOBAL uint16_t* t = (const SLIM_GLOBAL uint16_t*)p;
       const int k = here(n);
 #pragma unroll
       for (int e = 0; e < 7; ++e)
@@ -191,7 +195,7 @@ struct ActRows {
   }
   // eight codes: those past the last column are there, and zero
   static SLIM_DEV u32x4_t load_codes(const char* p) {
-    const u32x2_t v = *reinterpret_cast<const u32x2_t*>(p);
+    const u32x2_t v = *(const SLIM_GLOBAL u32x2_t*)p;
     return u32x4_t{v[0], v[1], 0, 0};
   }
   static SLIM_DEV void values(u32x4_t v, uint32_t b, bool q8, float* f) {
@@ -224,7 +228,7 @@ struct ActRows {
         if (BWD && (todo & kQ8)) {
           if (there(b)) {
             in[b].p = load_codes(l.p);
-            in[b].pe = *l.pe;
+            in[b].pe = *(const SLIM_GLOBAL uint8_t*)l.pe;
           }
           l.pe += l.e_by;
         } else if (there(b)) {
@@ -238,7 +242,7 @@ struct ActRows {
         if (BWD && (todo & kQ8)) {
           if (there(b)) {
             in[b].q = load_codes(l.q);
-            in[b].qe = *l.qe;
+            in[b].qe = *(const SLIM_GLOBAL uint8_t*)l.qe;
           }
           l.qe += l.e_by;
         } else if (there(b)) {
@@ -275,14 +279,24 @@ struct ActRows {
       const uint32_t x = q8_exponent(row16_max_u32(largest(v)));
       if (!WHOLE && (step * b >= more || l.place < 0)) continue;
       const float s = q8_inverse(x);
-      *reinterpret_cast<u32x2_t*>(p) = u32x2_t{q8_codes4(v[0], v[1], v[2], v[3], s), q8_codes4(v[4], v[5], v[6], v[7], s)};
-      if (l.place == 0 || l.tail) *ep = l.tail ? 0 : (uint8_t)x;      // the row's last word ends in zeros
+      *(SLIM_GLOBAL u32x2_t*)p = u32x2_t{q8_codes4(v[0], v[1], v[2], v[3], s), q8_codes4(v[4], v[5], v[6], v[7], s)};
+      if (l.place == 0 || l.tail) *(SLIM_GLOBAL uint8_t*)ep = l.tail ? 0 : (uint8_t)x;      // the row's last word ends in zeros
     }
   }
   template <bool WHOLE>
   static SLIM_DEV void store_row(char* at, const Lane& l, bool there, const float* f) {
-    if constexpr (WHOLE) store8<DT>(at, 0, 8, f);
-    else if (there && l.n) store8<DT>(at, 0, l.n == 8 ? 8 : here(l.n), f);
+    if (!WHOLE && !(there && l.n)) return;
+    u32x4_t v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = to_16<DT>(f[2 * e]) | (to_16<DT>(f[2 * e + 1]) << 16);
+    if (WHOLE || l.n == 8) {
+      *(SLIM_GLOBAL u32x4_any_t*)at = v;
+    } else {
+      const int n = here(l.n);
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < n) ((SLIM_GLOBAL uint16_t*)at)[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+    }
   }
   template <bool WHOLE, int NB>
   static SLIM_DEV void store_rows(char*& p, int64_t by, const Lane& l, int step, int more, const float (*f)[8]) {
