@@ -574,9 +574,10 @@ int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int
  *   mul, residual  [M, N] of `dtype` with row strides ldmul, ldres, or NULL: a gate's factor, what Y is added to.
  *   dtype, q8   SLIM_F16 or SLIM_BF16: the type of mul, residual, Y and pre; with q8 nonzero Y and pre leave as 8-bit
  *               rows instead (codes with exponents yexps, preexps; ldy, ldpre are not looked at), rounded from fp32.
- *   Y           out, row stride ldy; may be mul or residual, but share nothing with X or pre (SLIM_EINVAL where it starts as
- *               they do).
+ *   Y           out, row stride ldy.
  *   pre         out, NULL if not wanted: z, for the backward; row stride ldpre.
+ *               In 16 bits Y and pre may each be mul or residual, in the very place: the same address and row stride. But
+ *               for that they and their exponents share no memory with each other, X, bias, mul or residual (SLIM_EINVAL).
  *   ws          slim_linear8_act_workspace(xdtype, M, N, K, dtype, q8) bytes; its contents need not be kept or cleared.
  *
  * slim_bwd_dx8_act - the gradient through the activation in front of a product: dh = dY W, the input gradient of the

@@ -33,6 +33,44 @@ extern "C" const char* slim_status_string(int status) {
 
 extern "C" int slim_abi_version(void) { return SLIM_ABI_VERSION; }
 
+namespace {
+// Row i of an operand as a range of addresses, which counts and steps of 64 bits may pass.
+typedef unsigned __int128 place_t;
+place_t start_of(const SlimRows& r, int64_t i) { return (uintptr_t)r.at + (place_t)i * (place_t)r.step; }
+place_t end_of(const SlimRows& r, int64_t i) { return start_of(r, i) + (place_t)r.bytes; }
+// Whether row i of a meets a row of b: the first that ends behind its start does, or none.
+bool row_meets(const SlimRows& a, int64_t i, const SlimRows& b) {
+  const place_t from = start_of(a, i), first = end_of(b, 0);
+  const place_t k = from < first ? 0 : b.step > 0 ? (from - first) / (place_t)b.step + 1 : (place_t)b.rows;
+  return k < (place_t)b.rows && start_of(b, (int64_t)k) < end_of(a, i);
+}
+}  // namespace
+
+bool slim_rows_meet(const SlimRows& a, const SlimRows& b) {
+  if (!a.at || !b.at || a.rows < 1 || b.rows < 1) return false;
+  if (end_of(a, a.rows - 1) <= start_of(b, 0) || end_of(b, b.rows - 1) <= start_of(a, 0)) return false;
+  // at one step rows that meet do so down to the first of either: what lies side by side in one buffer costs two looks
+  if (a.step == b.step) return row_meets(a, 0, b) || row_meets(b, 0, a);
+  const SlimRows &few = a.rows < b.rows ? a : b, &many = a.rows < b.rows ? b : a;
+  for (int64_t i = 0; i < few.rows; ++i)
+    if (row_meets(few, i, many)) return true;
+  return false;
+}
+
+bool slim_may_write(std::initializer_list<SlimRows> outs, std::initializer_list<SlimRows> in_place, std::initializer_list<SlimRows> apart) {
+  for (auto o = outs.begin(); o != outs.end(); ++o) {
+    for (auto p = outs.begin(); p != o; ++p)
+      if (slim_rows_meet(*o, *p)) return false;
+    for (const SlimRows& r : apart)
+      if (slim_rows_meet(*o, r)) return false;
+    for (const SlimRows& r : in_place) {
+      const bool same = o->at == r.at && o->rows == r.rows && o->bytes == r.bytes && (o->rows == 1 || o->step == r.step);
+      if (!same && slim_rows_meet(*o, r)) return false;
+    }
+  }
+  return true;
+}
+
 int slim_check_pack(const float* W, int64_t N, int64_t K, const void* codes, const void* meta,
                     const void* scales, const void* mask) {
   if (!W || !codes || !meta || !scales) return SLIM_EINVAL;

@@ -293,6 +293,12 @@ bool is_16(int t) { return t == SLIM_F16 || t == SLIM_BF16; }
 bool is_float(int t) { return is_16(t) || t == SLIM_F32; }
 size_t elem(int t) { return t == SLIM_F32 ? 4 : 2; }
 
+// Operands and results in memory.
+SlimRows rows_of(const void* p, int64_t M, int64_t N, int64_t ld, size_t bytes) { return {p, M, N * (int64_t)bytes, ld * (int64_t)bytes}; }
+SlimRows codes_of(const void* p, int64_t M, int64_t N) { return {p, M, q8_row(N), q8_row(N)}; }
+SlimRows exps_of(const void* p, int64_t M, int64_t N) { return {p, M, q8_exp_row(N), q8_exp_row(N)}; }
+SlimRows vector_of(const void* p, int64_t N, size_t bytes) { return {p, 1, N * (int64_t)bytes, 0}; }
+
 // Whether X's rows are turned into codes in the product's own launch (few rows of the results' type).
 bool in_launch(bool bwd, int xdtype, int dtype, int64_t M, int64_t K, bool groups) {
   return !bwd && !groups && xdtype == dtype && M <= 4 && M * q8_row(K) <= kFewLds;
@@ -313,16 +319,22 @@ int product_workspace(bool bwd, int xdtype, int64_t M, int64_t N, int64_t K, int
   return SLIM_OK;
 }
 
-// The product of both entry points, checked, as `need` bytes of workspace say.
-template <bool BWD>
-int product(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t N, int64_t K, int64_t ldx, const uint8_t* codes,
-            const uint8_t* exps, ActArgs args, int dtype, bool groups, void* dbias, size_t need, void* ws, size_t ws_bytes, void* stream) {
+// What both entry points ask of the product's operands and of `need` bytes of workspace.
+int check_product(const void* X, int xdtype, const uint8_t* xexps, const uint8_t* codes, const uint8_t* exps, size_t need, const void* ws,
+                  size_t ws_bytes) {
   const bool packed = xdtype == SLIM_Q8_E4M3;
   if (!X || (packed && !xexps) || !codes || !exps) return SLIM_EINVAL;
   if (!slim_aligned_to(X, packed ? 16 : elem(xdtype)) || !slim_aligned16(xexps) || !slim_aligned16(codes) || !slim_aligned16(exps))
     return SLIM_EALIGN;
   if (need && (!ws || ws_bytes < need)) return SLIM_EWORKSPACE;
   if (need && !slim_aligned16(ws)) return SLIM_EALIGN;
+  return SLIM_OK;
+}
+
+// The product of both entry points, of checked operands.
+template <bool BWD>
+int product(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t N, int64_t K, int64_t ldx, const uint8_t* codes,
+            const uint8_t* exps, ActArgs args, int dtype, bool groups, void* dbias, void* ws, void* stream) {
   hipStream_t s = (hipStream_t)stream;
   Product d{reinterpret_cast<const uint8_t*>(X), xexps, codes, exps, ldx, M, N, K};
   if (in_launch(BWD, xdtype, dtype, M, K, groups)) {
@@ -334,7 +346,7 @@ int product(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t 
   }
   const ActPlan a = act_plan(BWD, xdtype, M, N, K, groups, dbias != nullptr);
   char* at = reinterpret_cast<char*>(ws);
-  if (!packed) {
+  if (xdtype != SLIM_Q8_E4M3) {
     uint8_t* c = reinterpret_cast<uint8_t*>(at);
     uint8_t* e = c + code_bytes(M, K);
     const int q = slim_quant8(X, xdtype, M, K, ldx, c, e, stream);
@@ -400,11 +412,20 @@ extern "C" int slim_linear8_act(const void* X, int xdtype, const uint8_t* xexps,
     return SLIM_ESHAPE;
   if (M == 0) return SLIM_OK;
   if (!Y || (q8 && (!yexps || (pre && !preexps)))) return SLIM_EINVAL;
-  if (Y == X || pre == X || Y == pre) return SLIM_EINVAL;      // blocks read X while others write
   const size_t to = q8 ? 16 : 2;
   if (!slim_aligned_to(Y, to) || (pre && !slim_aligned_to(pre, to)) || (mul && !slim_aligned_to(mul, 2)) ||
       (residual && !slim_aligned_to(residual, 2)) || (bias && !slim_aligned_to(bias, elem(bdtype))))
     return SLIM_EALIGN;
+  const int bad = check_product(X, xdtype, xexps, codes, exps, need, ws, ws_bytes);
+  if (bad != SLIM_OK) return bad;
+  // Blocks read X while others write. mul and residual are read element for element by the lane that writes Y and pre there, before
+  // it does, so 16-bit results may take their very rows; 8-bit ones would lie over rows of other lanes.
+  const bool packed = xdtype == SLIM_Q8_E4M3;
+  const SlimRows x = packed ? codes_of(X, M, K) : rows_of(X, M, K, ldx, elem(xdtype)), xe = exps_of(packed ? xexps : nullptr, M, K);
+  const SlimRows b = vector_of(bias, N, elem(bdtype)), m = rows_of(mul, M, N, ldmul, 2), r = rows_of(residual, M, N, ldres, 2);
+  if (q8 ? !slim_may_write({codes_of(Y, M, N), exps_of(yexps, M, N), codes_of(pre, M, N), exps_of(pre ? preexps : nullptr, M, N)}, {}, {x, xe, b, m, r})
+         : !slim_may_write({rows_of(Y, M, N, ldy, 2), rows_of(pre, M, N, ldpre, 2)}, {m, r}, {x, xe, b}))
+    return SLIM_EINVAL;
   ActArgs a{};
   a.act = act;
   a.bdt = bdtype;
@@ -415,7 +436,7 @@ extern "C" int slim_linear8_act(const void* X, int xdtype, const uint8_t* xexps,
   a.res = reinterpret_cast<const uint16_t*>(residual); a.ldres = ldres;
   a.y = Y; a.ye = yexps; a.ldy = ldy;
   a.w = pre; a.we = preexps; a.ldw = ldpre;
-  return product<false>(X, xdtype, xexps, M, N, K, ldx, codes, exps, a, dtype, q8 != 0, nullptr, need, ws, ws_bytes, stream);
+  return product<false>(X, xdtype, xexps, M, N, K, ldx, codes, exps, a, dtype, q8 != 0, nullptr, ws, stream);
 }
 
 extern "C" int slim_bwd_dx8_act_workspace(int dydtype, int64_t M, int64_t N, int64_t K, int dtype, int sums, size_t* bytes) {
@@ -437,9 +458,10 @@ extern "C" int slim_bwd_dx8_act(const void* dY, int dydtype, const uint8_t* dyex
     if (dbias) launch_sums(nullptr, 0, K, dbias, dtype, (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
   }
+  rc = check_product(dY, dydtype, dyexps, codesT, expsT, need, ws, ws_bytes);
+  if (rc != SLIM_OK) return rc;
   return product<true>(dY, dydtype, dyexps, M, K, N, lddy, codesT, expsT,
-                       bwd_args(K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul), dtype, true, dbias, need, ws,
-                       ws_bytes, stream);
+                       bwd_args(K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul), dtype, true, dbias, ws, stream);
 }
 
 extern "C" int slim_act_bwd_workspace(int64_t M, int64_t K, int sums, size_t* bytes) {

@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "slim.h"
 
 // Completion counters live in a fixed-size region at the start of the workspace.
@@ -74,3 +76,14 @@ int slim_check_linear(bool bwd, const void* X, int xdtype, int64_t M, int64_t N,
 
 inline bool slim_aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline bool slim_aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// An operand's or a result's rows in memory: `rows` of them, `bytes` long, `step` bytes apart. Rows of null are none.
+struct SlimRows {
+  const void* at;
+  int64_t rows, bytes, step;
+};
+// Whether a byte is in both.
+bool slim_rows_meet(const SlimRows& a, const SlimRows& b);
+// Whether a launch may write each of `outs` while it reads the others: results apart from each other and from `apart`, and apart from
+// `in_place` or the very rows of one, each element of which the lane that writes it reads before.
+bool slim_may_write(std::initializer_list<SlimRows> outs, std::initializer_list<SlimRows> in_place, std::initializer_list<SlimRows> apart);

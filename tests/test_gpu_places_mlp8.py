@@ -1,0 +1,64 @@
+"""Results of the MLP operators in the places that they may take: an operand's very rows, and beside operands in one buffer. The same
+bits as in a place of their own."""
+import pytest
+import torch
+
+from paper_2608_24070_amd import slim
+
+pytestmark = pytest.mark.gpu
+
+BF16 = slim.SLIM_BF16
+# few rows (quantised in the launch, from codes), tiles, 64-column tiles and slices by sums in memory
+SIZES = [(3, 200, 300), (40, 333, 600), (300, 333, 600), (1500, 2050, 300), (64, 515, 28672)]
+
+
+def rand(*s):
+    return torch.randn(s, device="cuda").bfloat16()
+
+
+def workspace(n):
+    return torch.full((n + 16,), 0xFF, dtype=torch.uint8, device="cuda")
+
+
+def checked(status):
+    assert status == slim.SLIM_OK, slim.SlimError(status, "call")
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+def test_forward(m, n, k, act):
+    print(f"linear8_act in place m={m} n={n} k={k} {act}", flush=True)
+    x, w = rand(m, k), torch.randn((n, k), device="cuda") * k ** -0.5
+    p, mul, res = slim.pack8(w), rand(m, n), rand(m, n)
+    y, z = slim.linear8_act(x, p, act=act, mul=mul, residual=res, pre=True)
+    ws = workspace(slim.slim_linear8_act_workspace(BF16, m, n, k, BF16, 0))
+
+    def call(mt, rt, yt, zt):
+        checked(slim.slim_linear8_act(x.data_ptr(), BF16, None, m, n, k, k, p["codes"].data_ptr(), p["exps"].data_ptr(), slim.ACTS[act], None,
+                                      slim.SLIM_F32, mt.data_ptr(), mt.stride(0), rt.data_ptr(), rt.stride(0), BF16, 0, yt.data_ptr(), yt.stride(0),
+                                      None, zt.data_ptr(), zt.stride(0), None, ws.data_ptr(), ws.numel(), slim._stream_on(0)))
+        assert torch.equal(yt, y) and torch.equal(zt, z)
+
+    for cross in (False, True):            # Y and pre each in the place of one of the two
+        a, b = mul.clone(), res.clone()
+        call(a, b, *((b, a) if cross else (a, b)))
+    # one buffer: factor, residual, result and argument side by side, and the result in the factor's columns
+    wide = torch.full((m, 4 * n + 5), -7.0, dtype=torch.bfloat16, device="cuda")
+    part = [wide[:, i * n + i:(i + 1) * n + i] for i in range(4)]
+    part[0].copy_(mul)
+    part[1].copy_(res)
+    call(*part)
+    assert torch.equal(part[0], mul) and torch.equal(part[1], res) and bool((wide[:, n::n + 1][:, :4] == -7).all())
+    call(part[0], part[1], part[0], part[3])
+    # a buffer's rows in turn
+    if m > 1:
+        tall = torch.zeros((2 * m, n), dtype=torch.bfloat16, device="cuda")
+        mt, yt = tall[0::2], tall[1::2]
+        mt.copy_(mul)
+        call(mt, res, yt, torch.empty_like(z))
+    # one row has no stride
+    if m > 2:
+        one = slim.linear8_act(x[:1], p, act=act, mul=mul[:1], residual=res[:1])
+        row = mul[:1].clone()
+        wide_row = torch.as_strided(row, (1, n), (n + 9, 1))
+        assert torch.equal(slim.linear8_act(x[:1], p, act=act, mul=row, residual=res[:1], out=wide_row), one)
