@@ -588,12 +588,13 @@ int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int
  *               SLIM_ACT_NONE where mul is.
  *   mul         [M, K] like U (ldmul or mulexps), the gate's factor, or NULL; then dmul is NULL too.
  *   dtype       SLIM_F16 or SLIM_BF16, of dU, dmul (row strides lddu, lddmul) and dbias.
- *   dU, dmul    out; may be U and mul.
+ *   dU, dmul    out. Each may be U or mul in 16 bits, in the very place: the same address and row stride. But for that dU, dmul and
+ *               dbias share no memory with each other, U, mul or an 8-bit dY (SLIM_EINVAL).
  *   dbias       out, [K] of `dtype`, or NULL. It is as near as the product's sums (2e-5 to 4.5e-5 of its norm), then
  *               rounded; fp32 is not offered for it, as for Y above.
  *   ws          slim_bwd_dx8_act_workspace(dydtype, M, N, K, dtype, dbias != NULL) bytes, as above.
  *
- * slim_act_bwd - the same from a dh at hand: dH [M, K] of `dtype`, row stride lddh. dU may be dH. dbias fp32.
+ * slim_act_bwd - the same from a dh at hand: dH [M, K] of `dtype`, row stride lddh. dU or dmul may be dH, as above. dbias fp32.
  *   ws          slim_act_bwd_workspace(M, K, dbias != NULL) bytes, as above.
  */
 int slim_linear8_act_workspace(int xdtype, int64_t M, int64_t N, int64_t K, int dtype, int q8, size_t* bytes);

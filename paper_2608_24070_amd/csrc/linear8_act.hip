@@ -380,6 +380,16 @@ int check_bwd(int64_t N, int act, const void* U, int udtype, const uint8_t* uexp
   return SLIM_OK;
 }
 
+// Whether the backward's results may be written while U, mul and `src` (dH) are read: the lane that writes an element has read it in
+// 16-bit operands before. 8-bit ones (and a product's operand `x` with exponents `xe`) have their elements elsewhere.
+bool bwd_may_write(int64_t M, int64_t N, const ActArgs& a, const void* dbias, size_t bias_bytes, SlimRows src, SlimRows x, SlimRows xe) {
+  const SlimRows du = rows_of(a.y, M, N, a.ldy, 2), dm = rows_of(a.w, M, N, a.ldw, 2), db = vector_of(dbias, N, bias_bytes);
+  if (a.q8)
+    return slim_may_write({du, dm, db}, {src}, {x, xe, codes_of(a.u, M, N), exps_of(a.u ? a.ue : nullptr, M, N), codes_of(a.mul, M, N),
+                                                exps_of(a.mul ? a.me : nullptr, M, N)});
+  return slim_may_write({du, dm, db}, {src, rows_of(a.u, M, N, a.ldu, 2), rows_of(a.mul, M, N, a.ldmul, 2)}, {x, xe});
+}
+
 ActArgs bwd_args(int64_t N, int act, const void* U, int udtype, const uint8_t* uexps, int64_t ldu, const void* mul, const uint8_t* mulexps,
                  int64_t ldmul, void* dU, int64_t lddu, void* dmul, int64_t lddmul) {
   ActArgs a{};
@@ -460,8 +470,12 @@ extern "C" int slim_bwd_dx8_act(const void* dY, int dydtype, const uint8_t* dyex
   }
   rc = check_product(dY, dydtype, dyexps, codesT, expsT, need, ws, ws_bytes);
   if (rc != SLIM_OK) return rc;
-  return product<true>(dY, dydtype, dyexps, M, K, N, lddy, codesT, expsT,
-                       bwd_args(K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul), dtype, true, dbias, ws, stream);
+  const ActArgs a = bwd_args(K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul);
+  // a dY of another type is read, turned into 8 bits in the workspace, before anything is written
+  const bool packed = dydtype == SLIM_Q8_E4M3;
+  if (!bwd_may_write(M, K, a, dbias, 2, SlimRows{}, codes_of(packed ? dY : nullptr, M, N), exps_of(packed ? dyexps : nullptr, M, N)))
+    return SLIM_EINVAL;
+  return product<true>(dY, dydtype, dyexps, M, K, N, lddy, codesT, expsT, a, dtype, true, dbias, ws, stream);
 }
 
 extern "C" int slim_act_bwd_workspace(int64_t M, int64_t K, int sums, size_t* bytes) {
@@ -496,6 +510,7 @@ extern "C" int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, 
   if (need && (!ws || ws_bytes < need)) return SLIM_EWORKSPACE;
   if (need && !slim_aligned16(ws)) return SLIM_EALIGN;
   ActArgs a = bwd_args(K, act, U, udtype, uexps, ldu, mul, mulexps, ldmul, dU, lddu, dmul, lddmul);
+  if (!bwd_may_write(M, K, a, dbias, 4, rows_of(dH, M, K, lddh, 2), SlimRows{}, SlimRows{})) return SLIM_EINVAL;
   const int64_t blocks = row_plan(M, K).blocks;
   a.part = !dbias ? nullptr : blocks > 1 ? reinterpret_cast<float*>(ws) : dbias;
   if (dtype == SLIM_F16) launch_rows<true, 0, false>(dH, lddh, 1, 0, M, a, s);

@@ -62,3 +62,53 @@ def test_forward(m, n, k, act):
         row = mul[:1].clone()
         wide_row = torch.as_strided(row, (1, n), (n + 9, 1))
         assert torch.equal(slim.linear8_act(x[:1], p, act=act, mul=row, residual=res[:1], out=wide_row), one)
+
+
+@pytest.mark.parametrize("m,n,k", SIZES + [(1, 130, 4100), (100, 129, 4097)])
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+def test_backward(m, n, k, act):
+    # n: the reduction, k: the columns of dh
+    n, k = k, n
+    print(f"gradients in place m={m} n={n} k={k} {act}", flush=True)
+    dy, w = rand(m, n), torch.randn((n, k), device="cuda") * n ** -0.5
+    p, u, mul, dh = slim.pack8(w, bwd=True), rand(m, k), rand(m, k), rand(m, k)
+    a = slim.ACTS[act]
+    ws = workspace(max(slim.slim_bwd_dx8_act_workspace(BF16, m, n, k, BF16, 1), slim.slim_act_bwd_workspace(m, k, 1)))
+
+    def product(src, ut, mt, dut, dmt):
+        db = torch.empty(k, dtype=torch.bfloat16, device="cuda")
+        checked(slim.slim_bwd_dx8_act(src.data_ptr(), BF16, None, m, n, k, src.stride(0), p["codesT"].data_ptr(), p["expsT"].data_ptr(), a,
+                                      ut.data_ptr(), BF16, None, ut.stride(0), mt.data_ptr(), None, mt.stride(0), BF16, dut.data_ptr(), dut.stride(0),
+                                      dmt.data_ptr(), dmt.stride(0), db.data_ptr(), ws.data_ptr(), ws.numel(), slim._stream_on(0)))
+        return dut, dmt, db
+
+    def alone(src, ut, mt, dut, dmt):
+        db = torch.empty(k, device="cuda")
+        checked(slim.slim_act_bwd(src.data_ptr(), BF16, src.stride(0), m, k, a, ut.data_ptr(), BF16, None, ut.stride(0), mt.data_ptr(), None,
+                                  mt.stride(0), dut.data_ptr(), dut.stride(0), dmt.data_ptr(), dmt.stride(0), db.data_ptr(), ws.data_ptr(), ws.numel(),
+                                  slim._stream_on(0)))
+        return dut, dmt, db
+
+    for call, src in ((product, dy), (alone, dh)):
+        want = [t.clone() for t in call(src, u, mul, torch.empty_like(u), torch.empty_like(u))]
+        same = lambda got: all(torch.equal(s, t) for s, t in zip(got, want))
+        for cross in (False, True):
+            ut, mt = u.clone(), mul.clone()
+            assert same(call(src, ut, mt, *((mt, ut) if cross else (ut, mt))))
+        # side by side in one buffer, and the gradient in u's columns
+        wide = torch.full((m, 4 * k + 5), -7.0, dtype=torch.bfloat16, device="cuda")
+        part = [wide[:, i * k + i:(i + 1) * k + i] for i in range(4)]
+        part[0].copy_(u)
+        part[1].copy_(mul)
+        assert same(call(src, *part)) and torch.equal(part[0], u) and torch.equal(part[1], mul)
+        assert same(call(src, part[0], part[1], part[0], part[3]))
+        if call is alone:
+            for cross in (False, True):
+                s, other = dh.clone(), torch.empty_like(dh)
+                assert same(call(s, u, mul, *((other, s) if cross else (s, other))))
+    # a 16-bit dY's own rows: it is read before anything is written
+    if m * n >= m * k and m > 1:
+        want = [t.clone() for t in product(dy, u, mul, torch.empty_like(u), torch.empty_like(u))]
+        s = dy.clone()
+        got = product(s, u, mul, s.view(-1)[:m * k].view(m, k), torch.empty_like(u))
+        assert all(torch.equal(x, y) for x, y in zip(got, want))

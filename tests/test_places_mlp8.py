@@ -55,3 +55,36 @@ def forward(kw):
     dict(pre=at(5)), dict(pre=at(5) + 2), dict(pre=at(5) + 2 * N, ldp=3 * N), dict(q8=1, pre=at(5)), dict(q8=1, pe=at(6)), dict(q8=1, ye=at(5) + 256)])
 def test_forward(kw):
     assert forward(kw) == INV
+
+
+# places, of [M, K]: U, mul in 16 bits (K columns, ld) or in 8 bits; exponents are Q8's only
+BWD = [
+    # 16-bit results over 8-bit operands or their exponents
+    dict(udt=Q8, dU=at(2)), dict(udt=Q8, dmul=at(4)), dict(udt=Q8, dU=at(4)), dict(udt=Q8, dmul=at(2) + 16 * K), dict(udt=Q8, dU=at(3)),
+    dict(udt=Q8, dmul=at(5)), dict(udt=Q8, db=at(2)),
+    # an operand's own place at another stride, a row or a column further, or so that only the last rows meet
+    dict(dU=at(2), ldo=K + 8), dict(dmul=at(4), ldm=2 * K), dict(dU=at(2) + 2 * K), dict(dU=at(4) + 2), dict(dmul=at(2) + 2 * K * (M - 1)),
+    dict(dU=at(4) - 2 * K * (M - 1)), dict(db=at(2) + 2 * K), dict(db=at(4)),
+    # each other
+    dict(dmul=at(6)), dict(dmul=at(6) + 2), dict(dmul=at(6) + 2 * K, ldd=3 * K), dict(db=at(6)), dict(db=at(7) + 2 * K * (M - 1)),
+    dict(dU=at(2), dmul=at(2)), dict(M=1, db=at(6)), dict(M=1, dmul=at(6) + K)]
+
+
+@pytest.mark.parametrize("kw", BWD + [
+    # dY where blocks read it as it is
+    dict(xdt=Q8, dU=at(0)), dict(xdt=Q8, dmul=at(0)), dict(xdt=Q8, dU=at(0) + 128), dict(xdt=Q8, dU=at(1)), dict(xdt=Q8, db=at(0))])
+def test_bwd_dx8_act(kw):
+    a = dict(dict(X=at(0), xdt=BF16, xe=at(1), U=at(2), ue=at(3), ldu=K, mul=at(4), me=at(5), ldm=K, udt=BF16, dU=at(6), ldo=K, dmul=at(7), ldd=K,
+                  db=at(8), M=M), **kw)
+    need = slim.slim_bwd_dx8_act_workspace(a["xdt"], a["M"], N, K, BF16, 1)
+    assert slim.slim_bwd_dx8_act(a["X"], a["xdt"], a["xe"], a["M"], N, K, N, at(9), at(10), slim.SLIM_ACT_GELU, a["U"], a["udt"], a["ue"], a["ldu"],
+                                 a["mul"], a["me"], a["ldm"], BF16, a["dU"], a["ldo"], a["dmul"], a["ldd"], a["db"], at(11), need, None) == INV
+
+
+@pytest.mark.parametrize("kw", BWD + [dict(dU=at(0), ldx=K + 1), dict(dmul=at(0) + 2 * K), dict(dU=at(0), dmul=at(0)), dict(db=at(0))])
+def test_act_bwd(kw):
+    a = dict(dict(X=at(0), ldx=K, U=at(2), ue=at(3), ldu=K, mul=at(4), me=at(5), ldm=K, udt=BF16, dU=at(6), ldo=K, dmul=at(7), ldd=K, db=at(8), M=M),
+             **kw)
+    need = slim.slim_act_bwd_workspace(a["M"], K, 1)
+    assert slim.slim_act_bwd(a["X"], BF16, a["ldx"], a["M"], K, slim.SLIM_ACT_GELU, a["U"], a["udt"], a["ue"], a["ldu"], a["mul"], a["me"], a["ldm"],
+                             a["dU"], a["ldo"], a["dmul"], a["ldd"], a["db"], at(11), need, None) == INV
