@@ -630,7 +630,8 @@ int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, int64_t K, 
  *   ids, weights  [M, top] as slim_route's, E <= 512, top <= 16. A number outside 0 .. E - 1 adds nothing (a row of padding, a dropped
  *               token); one that is twice in a row adds twice.
  *   residual    [M, D] of `dtype`, row stride ldres, or NULL.
- *   Y, dtype    out, SLIM_F16 or SLIM_BF16, row stride ldy; may be the residual, and X.
+ *   Y, dtype    out, SLIM_F16 or SLIM_BF16, row stride ldy; may be X, and the residual in the very place (the same address and row
+ *               stride), but share no other memory with the residual, ids or weights (SLIM_EINVAL).
  *   ws          slim_moe8_workspace(M, D, F, E, top) bytes; its contents need not be kept or cleared.
  * x is not rounded to 8 bits, nor is h, which is held to 16 significant bits; sums are fp32, the experts' of a row in order of number.
  */

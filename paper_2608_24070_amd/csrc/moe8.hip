@@ -755,6 +755,10 @@ extern "C" int slim_moe8(const void* X, int xdtype, const uint8_t* xexps, int64_
     return SLIM_EALIGN;
   if (!ws || ws_bytes < need) return SLIM_EWORKSPACE;
   if (!slim_aligned16(ws)) return SLIM_EALIGN;
+  // X is read before the launch that writes Y; the residual in that launch, element for element by the lane that writes there, and with
+  // one row ids and weights, by every block
+  const SlimRows picked{ids, 1, M * top * 4, 0}, weighed{weights, 1, M * top * 4, 0};
+  if (!slim_may_write({{Y, M, 2 * D, 2 * ldy}}, {{residual, M, 2 * D, 2 * ldres}}, {picked, weighed})) return SLIM_EINVAL;
   hipStream_t s = (hipStream_t)stream;
   const MoePlan p = moe_plan(M, D, F, E, top);
   char* at = reinterpret_cast<char*>(ws);

@@ -112,3 +112,26 @@ def test_backward(m, n, k, act):
         s = dy.clone()
         got = product(s, u, mul, s.view(-1)[:m * k].view(m, k), torch.empty_like(u))
         assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+# one row, few rows, and rows whose reduction is in parts (their sums are added by a launch of its own)
+@pytest.mark.parametrize("m,e,d,f,top", [(1, 8, 300, 200, 3), (9, 4, 300, 200, 2), (40, 6, 130, 2100, 4)])
+def test_experts(m, e, d, f, top):
+    gate, up, down = (slim.pack8_experts(torch.randn((e, *s), device="cuda") * s[1] ** -0.5) for s in ((f, d), (f, d), (d, f)))
+    x, res = rand(m, d), rand(m, d)
+    ids, weights = slim.route(x, rand(e, d), top)
+    want = slim.moe8(x, gate, up, down, ids, weights, residual=res)
+    wide = torch.full((m, 3 * d + 4), -7.0, dtype=torch.bfloat16, device="cuda")
+    part = [wide[:, i * d + i:(i + 1) * d + i] for i in range(3)]
+    part[0].copy_(x)
+    part[1].copy_(res)
+    assert torch.equal(slim.moe8(part[0], gate, up, down, ids, weights, residual=part[1], out=part[2]), want)
+    assert torch.equal(part[0], x) and torch.equal(part[1], res)
+    assert torch.equal(slim.moe8(part[0], gate, up, down, ids, weights, residual=part[1], out=part[1]), want)
+    part[1].copy_(res)
+    assert torch.equal(slim.moe8(part[0], gate, up, down, ids, weights, residual=part[1], out=part[0]), want)
+    # X's memory at another stride
+    flat = torch.empty(m * (d + 8), dtype=torch.bfloat16, device="cuda")
+    xs, out = flat[:m * d].view(m, d), flat.view(m, d + 8)[:, :d]
+    xs.copy_(x)
+    assert torch.equal(slim.moe8(xs, gate, up, down, ids, weights, residual=res, out=out), want)

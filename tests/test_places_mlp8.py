@@ -88,3 +88,14 @@ def test_act_bwd(kw):
     need = slim.slim_act_bwd_workspace(a["M"], K, 1)
     assert slim.slim_act_bwd(a["X"], BF16, a["ldx"], a["M"], K, slim.SLIM_ACT_GELU, a["U"], a["udt"], a["ue"], a["ldu"], a["mul"], a["me"], a["ldm"],
                              a["dU"], a["ldo"], a["dmul"], a["ldd"], a["db"], at(11), need, None) == INV
+
+
+@pytest.mark.parametrize("kw", [
+    # the residual's rows at another stride, or a part of them; what other blocks look up
+    dict(Y=at(2), ldy=K + 8), dict(Y=at(2), ldr=2 * K), dict(Y=at(2) + 2 * K), dict(Y=at(2) + 2), dict(Y=at(2) - 2 * K * 6), dict(Y=at(3)),
+    dict(Y=at(4)), dict(Y=at(3) - 2 * K * 6), dict(M=1, Y=at(3)), dict(M=1, Y=at(2) + K)])
+def test_moe8(kw):
+    a = dict(dict(M=7, X=at(0), res=at(2), ldr=K, Y=at(5), ldy=K), **kw)
+    need = slim.slim_moe8_workspace(a["M"], K, 300, 40, 4)
+    assert slim.slim_moe8(a["X"], BF16, None, a["M"], K, K, 300, 40, at(6), at(7), at(8), at(9), at(10), at(11), slim.SLIM_ACT_SILU, at(3), at(4), 4,
+                          a["res"], a["ldr"], a["Y"], BF16, a["ldy"], at(12), need, None) == INV
