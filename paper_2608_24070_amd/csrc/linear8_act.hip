@@ -206,25 +206,22 @@ void launch_sums(const float* part, int64_t blocks, int64_t N, void* out, int dt
   else SLIM_LAUNCH(timer, k_act8_sums<0>, grid, dim3(1024), s, part, blocks, N, out);
 }
 
-// How a product ends: in its own launch, or by fp32 sums in memory and k_act8_rows.
-struct ActPlan {
-  Plan p;
-  bool direct;
-  int64_t blocks;                       // of sums over rows
-  size_t x_bytes, sum_bytes, part_bytes;
-};
+}  // namespace
+
 // The few kernel's blocks have 16 or 32 columns, the narrowest tile's 64.
-ActPlan act_plan(bool bwd, int xdtype, int64_t M, int64_t N, int64_t K, bool groups, bool sums) {
-  ActPlan a;
-  a.p = plan(M, N, K, 3.5 + 2.0 * M * N * 4 / 4e6);      // the sums' way through memory, as tile_time's of one slice more
-  const TileKind& k = kTiles[a.p.kind];
-  a.direct = a.p.few ? !bwd && !groups : a.p.slices == 1 && k.wn > 1;
-  a.sum_bytes = a.direct ? 0 : round256((size_t)a.p.slices * (size_t)M * (size_t)((N + 3) & ~int64_t(3)) * 4);
+SlimActPlan slim_act_plan(bool bwd, int xdtype, int64_t M, int64_t N, int64_t K, bool groups, bool sums) {
+  const Plan p = plan(M, N, K, 3.5 + 2.0 * M * N * 4 / 4e6);      // the sums' way through memory, as tile_time's of one slice more
+  const TileKind& k = kTiles[p.kind];
+  SlimActPlan a{p.few, p.kind, p.slices, p.fours};
+  a.direct = a.few ? !bwd && !groups : a.slices == 1 && k.wn > 1;
+  a.sum_bytes = a.direct ? 0 : round256((size_t)a.slices * (size_t)M * (size_t)((N + 3) & ~int64_t(3)) * 4);
   a.blocks = a.direct ? cdiv(M, 16 * k.fm) : row_plan(M, N).blocks;
   a.part_bytes = sums ? round256((size_t)a.blocks * (size_t)N * 4) : 0;
   a.x_bytes = xdtype == SLIM_Q8_E4M3 ? 0 : code_bytes(M, K) + round256((size_t)M * (size_t)q8_exp_row(K));
   return a;
 }
+
+namespace {
 
 struct Product {
   const uint8_t *X, *ex, *W, *ew;
@@ -232,7 +229,7 @@ struct Product {
 };
 
 template <int FM, int WN, class Fin>
-void launch_act_tile(const Plan& p, const Product& d, float* sums, const Fin& fin, hipStream_t s) {
+void launch_act_tile(const SlimActPlan& p, const Product& d, float* sums, const Fin& fin, hipStream_t s) {
   const int64_t T = cdiv(d.M, 16 * FM) * cdiv(d.N, 64 * WN);
   SlimKernelTimer timer("act8_tile", s);
   SLIM_LAUNCH(timer, (k_act8_tile<FM, WN, Fin>), dim3((unsigned)(8 * cdiv(T, 8)), (unsigned)p.slices), dim3(256), s,
@@ -256,36 +253,36 @@ void launch_few(int few, const Product& d, const Fin& fin, hipStream_t s) {
 }
 
 template <bool BWD, int DT>
-int launch_act(const ActPlan& a, const Product& d, float* sums, const ActArgs& args, hipStream_t s) {
+int launch_act(const SlimActPlan& a, const Product& d, float* sums, const ActArgs& args, hipStream_t s) {
   const ActRows<BWD, DT> fin{args};
   if (a.direct) {
     if constexpr (!BWD)
-      if (a.p.few) {
-        launch_few<SLIM_Q8_E4M3>(a.p.few, d, fin, s);
+      if (a.few) {
+        launch_few<SLIM_Q8_E4M3>(a.few, d, fin, s);
         return SLIM_OK;
       }
-    switch (a.p.kind) {
-      case 0: launch_act_tile<16, 4>(a.p, d, nullptr, fin, s); break;
-      case 1: launch_act_tile<12, 4>(a.p, d, nullptr, fin, s); break;
-      case 2: launch_act_tile<8, 4>(a.p, d, nullptr, fin, s); break;
-      case 3: launch_act_tile<8, 2>(a.p, d, nullptr, fin, s); break;
-      default: launch_act_tile<4, 2>(a.p, d, nullptr, fin, s); break;
+    switch (a.kind) {
+      case 0: launch_act_tile<16, 4>(a, d, nullptr, fin, s); break;
+      case 1: launch_act_tile<12, 4>(a, d, nullptr, fin, s); break;
+      case 2: launch_act_tile<8, 4>(a, d, nullptr, fin, s); break;
+      case 3: launch_act_tile<8, 2>(a, d, nullptr, fin, s); break;
+      default: launch_act_tile<4, 2>(a, d, nullptr, fin, s); break;
     }
     return SLIM_OK;
   }
   const int64_t ld = (d.N + 3) & ~int64_t(3);
   const SumRows out{sums, ld};
-  if (a.p.few) {
-    launch_few<SLIM_Q8_E4M3>(a.p.few, d, out, s);
+  if (a.few) {
+    launch_few<SLIM_Q8_E4M3>(a.few, d, out, s);
   } else {
-    switch (a.p.kind) {
-      case 3: launch_act_tile<8, 2>(a.p, d, sums, out, s); break;
-      case 4: launch_act_tile<4, 2>(a.p, d, sums, out, s); break;
-      case 5: launch_act_tile<4, 1>(a.p, d, sums, out, s); break;
+    switch (a.kind) {
+      case 3: launch_act_tile<8, 2>(a, d, sums, out, s); break;
+      case 4: launch_act_tile<4, 2>(a, d, sums, out, s); break;
+      case 5: launch_act_tile<4, 1>(a, d, sums, out, s); break;
       default: return SLIM_EUNSUPPORTED;      // wide tiles have no slices
     }
   }
-  launch_rows<BWD, DT, true>(sums, ld, a.p.slices, d.M * ld, d.M, args, s);
+  launch_rows<BWD, DT, true>(sums, ld, a.slices, d.M * ld, d.M, args, s);
   return SLIM_OK;
 }
 
@@ -311,9 +308,9 @@ int product_workspace(bool bwd, int xdtype, int64_t M, int64_t N, int64_t K, int
   if (!is_16(dtype)) return SLIM_EDTYPE;
   *bytes = 0;
   if (M == 0 || in_launch(bwd, xdtype, dtype, M, K, groups)) return SLIM_OK;
-  const ActPlan a = act_plan(bwd, xdtype, M, N, K, groups, sums);
-  const TileKind& k = kTiles[a.p.kind];
-  if (!a.p.few && !one_launch(8 * cdiv(cdiv(M, 16 * k.fm) * cdiv(N, 64 * k.wn), 8), 256)) return SLIM_EUNSUPPORTED;
+  const SlimActPlan a = slim_act_plan(bwd, xdtype, M, N, K, groups, sums);
+  const TileKind& k = kTiles[a.kind];
+  if (!a.few && !one_launch(8 * cdiv(cdiv(M, 16 * k.fm) * cdiv(N, 64 * k.wn), 8), 256)) return SLIM_EUNSUPPORTED;
   if (M > kMaxGroups8 / cdiv(N, 128)) return SLIM_EUNSUPPORTED;       // rows kept in 8 bits
   *bytes = a.x_bytes + a.sum_bytes + a.part_bytes;
   return SLIM_OK;
@@ -344,7 +341,7 @@ int product(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int64_t 
     }
     return hipGetLastError() == hipSuccess ? SLIM_OK : SLIM_EDEVICE;
   }
-  const ActPlan a = act_plan(BWD, xdtype, M, N, K, groups, dbias != nullptr);
+  const SlimActPlan a = slim_act_plan(BWD, xdtype, M, N, K, groups, dbias != nullptr);
   char* at = reinterpret_cast<char*>(ws);
   if (xdtype != SLIM_Q8_E4M3) {
     uint8_t* c = reinterpret_cast<uint8_t*>(at);

@@ -87,3 +87,14 @@ bool slim_rows_meet(const SlimRows& a, const SlimRows& b);
 // Whether a launch may write each of `outs` while it reads the others: results apart from each other and from `apart`, and apart from
 // `in_place` or the very rows of one, each element of which the lane that writes it reads before.
 bool slim_may_write(std::initializer_list<SlimRows> outs, std::initializer_list<SlimRows> in_place, std::initializer_list<SlimRows> apart);
+
+// How a product that ends in an activation runs (linear8_act.hip): the few-rows kernel with `few` fragments of rows, or tile kernel `kind`
+// over slices of the reduction of `fours` times four groups; it ends in that launch (direct), or by fp32 sums in memory and a second one.
+struct SlimActPlan {
+  int few, kind, slices, fours;
+  bool direct;
+  int64_t blocks;                       // of sums over rows
+  size_t x_bytes, sum_bytes, part_bytes;
+};
+// groups: results leave in 8 bits, or sums over rows (the backward always).
+SlimActPlan slim_act_plan(bool bwd, int xdtype, int64_t M, int64_t N, int64_t K, bool groups, bool sums);

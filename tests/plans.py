@@ -27,3 +27,22 @@ def plan(kind, m, n, k, r, ws_bytes=1 << 62):
     query = slim.slim_bwd_dx_workspace if kind == "dx" else slim.slim_linear_workspace
     assert p.query == query(m, n, k, r)
     return p
+
+
+class ActPlan(ctypes.Structure):
+    _fields_ = [("few", _int), ("kind", _int), ("slices", _int), ("fours", _int), ("direct", ctypes.c_bool), ("blocks", _i64),
+                ("x_bytes", _size), ("sum_bytes", _size), ("part_bytes", _size)]
+
+
+def act_plan(bwd, m, n, k, groups, sums=False, xdtype=slim.SLIM_Q8_E4M3):
+    """The plan of a product of m rows, n columns and a reduction of k that ends in an activation (`groups`: to 8 bits) or, `bwd`, in its
+    gradient (`sums`: with dbias)."""
+    f = slim.lib()._Z13slim_act_planbilllbb
+    f.argtypes, f.restype = [ctypes.c_bool, _int, _i64, _i64, _i64, ctypes.c_bool, ctypes.c_bool], ActPlan
+    p = f(bwd, xdtype, m, n, k, groups, sums)
+    # the layout above is the library's: its workspace queries agree
+    if xdtype == slim.SLIM_Q8_E4M3:
+        query = (slim.slim_bwd_dx8_act_workspace(xdtype, m, k, n, slim.SLIM_BF16, sums) if bwd
+                 else slim.slim_linear8_act_workspace(xdtype, m, n, k, slim.SLIM_BF16, groups))
+        assert query == p.x_bytes + p.sum_bytes + p.part_bytes
+    return p
