@@ -523,7 +523,9 @@ int slim_linear_hybrid(const void* X, int64_t M, int64_t N, int64_t K, const uin
  * SLIM_EUNSUPPORTED: 2^29 groups in slim_quant8 and slim_dequant8, 2^22 rows of more than 16384 columns
  * in the norms (slim_norm_bwd in fp32: of more than 8192 that are no multiple of 8), 2^36 elements of dY
  * in slim_grad_w8, 2^23 tiles in slim_grad_w8 and 2^24 in slim_linear8 (2^36 results at least) and in the products that end
- * in an activation, 2^32 - 64 groups of dh in slim_act_bwd, 2^24 blocks of 16 rows, 2048 columns and one expert in slim_route.
+ * in an activation, 2^32 - 64 groups of dh in slim_act_bwd, 2^26 - 3 rows or 2^24 blocks of 16 rows, 2048 columns
+ * and one expert in slim_route, 2^24 tiles of 16 columns of h over the experts that slim_moe8's rows may pick (512 experts: F
+ * past 2^19 - 128).
  * Every call is asynchronous, allocates nothing, may be captured into a graph, and gives the same bits for the same
  * inputs.
  * ----
