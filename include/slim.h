@@ -592,8 +592,9 @@ int slim_linear8(const void* X, int xdtype, const uint8_t* xexps, int64_t M, int
  *   dtype       SLIM_F16 or SLIM_BF16, of dU, dmul (row strides lddu, lddmul) and dbias.
  *   dU, dmul    out. Each may be U or mul in 16 bits, in the very place: the same address and row stride. But for that dU, dmul and
  *               dbias share no memory with each other, U, mul or an 8-bit dY (SLIM_EINVAL).
- *   dbias       out, [K] of `dtype`, or NULL. It is as near as the product's sums (2e-5 to 4.5e-5 of its norm), then
- *               rounded; fp32 is not offered for it, as for Y above.
+ *   dbias       out, [K] of `dtype`, or NULL: sums in fp32, rounded once at the end. That rounding is most of its error (bf16's some
+ *               forty times what the product's sums are off, fp16's five times), and past fp16's range it is infinite: where the
+ *               bias's gradient is to be fp32, slim_act_bwd gives it, from a dh that is rounded to 16 bits instead.
  *   ws          slim_bwd_dx8_act_workspace(dydtype, M, N, K, dtype, dbias != NULL) bytes, as above.
  *
  * slim_act_bwd - the same from a dh at hand: dH [M, K] of `dtype`, row stride lddh. dU or dmul may be dH, as above. dbias fp32.
@@ -622,7 +623,8 @@ int slim_act_bwd(const void* dH, int dtype, int64_t lddh, int64_t M, int64_t K, 
  *   ids         out, int32 [M, top]: experts by falling logit, the lower number first where two are equal.
  *   weights     out, fp32 [M, top]: their p.
  *   ws          slim_route_workspace(M, E, K) bytes; its contents need not be kept or cleared.
- * Arithmetic is fp32. A row with a NaN among its logits has weights of NaN, and those experts last that gave it.
+ * Arithmetic is fp32: experts whose logits differ by less than the error of their sums, (K / 256 + 80) 2^-24 of the magnitudes', may
+ * change places. A row with a NaN among its logits has weights of NaN, and those experts last that gave it.
  *
  * slim_moe8 - a layer of experts for a few tokens: y_i = sum_j w_ij down_e(act(gate_e x_i) * (up_e x_i)) (+ residual), e = ids_ij.
  *   X, xdtype   [M, D], M <= 64: SLIM_F16 or SLIM_BF16 with row stride ldx, or SLIM_Q8_E4M3 with xexps, whose values stand for x.
