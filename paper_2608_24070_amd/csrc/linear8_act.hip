@@ -30,9 +30,10 @@ k_act8_few(const uint8_t* __restrict__ X, const uint8_t* __restrict__ ex, int64_
   few_body<FM, NT, 2, XT>(X, ex, ldx, K, W, ew, M, N, G, fin);
 }
 
-// 4096 x 28672 x 8192: 695 us with nothing added (the bare product 695), silu 703, gelu_tanh 707, gelu 742, gelu to 8 bits 762, its
-// argument too 794; backward with a gate, from 8 bits, 818: bound in its end by the instructions of
-// one wave a SIMD (tiles that start apart, so that their memory traffic does not meet, took as long).
+// 4096 x 28672 x 8192 on one card: 673 to 712 us with nothing added (the bare product 645 to 712, by what ran before: power), with a bias
+// relu 680, silu 688, gelu_tanh 695, gelu 729, gelu to 8 bits 742, its argument too 773; backward of silu from 8 bits 738, with a gate
+// 794: bound in its end by the instructions of one wave a SIMD (tiles that start apart, so that their memory traffic does not meet,
+// took as long).
 // What ends the rows is some thirty scalars, which the loop has no registers for: they are read from the launch's arguments anew
 // after it (a copy behind an opaque address, which the compiler cannot move up; held over the loop they were spilled).
 template <class Fin>
@@ -64,7 +65,7 @@ k_act8_tile(TileCall<Fin> c) {
 
 // Ends rows whose sums (`slices` of them, fp32 [M][N up to 4] each, added in slice order) or whose dh (16 bits) lie in memory: `lpr`
 // lanes take a row of 8 lpr columns, a block the rows r0 .. r0 + per, two of a lane's in flight while two are ended.
-// Bound by HBM: the gradient of gelu_tanh from 8 bits over 8192 x 28672, with sums over rows, 245 us (4.8 TB/s; four rows at a
+// Bound by HBM: the gradient of gelu_tanh from 8 bits over 8192 x 28672, with sums over rows, 243 us (4.9 TB/s; four rows at a
 // time without any ahead 268).
 template <bool BWD, int DT, bool SUMS>
 __global__ void __launch_bounds__(256, 2)

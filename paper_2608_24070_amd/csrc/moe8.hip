@@ -435,8 +435,9 @@ SLIM_DEV void up_groups(const uint8_t* X, const uint8_t* xe, int64_t ldx, const 
 // waves, whose sums are added through LDS in wave order. h leaves as the sum of two bf16 values, 16 significant bits in fp32's range:
 // hi [pairs][F up to 128], then lo. GATED: whether there is an up. (A template's parameter: with a branch on w.up between the gate's
 // products and the reads of their results the compiler leaves out the wait states that the way past the up's products needs.)
-// Bound by the weights' bytes: 7 rows, 2 of 8 experts, 4096 x 11008 144 us (4.3 TB/s from memory, where a plain reduction of 1 GiB reads
-// 4.6); 8 of 64 of 4096 x 1024 for one row 19 us (3.5), as one of many calls: a block's first loads wait for its slot.
+// Bound by the weights' bytes: 7 rows, 2 of 8 experts, 4096 x 11008 95 to 101 us where 6 of the eight are picked, 123 to 145 where all are (4.9
+// to 5.9 TB/s; more where calls on two sets of weights take turns); 8 of 64 of 4096 x 1024 for one row 17 to 19 us (3.9 to 3.5), as one of
+// many calls: a block's first loads wait for its slot.
 template <int XT, bool GATED>
 __global__ void __launch_bounds__(256, 2)
 k_moe_up(const uint8_t* __restrict__ X, const uint8_t* __restrict__ xe, int64_t ldx, Experts w, Picks picks, uint16_t* __restrict__ hi,
@@ -570,8 +571,8 @@ SLIM_DEV void down_groups(const u32x4_t* hi, const u32x4_t* lo, const Picks& pic
 // y = sum over the slots of weight * (down h): a block takes 16 NT columns of y and one of `parts` parts of all slots' groups of 128; its
 // W waves take consecutive ones, and add each expert's results to sums of their own in LDS, which are added in wave order. With one
 // part y leaves (with the residual), else its fp32 sums. (Eight tiles of a weight share one row of exponents, and NT divides eight.)
-// 7 rows, 2 of 8, 4096 x 11008 54 us with its sum (5.3 TB/s), 61 rows, 4 of 40, 5120 x 1700 86 (4.1); one row, 8 of 64, 4096 x 1024
-// 12.6 (2.7): eight groups a wave, one round of loads.
+// 7 rows, 2 of 8, 4096 x 11008 54 us where 6 of the eight are picked, 69 to 82 where all are (4.4 to 5.2 TB/s), and 4 for the parts' sum; 61 rows,
+// 4 of 40, 5120 x 1700, 39 picked, 80 to 90 (3.8 to 4.1); one row, 8 of 64, 4096 x 1024 12.6 (2.7): eight groups a wave, one round of loads.
 template <int DT, int NT, int W>
 __global__ void __launch_bounds__(64 * W, W == 4 ? 2 : 1)
 k_moe_down(const u32x4_t* __restrict__ hi, const u32x4_t* __restrict__ lo, Experts w, Picks picks, int slots, int M, int parts,
@@ -669,7 +670,7 @@ void launch_logits(const void* X, const uint8_t* xe, int64_t ldx, const void* Wr
   SlimKernelTimer timer("route_logits", s);
   const int parts = (int)cdiv(K, kRouteCols);
   // few rows: a block for every expert and two of them, which is all latency (7 x 8 x 4096 3.9 us against 7.7); more: the router's values
-  // are kept over 16 rows (61 x 250 x 8192, fp32 router: 16 us; over all 61 rows, in a quarter of the blocks, 37)
+  // are kept over 16 rows (61 x 250 x 8192, fp32 router: 15 us; over all 61 rows, in a quarter of the blocks, 37; 8192 x 64 x 4096, 156)
   if (M >= 8)
     SLIM_LAUNCH(timer, (k_route_logits<XT, WT, 8, 4>), dim3((unsigned)(cdiv(M, route_rows(8)) * parts * cdiv(E, 4))), dim3(256), s, X, xe, ldx, Wr,
                 ldw, M, (int)K, E, parts, logits);
