@@ -1119,7 +1119,8 @@ def linear8_act(X, p: dict, act: str = "none", bias=None, mul=None, residual=Non
                 out=None, ws=None, stream=None):
     """slim_linear8_act: Y [M, N] = act(X W^T + bias) * mul + residual with an 8-bit weight (pack8), X as in linear8. `act`: "none",
     "relu", "gelu", "gelu_tanh" or "silu"; bias [N] of any float type; mul and residual [M, N] of `dtype` (fp16 or bf16; default
-    theirs, else as linear8). Y in `dtype`, or with `q8` 8-bit rows. With `pre`: (Y, X W^T + bias), the second like Y, for the backward."""
+    theirs, else as linear8). Y in `dtype`, or with `q8` 8-bit rows. With `pre`: (Y, X W^T + bias), the second like Y, for the backward. A 16-bit
+    `out` may be mul or residual itself; it may share no other memory with the operands."""
     if stream is not None:
         return _on_its_stream(stream, linear8_act, X, p, act, bias, mul, residual, pre, q8, dtype, out, ws)
     N, K, a = p["N"], p["K"], _act_code(act)
@@ -1181,7 +1182,8 @@ def _kept_operands(u, mul, M: int, K: int, dtype, dev: int):
 def bwd_dx8_act(dY, p: dict, u, act: str = "none", mul=None, bias: bool = False, dtype=None, out=None, ws=None, stream=None):
     """slim_bwd_dx8_act: (du, dmul, dbias) from dY [M, N] of a product Y = h W^T with h = act(u) * mul: with dh = dY W (pack8 with
     bwd=True) du = dh * mul * act'(u), dmul = dh * act(u) (None without mul), dbias [K] = the sums of du's columns (None unless
-    `bias`), all of `dtype` (default out's or u's, else as linear8). u and mul [M, K]: of `dtype`, or 8-bit rows."""
+    `bias`), all of `dtype` (default out's or u's, else as linear8). u and mul [M, K]: of `dtype`, or 8-bit rows. `out`, du's place,
+    may be a 16-bit u or mul itself; it may share no other memory with them or with a dY of 8-bit rows."""
     if stream is not None:
         return _on_its_stream(stream, bwd_dx8_act, dY, p, u, act, mul, bias, dtype, out, ws)
     N, K, a = p["N"], p["K"], _act_code(act)
@@ -1211,7 +1213,8 @@ def bwd_dx8_act(dY, p: dict, u, act: str = "none", mul=None, bias: bool = False,
 
 
 def act_bwd(dh, u, act: str = "none", mul=None, bias: bool = False, out=None, ws=None, stream=None):
-    """slim_act_bwd: (du, dmul, dbias) as bwd_dx8_act's from a dh [M, K] at hand (fp16 or bf16), of whose type they are; dbias fp32."""
+    """slim_act_bwd: (du, dmul, dbias) as bwd_dx8_act's from a dh [M, K] at hand (fp16 or bf16), of whose type they are; dbias fp32.
+    `out`, du's place, may be dh or a 16-bit u or mul itself; it may share no other memory with them."""
     if stream is not None:
         return _on_its_stream(stream, act_bwd, dh, u, act, mul, bias, out, ws)
     M, K, ldh, dev = _matrix(dh, "dh")
@@ -1311,7 +1314,8 @@ def moe8(X, gate: dict, up: dict | None, down: dict, ids, weights, act: str = "s
          stream=None):
     """slim_moe8: Y [M, D] = sum over a row's experts e of weight * down_e(act(gate_e x) * (up_e x)) (+ residual) for up to 64 rows X
     [M, D] (fp16, bf16 or 8-bit rows). gate, up (or None) and down: pack8_experts of [E, F, D], [E, F, D], [E, D, F]; ids int32 and
-    weights fp32 [M, top] as route's. Y in `dtype`, fp16 or bf16 (default X's type; bf16 for 8-bit rows)."""
+    weights fp32 [M, top] as route's. Y in `dtype`, fp16 or bf16 (default X's type; bf16 for 8-bit rows). `out`
+    may be X, or the residual itself; it may share no other memory with the residual, ids or weights."""
     if stream is not None:
         return _on_its_stream(stream, moe8, X, gate, up, down, ids, weights, act, residual, dtype, out, ws)
     torch = _torch()
